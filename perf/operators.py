@@ -216,9 +216,7 @@ def prepare(case, seed):
             s.opt = B.decode_options(case["g"], s.max_length, scale=D ** -0.5, softcap=case["softcap"], accumulate=case["accumulate"])
             s.ws = B.alloc_paged_attention_workspace(s.cache, s.opt)
         else:
-            seqlens = lens if case["op"] == "fill" else [case["block"]] * batch
-            s.shape = B.Shape(layers, heads, D, 48, seqlens)
-            s.ws = B.alloc_paged_fill_workspace(s.shape)
+            s.shape = B.Shape(layers, heads, D, 48, lens if case["op"] == "fill" else [case["block"]] * batch)
     return s
 
 
@@ -315,13 +313,14 @@ def _plain_evict(s):
     j = torch.arange(e, device=dev).repeat(units)
     _plain_put(s, s.k_in.view(layers * heads, -1, D), s.v_in.view(layers * heads, -1, D), s.mass_in.view(layers * heads, -1),
                s.next_position.long(), j, unit, budget[unit] + j, (unit % batch) * e + j)
+    s.next_position += e
     # rank: recent tokens first, then by weight, then by slot
     slot = torch.arange(min(s.max_length, s.table.shape[-1] * page), device=dev)
     rows = _slot_rows(s.table.view(units, -1), page, slot).clamp(min=0)
     live = slot < (budget + e).unsqueeze(1)
     w, pos = s.mass.view(-1)[rows], torch.where(live, s.positions.view(-1)[rows].long(), -1)
     recent = torch.minimum(torch.tensor(c["recent"], device=dev), budget).unsqueeze(1)
-    w = torch.where(pos > pos.amax(1, keepdim=True) - recent, math.inf, w)
+    w = torch.where(pos >= s.next_position.long().repeat(layers * heads).unsqueeze(1) - recent, math.inf, w)
     order = torch.where(live, w, -1.0).sort(dim=1, descending=True, stable=True).indices
     kept = torch.zeros_like(live).scatter_(1, order, slot < budget.unsqueeze(1))
     # the j-th hole among the first `budget` slots takes the j-th token that is kept behind them
@@ -332,7 +331,6 @@ def _plain_evict(s):
     k, v, m, p = (x[frm] for x in for_all)
     for_all[0][to], for_all[1][to], for_all[2][to], for_all[3][to] = k, v, m, p
     s.lengths_out.copy_(s.budgets)
-    s.next_position += e
 
 
 def run(s):
@@ -346,12 +344,12 @@ def run(s):
                 B.paged_attention(s.cache, 0, s.opt, s.q, s.lengths, s.out, s.ws, lse_out=s.lse)
             return {"out": s.out, "lse": s.lse, "mass": s.mass, "positions": s.positions, "k_pages": s.k_pages, "v_pages": s.v_pages}
         if c["op"] == "fill":
-            B.paged_fill(s.cache, s.shape, s.k, s.v, s.keep, s.ws, idx=s.idx, head_offsets=s.head_offsets, mass_in=s.attn,
+            B.paged_fill(s.cache, s.shape, s.k, s.v, s.keep, idx=s.idx, head_offsets=s.head_offsets, mass_in=s.attn,
                          first_position=s.first_position, lengths_out=s.lengths_out)
         else:
-            B.paged_fill(s.cache, s.shape, s.k_in, s.v_in, s.shape.seqlens, s.ws, mass_in=s.mass_in, first_position=s.next_position, lengths=s.budgets)
-            B.paged_evict(s.cache, s.full, s.budgets, s.lengths_out, s.max_length, recent=c["recent"])
+            B.paged_fill(s.cache, s.shape, s.k_in, s.v_in, s.shape.seqlens, mass_in=s.mass_in, first_position=s.next_position, lengths=s.budgets)
             s.next_position += c["block"]
+            B.paged_evict(s.cache, s.full, s.budgets, s.lengths_out, s.max_length, recent=c["recent"], next_position=s.next_position)
     elif c["op"] == "attention":
         return _plain_attention(s)
     elif c["op"] == "fill":
