@@ -59,6 +59,8 @@ extern "C" {
 #define COMPACTOR_STATUS_NONFINITE   1
 #define COMPACTOR_STATUS_RANK        2
 #define COMPACTOR_STATUS_TIMEOUT     4
+#define COMPACTOR_STATUS_PAGE        8    /* a page that is none (paged cache)           */
+#define COMPACTOR_STATUS_CAPACITY   16    /* a length beyond the unit's pages            */
 
 /* Small factorisations for compactor_score_variant (Appendix C). */
 #define COMPACTOR_FACTOR_CHOLESKY    0    /* G = L L^T: the R factor of the QR route          */
@@ -360,6 +362,134 @@ int compactor_compress_full(const compactor_shape* shape, const compactor_option
                             const float* phi, const int32_t* keep_counts, float* scores_out,
                             int32_t* idx_out, int32_t* head_offsets_out, void* k_out, void* v_out,
                             int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Paged cache: what the retained rows live in while a model decodes.  The paper compresses a prefill and
+ * leaves the cache to the engine around it; since heads keep different tokens (and, selected across
+ * heads, different numbers of them), every unit has a row of the page table and a length of its own.
+ *   k_pages, v_pages  device bf16; row (page p, slot s) is the d elements at p * stride_page + s * stride_token
+ *                     of either pool.  16-byte aligned; strides in elements, multiples of 8, stride_token >= d,
+ *                     stride_page >= page_tokens * stride_token.  A pool may exceed 2^32 elements.
+ *   mass              device fp32 [n_pages][page_tokens] or NULL: accumulated attention weight per slot.
+ *   positions         device int32 [n_pages][page_tokens] or NULL: position of the slot's token.
+ *   page_table        device int32 [layers*heads*batch][max_pages]: token t of unit u lies in slot
+ *                     t % page_tokens of page page_table[u][t / page_tokens].  Entries behind a unit's
+ *                     last token are not read.  A page that is written (filled, appended to, accumulated
+ *                     into or evicted from) must belong to one unit only and occur once in its row; pages that
+ *                     are only read may be shared.
+ *   page_tokens       a power of two, 8..1024.  d must be 128.
+ * Lengths are device int32 [layers*heads*batch] arrays of the caller, indexed by unit id, so that a recorded
+ * call follows them; a negative length marks a row without a sequence: it is neither read nor written.
+ * The calls do not change lengths except through their lengths_out arguments.  Slots behind a unit's last
+ * token keep what they hold and may hold anything, not-a-number included.
+ * `status` (device int32 [layers*heads*batch], may be NULL): the entries of the layers of a call are cleared when
+ * it starts; COMPACTOR_STATUS_PAGE = a page id outside [0, n_pages) was met where a row was needed,
+ * COMPACTOR_STATUS_CAPACITY = the unit's tokens do not fit its pages (or max_length).
+ * Calls that share pages, lengths or a workspace are ordered by the caller (one stream, or events); two calls on
+ * different layers may run at once if their workspaces differ.
+ */
+typedef struct compactor_paged_cache {
+    void* k_pages;
+    void* v_pages;
+    int64_t stride_page;
+    int64_t stride_token;
+    float* mass;
+    int32_t* positions;
+    const int32_t* page_table;
+    int32_t n_pages;
+    int32_t page_tokens;
+    int32_t max_pages;
+    int32_t layers;
+    int32_t heads;            /* KV heads */
+    int32_t batch;
+    int32_t d;
+} compactor_paged_cache;
+
+/* One row of d elements per (sequence, head): bf16, 16-byte aligned, strides in elements, multiples of 8. */
+typedef struct compactor_rows {
+    void* ptr;
+    int64_t stride_seq;
+    int64_t stride_head;
+} compactor_rows;
+
+/*
+ * Compaction into pages: the counterpart of compactor_compact / compactor_compact_across_heads for a paged
+ * cache.  Row j of a unit's kept rows goes to slot lengths[u] + j as a bit copy.
+ *   shape         the prefill (heads and batch those of the cache); its layers go to the cache's layers
+ *                 first_layer .. first_layer + shape->layers - 1.  m is not used (any valid value).
+ *   idx           device int32 in the layout of compactor_select, or of compactor_select_across_heads when
+ *                 head_offsets is given; NULL (without head_offsets): rows 0 .. keep_counts[b] - 1 of every
+ *                 sequence, i.e. the tokens are appended as they are.
+ *   head_offsets  device int32 [shape->layers][batch][heads + 1] from compactor_select_across_heads, or NULL.
+ *   keep_counts   HOST int32 [batch], as in compactor_compact.
+ *   mass_in       device fp32 [shape->layers][heads][total_tokens] (the attention term of Eq. 5 without
+ *                 pooling, say) or NULL: the slots' accumulated weight starts at mass_in[token], else 0.
+ *   first_position device int32 [batch] or NULL (0): the slots' positions are first_position[b] + token index.
+ *   lengths       device int32 [units of the cache] or NULL (all 0): tokens a unit holds before the call.
+ *   lengths_out   the same layout or NULL, may be `lengths`: tokens it holds after it (entries of other layers are
+ *                 left alone).
+ * A unit whose rows do not all fit its pages is left alone (COMPACTOR_STATUS_CAPACITY, length unchanged); rows whose
+ * index lies outside [0, length of the sequence) are skipped and leave their slot untouched; rows whose
+ * page is none are skipped (COMPACTOR_STATUS_PAGE).  No workspace.
+ */
+int compactor_paged_fill(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape,
+                         compactor_mat k_cache, compactor_mat v_cache, const int32_t* idx,
+                         const int32_t* head_offsets, const int32_t* keep_counts, const float* mass_in,
+                         const int32_t* first_position, const int32_t* lengths, int32_t* lengths_out,
+                         int32_t* status, void* stream);
+
+/*
+ * Attention of one new token per sequence over one layer of a paged cache:
+ *   y_j = scale q.k_j, capped as softcap * tanh(y_j / softcap) when softcap > 0;  p = softmax(y);
+ *   out = sum_j p_j v_j;  lse = log sum_j exp(y_j).
+ *   q, out       rows [batch][heads * q_per_kv]; query head j of KV head h is head h * q_per_kv + j.
+ *                1 <= q_per_kv <= 64.  Rows of out must not overlap.
+ *   k_new, v_new rows [batch][heads] of the new token (or both ptr NULL: attend to the cached tokens only).  The
+ *                token is attended to and written to slot lengths[u] of its unit (its page must be in the table), with position
+ *                new_positions[b] (device int32 [batch]; NULL: the slot's number).  `lengths` is not
+ *                changed: all layers of a step see the same lengths, the caller adds 1 after the last.
+ *   lengths      device int32 [units of the cache]: cached tokens, without the new one.
+ *   lse_out      device fp32 [batch][heads * q_per_kv] or NULL.
+ *   options (HOST): q_per_kv, scale (> 0), softcap (0: none), accumulate, and max_length, the most tokens a unit may have
+ *                in this call, the new one included (what lies beyond the table's pages does not count).
+ *                accumulate != 0 adds sum over the KV head's query heads of p_j to the weight of every cached
+ *                token (cache->mass) and sets the new token's; otherwise the new token's is set to 0.
+ * A unit without tokens (or with a negative length, or beyond its capacity: COMPACTOR_STATUS_CAPACITY) gives zero rows and
+ * lse = -inf.  Tokens on a page that is none are left out (COMPACTOR_STATUS_PAGE).
+ * Scores and sums are fp32; weights are rounded to bf16 for the product with V only.  Results do not depend on
+ * timing: a unit's partial sums are joined in a fixed order.
+ * Workspace: compactor_paged_attention_workspace_bytes(), 256-byte aligned, contents not preserved; 0 = bad arguments.
+ */
+typedef struct compactor_decode_options {
+    int32_t q_per_kv;
+    int32_t max_length;
+    float   scale;
+    float   softcap;
+    int32_t accumulate;
+} compactor_decode_options;
+size_t compactor_paged_attention_workspace_bytes(const compactor_paged_cache* cache, const compactor_decode_options* options);
+int compactor_paged_attention(const compactor_paged_cache* cache, int32_t layer, const compactor_decode_options* options,
+                              compactor_rows q, compactor_rows k_new, compactor_rows v_new, const int32_t* new_positions,
+                              const int32_t* lengths, compactor_rows out, float* lse_out, int32_t* status,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction by accumulated attention weight, for the units of `layers` layers from first_layer on.  A unit
+ * with n = lengths[u] tokens and a budget B = budgets[u] (device int32 [units of the cache]) with 0 <= B < n keeps B
+ * tokens: those whose position is at least next_position[b] - min(recent, B), then those of the greatest weight;
+ * of equal weights the lower slots stay.  Not-a-number ranks above +inf.  (If more tokens than B are that recent, which takes repeated
+ * positions, the lower slots of them stay.)  The others leave, and the holes they leave in slots [0, B) are filled from
+ * behind: the j-th evicted slot below B receives row, weight and position of the j-th kept slot at or above B.  Slots
+ * from B on keep what they hold.  lengths_out[u] (may be `lengths`; the entries of other layers are left alone) becomes B.
+ * A unit with n <= B, a negative length or a negative budget stays as it is, lengths_out[u] = lengths[u]; so does one with
+ * n > max_length or beyond its pages (COMPACTOR_STATUS_CAPACITY) and one with a page that is none (COMPACTOR_STATUS_PAGE).
+ *   next_position  device int32 [batch]; may be NULL when recent = 0.
+ *   max_length     the most tokens a unit may have, at most 393216 (COMPACTOR_E_TOO_LARGE beyond).
+ * cache->mass is required, cache->positions when recent > 0.  No workspace.
+ */
+int compactor_paged_evict(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* lengths,
+                          const int32_t* budgets, const int32_t* next_position, int32_t recent, int32_t max_length,
+                          int32_t* lengths_out, int32_t* status, void* stream);
 
 /*
  * compactor_score for callers that cannot allocate device memory (the paper has no counterpart;

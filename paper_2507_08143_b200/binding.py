@@ -29,6 +29,21 @@ class CompactorOptions(Structure):
                 ("q_per_kv", c_int32), ("chunk", c_int32), ("scale", c_float), ("pool", c_int32)]
 
 
+class CompactorPagedCache(Structure):
+    _fields_ = [("k_pages", c_void_p), ("v_pages", c_void_p), ("stride_page", c_int64), ("stride_token", c_int64),
+                ("mass", c_void_p), ("positions", c_void_p), ("page_table", c_void_p),
+                ("n_pages", c_int32), ("page_tokens", c_int32), ("max_pages", c_int32),
+                ("layers", c_int32), ("heads", c_int32), ("batch", c_int32), ("d", c_int32)]
+
+
+class CompactorRows(Structure):
+    _fields_ = [("ptr", c_void_p), ("stride_seq", c_int64), ("stride_head", c_int64)]
+
+
+class CompactorDecodeOptions(Structure):
+    _fields_ = [("q_per_kv", c_int32), ("max_length", c_int32), ("scale", c_float), ("softcap", c_float), ("accumulate", c_int32)]
+
+
 class CompactorError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -79,6 +94,16 @@ def _load() -> ctypes.CDLL:
     lib.compactor_compress_full.argtypes = [POINTER(CompactorShape), POINTER(CompactorOptions), CompactorMat, CompactorMat,
                                             CompactorMat, CompactorMat, c_void_p, POINTER(c_int32), c_void_p, c_void_p,
                                             c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.compactor_paged_fill.argtypes = [POINTER(CompactorPagedCache), c_int32, POINTER(CompactorShape), CompactorMat, CompactorMat,
+                                         c_void_p, c_void_p, POINTER(c_int32), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                         c_void_p]
+    lib.compactor_paged_attention_workspace_bytes.restype = c_size_t
+    lib.compactor_paged_attention_workspace_bytes.argtypes = [POINTER(CompactorPagedCache), POINTER(CompactorDecodeOptions)]
+    lib.compactor_paged_attention.argtypes = [POINTER(CompactorPagedCache), c_int32, POINTER(CompactorDecodeOptions), CompactorRows,
+                                              CompactorRows, CompactorRows, c_void_p, c_void_p, CompactorRows, c_void_p, c_void_p,
+                                              c_void_p, c_size_t, c_void_p]
+    lib.compactor_paged_evict.argtypes = [POINTER(CompactorPagedCache), c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32,
+                                          c_int32, c_void_p, c_void_p, c_void_p]
     lib.compactor_wait_selftest.argtypes = [c_void_p, c_void_p]
     lib.compactor_builtin_scratch_bytes.restype = c_size_t
     lib.compactor_score_builtin_scratch.argtypes = [POINTER(CompactorShape), CompactorMat, c_void_p, c_void_p, c_float,
@@ -94,7 +119,8 @@ EXPORTS = ["compactor_version", "compactor_error_string", "compactor_make_sketch
            "compactor_compact", "compactor_compress", "compactor_compress_profiled",
            "compactor_builtin_scratch_bytes", "compactor_score_builtin_scratch", "compactor_attention_scores", "compactor_attention_scores_status", "compactor_wait_selftest",
            "compactor_across_heads_workspace_bytes", "compactor_select_across_heads", "compactor_compact_across_heads",
-           "compactor_score_variant", "compactor_nll", "compactor_compress_full_workspace_bytes", "compactor_compress_full"]
+           "compactor_score_variant", "compactor_nll", "compactor_compress_full_workspace_bytes", "compactor_compress_full",
+           "compactor_paged_fill", "compactor_paged_attention_workspace_bytes", "compactor_paged_attention", "compactor_paged_evict"]
 
 FACTOR_CHOLESKY = 0
 FACTOR_EIG = 1
@@ -333,6 +359,140 @@ def compress_full(shape: Shape, opt: CompactorOptions, q: Optional[torch.Tensor]
                                        _keep_array(keep_counts), _ptr(scores_out), _ptr(idx_out), _ptr(head_offsets_out),
                                        _ptr(k_out), _ptr(v_out), _ptr(status), _ptr(workspace), workspace.numel(),
                                        _stream()), "compactor_compress_full")
+
+
+class PagedCache:
+    """A paged cache (compactor_paged_cache) over the caller's tensors, which it keeps alive.
+
+    k_pages, v_pages  bf16 [n_pages, page_tokens, d], same strides, contiguous along d; views of larger tensors are fine.
+    page_table        int32 [layers, heads, batch, max_pages], contiguous.
+    mass, positions   fp32 / int32 [n_pages, page_tokens], contiguous, or None."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                 mass: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
+        if k_pages.dim() != 3 or k_pages.dtype != torch.bfloat16 or v_pages.dtype != torch.bfloat16 or \
+                k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride() or k_pages.stride(2) != 1:
+            raise ValueError("k_pages and v_pages: bf16 [n_pages, page_tokens, d] with the same strides, contiguous along d")
+        if page_table.dim() != 4 or page_table.dtype != torch.int32 or not page_table.is_contiguous():
+            raise ValueError("page_table: contiguous int32 [layers, heads, batch, max_pages]")
+        for t, dtype, name in ((mass, torch.float32, "mass"), (positions, torch.int32, "positions")):
+            if t is not None and (t.dtype != dtype or t.shape != k_pages.shape[:2] or not t.is_contiguous()):
+                raise ValueError(f"{name}: contiguous {dtype} [n_pages, page_tokens]")
+        self.tensors = (k_pages, v_pages, page_table, mass, positions)
+        self.device = k_pages.device
+        if any(t is not None and t.device != self.device for t in self.tensors):
+            raise ValueError("the tensors of a cache live on one device")
+        self.layers, self.heads, self.batch, self.max_pages = page_table.shape
+        self.n_pages, self.page_tokens, self.d = k_pages.shape
+        self.units = self.layers * self.heads * self.batch
+        self.c = CompactorPagedCache(k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride(0), k_pages.stride(1),
+                                     None if mass is None else mass.data_ptr(), None if positions is None else positions.data_ptr(),
+                                     page_table.data_ptr(), self.n_pages, self.page_tokens, self.max_pages,
+                                     self.layers, self.heads, self.batch, self.d)
+
+    def _stream(self) -> c_void_p:
+        if self.device.type != "cuda" or self.device.index != torch.cuda.current_device():
+            raise ValueError(f"the cache lives on {self.device}, which is not the current CUDA device")
+        return _stream()
+
+    def _per_unit(self, t: Optional[torch.Tensor], name: str) -> Optional[int]:
+        """Address of an int32 [layers, heads, batch] array (any shape of that many elements)."""
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or t.numel() != self.units or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{name}: contiguous int32, one entry per (layer, head, sequence), on the cache's device")
+        return t.data_ptr()
+
+    def _per_sequence(self, t: Optional[torch.Tensor], name: str) -> Optional[int]:
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or t.numel() != self.batch or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{name}: contiguous int32 [batch] on the cache's device")
+        return t.data_ptr()
+
+    def _rows(self, t: torch.Tensor, heads: int, name: str) -> CompactorRows:
+        if t.dtype != torch.bfloat16 or t.shape != (self.batch, heads, self.d) or t.stride(2) != 1 or t.device != self.device:
+            raise ValueError(f"{name}: bf16 [{self.batch}, {heads}, {self.d}], contiguous along the last axis, on the cache's device")
+        return CompactorRows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+_NO_ROWS = CompactorRows(None, 0, 0)
+
+
+def paged_fill(cache: PagedCache, shape: Shape, k_cache: torch.Tensor, v_cache: torch.Tensor, keep_counts: Sequence[int],
+               idx: Optional[torch.Tensor] = None, head_offsets: Optional[torch.Tensor] = None,
+               mass_in: Optional[torch.Tensor] = None, first_position: Optional[torch.Tensor] = None,
+               lengths: Optional[torch.Tensor] = None, lengths_out: Optional[torch.Tensor] = None, first_layer: int = 0,
+               status: Optional[torch.Tensor] = None) -> None:
+    """Compaction into pages: the kept rows (`idx`, and `head_offsets` after a selection across heads; without `idx` the first
+    keep_counts[b] rows of every sequence) of k_cache / v_cache [layers, heads, tokens, d] go behind `lengths`."""
+    stream = cache._stream()
+    total, kept = shape.total_tokens, sum(int(k) for k in keep_counts)
+    want = (shape.layers, shape.heads, total, shape.d)
+    if len(keep_counts) != shape.batch:
+        raise ValueError("keep_counts: one per sequence")
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if t.shape != want or t.device != cache.device:
+            raise ValueError(f"{name}: {want} on the cache's device")
+    for t, dtype, n, name in ((idx, torch.int32, shape.layers * shape.heads * kept, "idx"),
+                              (head_offsets, torch.int32, shape.layers * shape.batch * (shape.heads + 1), "head_offsets"),
+                              (mass_in, torch.float32, shape.layers * shape.heads * total, "mass_in")):
+        if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != cache.device):
+            raise ValueError(f"{name}: contiguous {dtype} of {n} elements on the cache's device")
+    _check(LIB.compactor_paged_fill(byref(cache.c), first_layer, byref(shape.c), mat(k_cache), mat(v_cache), _ptr(idx),
+                                    _ptr(head_offsets), _keep_array(keep_counts), _ptr(mass_in),
+                                    cache._per_sequence(first_position, "first_position"), cache._per_unit(lengths, "lengths"),
+                                    cache._per_unit(lengths_out, "lengths_out"), cache._per_unit(status, "status"), stream),
+           "compactor_paged_fill")
+
+
+def decode_options(q_per_kv: int, max_length: int, scale: float = 128 ** -0.5, softcap: float = 0.0,
+                   accumulate: bool = False) -> CompactorDecodeOptions:
+    return CompactorDecodeOptions(q_per_kv, max_length, scale, softcap, 1 if accumulate else 0)
+
+
+def paged_attention_workspace_bytes(cache: PagedCache, opt: CompactorDecodeOptions) -> int:
+    return int(LIB.compactor_paged_attention_workspace_bytes(byref(cache.c), byref(opt)))
+
+
+def alloc_paged_attention_workspace(cache: PagedCache, opt: CompactorDecodeOptions) -> torch.Tensor:
+    return torch.empty(max(256, paged_attention_workspace_bytes(cache, opt)), dtype=torch.uint8, device=cache.device)
+
+
+def paged_attention(cache: PagedCache, layer: int, opt: CompactorDecodeOptions, q: torch.Tensor, lengths: torch.Tensor,
+                    out: torch.Tensor, workspace: torch.Tensor, k_new: Optional[torch.Tensor] = None,
+                    v_new: Optional[torch.Tensor] = None, new_positions: Optional[torch.Tensor] = None,
+                    lse_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
+    """Attention of one new token per sequence: q, out [batch, heads * q_per_kv, d], k_new, v_new [batch, heads, d],
+    lse_out fp32 [batch, heads * q_per_kv]; `lengths` [layers, heads, batch] without the new token, left as it is."""
+    stream = cache._stream()
+    q_heads = cache.heads * opt.q_per_kv
+    if lse_out is not None and (lse_out.dtype != torch.float32 or lse_out.numel() != cache.batch * q_heads or
+                                not lse_out.is_contiguous() or lse_out.device != cache.device):
+        raise ValueError("lse_out: contiguous fp32 [batch, heads * q_per_kv] on the cache's device")
+    if workspace.device != cache.device or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous, on the cache's device")
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new come together")
+    _check(LIB.compactor_paged_attention(byref(cache.c), layer, byref(opt), cache._rows(q, q_heads, "q"),
+                                         _NO_ROWS if k_new is None else cache._rows(k_new, cache.heads, "k_new"),
+                                         _NO_ROWS if v_new is None else cache._rows(v_new, cache.heads, "v_new"),
+                                         cache._per_sequence(new_positions, "new_positions"), cache._per_unit(lengths, "lengths"),
+                                         cache._rows(out, q_heads, "out"), None if lse_out is None else lse_out.data_ptr(),
+                                         cache._per_unit(status, "status"), workspace.data_ptr(), workspace.nbytes, stream),
+           "compactor_paged_attention")
+
+
+def paged_evict(cache: PagedCache, lengths: torch.Tensor, budgets: torch.Tensor, lengths_out: torch.Tensor, max_length: int,
+                recent: int = 0, next_position: Optional[torch.Tensor] = None, first_layer: int = 0, layers: Optional[int] = None,
+                status: Optional[torch.Tensor] = None) -> None:
+    """Evicts every unit that holds more than its budget down to it: the `recent` newest tokens and those of the greatest
+    accumulated weight stay.  lengths, budgets, lengths_out: int32 [layers, heads, batch]; lengths_out may be lengths."""
+    _check(LIB.compactor_paged_evict(byref(cache.c), first_layer, cache.layers - first_layer if layers is None else layers,
+                                     cache._per_unit(lengths, "lengths"), cache._per_unit(budgets, "budgets"),
+                                     cache._per_sequence(next_position, "next_position"), recent, max_length,
+                                     cache._per_unit(lengths_out, "lengths_out"), cache._per_unit(status, "status"),
+                                     cache._stream()), "compactor_paged_evict")
 
 
 def wait_selftest() -> int:

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "paged.cuh"
 #include "sm100.cuh"
 
 using namespace compactor;
@@ -486,10 +487,10 @@ const char* compactor_error_string(int code) {
     switch (code) {
         case COMPACTOR_OK: return "ok";
         case COMPACTOR_E_INVALID_ARGUMENT: return "invalid argument";
-        case COMPACTOR_E_UNSUPPORTED: return "unsupported shape (d must be 128, 1 <= m <= 128)";
+        case COMPACTOR_E_UNSUPPORTED: return "unsupported shape (d must be 128, 1 <= m <= 128, at most 64 query heads per KV head)";
         case COMPACTOR_E_WORKSPACE: return "workspace too small";
         case COMPACTOR_E_CUDA: return "CUDA runtime error";
-        case COMPACTOR_E_TOO_LARGE: return "problem needs more scratch than the built-in 32 MiB array holds";
+        case COMPACTOR_E_TOO_LARGE: return "problem too large for the call (built-in 32 MiB scratch, or a limit stated with the entry point)";
         default: return "unknown status";
     }
 }
@@ -1078,5 +1079,186 @@ extern "C" int compactor_fit_calibration(int64_t n, const double* r, const doubl
         }
     *alpha_out = best_a; *beta_out = best_b;
     if (loss_out != nullptr) *loss_out = best;
+    return COMPACTOR_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// The paged cache: filling it, attending to it, evicting from it.
+namespace {
+
+constexpr int kMaxQPerKv = 64;
+
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+bool cache_ok(const compactor_paged_cache* c, int* err) {
+    *err = COMPACTOR_E_INVALID_ARGUMENT;
+    if (c == nullptr || c->k_pages == nullptr || c->v_pages == nullptr || c->page_table == nullptr) return false;
+    if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16) || !aligned(c->page_table, 4) || !aligned(c->mass, 4) ||
+        !aligned(c->positions, 4)) return false;
+    if (c->d != kD) { *err = COMPACTOR_E_UNSUPPORTED; return false; }
+    if (c->layers < 1 || c->heads < 1 || c->batch < 1 || c->n_pages < 1 || c->max_pages < 1) return false;
+    if ((long long)c->layers * c->heads > 65535 || (long long)c->layers * c->heads * c->batch > 0x7fffffffLL) return false;
+    if (c->page_tokens < 8 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1)) != 0) return false;
+    if ((long long)c->max_pages * c->page_tokens > 0x7fff0000LL) return false;           // a slot number and one tile more fit an int
+    if (c->stride_token < kD || (c->stride_token & 7) || (c->stride_page & 7) || c->stride_token > (1LL << 40)) return false;
+    if (c->stride_page < c->page_tokens * c->stride_token) return false;
+    return true;
+}
+
+Paged to_paged(const compactor_paged_cache* c) {
+    Paged p;
+    p.k = static_cast<__nv_bfloat16*>(c->k_pages); p.v = static_cast<__nv_bfloat16*>(c->v_pages);
+    p.stride_page = c->stride_page; p.stride_token = c->stride_token;
+    p.mass = c->mass; p.positions = c->positions; p.table = c->page_table;
+    p.n_pages = c->n_pages; p.max_pages = c->max_pages;
+    p.page_shift = 0;
+    while ((1 << p.page_shift) < c->page_tokens) ++p.page_shift;
+    p.layers = c->layers; p.heads = c->heads; p.batch = c->batch;
+    return p;
+}
+
+bool rows_ok(const compactor_rows& r) {
+    return r.ptr != nullptr && aligned(r.ptr, 16) && r.stride_seq >= 0 && r.stride_head >= 0 && (r.stride_seq & 7) == 0 &&
+           (r.stride_head & 7) == 0;
+}
+
+struct DecodeLayout {
+    int workers, groups, gs, capacity;
+    size_t off_ml, off_o, off_scores, total;
+};
+// Workspace of the attention: tile prefix, partial (max, sum) pairs, partial outputs, scores.
+bool decode_layout(const compactor_paged_cache* c, const compactor_decode_options* o, DecodeLayout* l, int* err) {
+    if (!cache_ok(c, err)) return false;
+    *err = COMPACTOR_E_INVALID_ARGUMENT;
+    if (o == nullptr || o->q_per_kv < 1 || o->max_length < 1 || !(o->scale > 0.f) || !isfinite(o->scale) ||
+        !(o->softcap >= 0.f) || !isfinite(o->softcap)) return false;
+    if (o->q_per_kv > kMaxQPerKv) { *err = COMPACTOR_E_UNSUPPORTED; return false; }
+    if (o->accumulate != 0 && c->mass == nullptr) return false;
+    const long long units = (long long)c->heads * c->batch;
+    l->capacity = (int)std::min<long long>(o->max_length, (long long)c->max_pages * c->page_tokens);
+    l->groups = (o->q_per_kv + kDecodeHeads - 1) / kDecodeHeads;
+    l->gs = (o->q_per_kv + 1) / 2 * 2;
+    const long long tiles = units * ((l->capacity + kDecodeTile - 1) / kDecodeTile);
+    if (tiles * l->groups > 0x7fffffffLL || units * o->q_per_kv > 0x7ff00000LL) { *err = COMPACTOR_E_TOO_LARGE; return false; }
+    l->workers = (int)std::min<long long>(sm_count(), tiles * l->groups) * kDecodeWarps;
+    const size_t slots = (size_t)l->workers + (size_t)units * l->groups;
+    size_t off = align_up(sizeof(int) * ((size_t)units + 1));
+    l->off_ml = off;     off += align_up(sizeof(float) * 32 * slots);
+    l->off_o = off;      off += align_up(sizeof(float) * kD * std::min(o->q_per_kv, kDecodeHeads) * slots);
+    l->off_scores = off; off += o->accumulate != 0 ? align_up(sizeof(float) * (size_t)tiles * kDecodeTile * l->gs) : 0;
+    l->total = off;
+    return true;
+}
+
+}  // namespace
+
+extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape,
+                                    compactor_mat k_cache, compactor_mat v_cache, const int32_t* idx,
+                                    const int32_t* head_offsets, const int32_t* keep_counts, const float* mass_in,
+                                    const int32_t* first_position, const int32_t* lengths, int32_t* lengths_out,
+                                    int32_t* status, void* stream) {
+    int err = 0;
+    if (!cache_ok(cache, &err) || !shape_ok(shape, &err)) return err;
+    if (!mat_ok(k_cache) || !mat_ok(v_cache) || keep_counts == nullptr || (head_offsets != nullptr && idx == nullptr) ||
+        shape->heads != cache->heads || shape->batch != cache->batch || first_layer < 0 ||
+        first_layer > cache->layers - shape->layers)
+        return COMPACTOR_E_INVALID_ARGUMENT;
+    long long kept = 0;
+    for (int b = 0; b < shape->batch; ++b) {
+        if (keep_counts[b] < 0 || keep_counts[b] > shape->cu_seqlens[b + 1] - shape->cu_seqlens[b]) return COMPACTOR_E_INVALID_ARGUMENT;
+        kept += keep_counts[b];
+    }
+    if (kept * shape->heads > 0x7fffffffLL) return COMPACTOR_E_INVALID_ARGUMENT;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    FillArgs a;
+    memset(&a, 0, sizeof(a));
+    a.c = to_paged(cache); a.k = to_mat(k_cache); a.v = to_mat(v_cache);
+    a.first_layer = first_layer; a.layers = shape->layers;
+    a.total_tokens = shape->cu_seqlens[shape->batch]; a.total_keep = (int)kept;
+    a.idx = idx; a.head_offsets = head_offsets; a.mass_in = mass_in; a.first_position = first_position;
+    a.lengths = lengths; a.lengths_out = lengths_out; a.status = status;
+    const size_t per_layer = (size_t)cache->heads * cache->batch;
+    if (status != nullptr) CK(cudaMemsetAsync(status + first_layer * per_layer, 0, sizeof(int32_t) * per_layer * shape->layers, st));
+    int done = 0;
+    for (a.b0 = 0; a.b0 < shape->batch; a.b0 += kFillSeqs) {
+        a.nb = std::min(kFillSeqs, shape->batch - a.b0);
+        FillTables t;
+        t.cu_keep[0] = done;
+        for (int b = 0; b <= a.nb; ++b) t.cu_seqlens[b] = shape->cu_seqlens[a.b0 + b];
+        for (int b = 0; b < a.nb; ++b) t.cu_keep[b + 1] = done += keep_counts[a.b0 + b];
+        CK(launch_paged_fill(a, t, st));
+        if (lengths_out != nullptr || status != nullptr) CK(launch_paged_fill_lengths(a, t, st));
+    }
+    return COMPACTOR_OK;
+}
+
+extern "C" size_t compactor_paged_attention_workspace_bytes(const compactor_paged_cache* cache, const compactor_decode_options* options) {
+    DecodeLayout l; int err = 0;
+    return decode_layout(cache, options, &l, &err) ? l.total : 0;
+}
+
+extern "C" int compactor_paged_attention(const compactor_paged_cache* cache, int32_t layer, const compactor_decode_options* options,
+                                         compactor_rows q, compactor_rows k_new, compactor_rows v_new, const int32_t* new_positions,
+                                         const int32_t* lengths, compactor_rows out, float* lse_out, int32_t* status,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+    DecodeLayout l; int err = 0;
+    if (!decode_layout(cache, options, &l, &err)) return err;
+    const bool append = k_new.ptr != nullptr;
+    if (layer < 0 || layer >= cache->layers || !rows_ok(q) || !rows_ok(out) || append != (v_new.ptr != nullptr) ||
+        (append && (!rows_ok(k_new) || !rows_ok(v_new))) || lengths == nullptr || workspace == nullptr || !aligned(workspace, kAlign))
+        return COMPACTOR_E_INVALID_ARGUMENT;
+    const int q_heads = cache->heads * options->q_per_kv;
+    if ((q_heads > 1 && out.stride_head < kD) || (cache->batch > 1 && out.stride_seq < kD)) return COMPACTOR_E_INVALID_ARGUMENT;
+    if (workspace_bytes < l.total) return COMPACTOR_E_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    char* ws = static_cast<char*>(workspace);
+    DecodeArgs a;
+    memset(&a, 0, sizeof(a));
+    a.c = to_paged(cache);
+    a.units = cache->heads * cache->batch;
+    const size_t first = (size_t)layer * a.units;
+    a.c.table += first * cache->max_pages;
+    a.lengths = lengths + first;
+    a.status = status != nullptr ? status + first : nullptr;
+    a.q = static_cast<const __nv_bfloat16*>(q.ptr); a.q_seq = q.stride_seq; a.q_head = q.stride_head;
+    a.k_new = static_cast<const __nv_bfloat16*>(k_new.ptr); a.kn_seq = k_new.stride_seq; a.kn_head = k_new.stride_head;
+    a.v_new = static_cast<const __nv_bfloat16*>(v_new.ptr); a.vn_seq = v_new.stride_seq; a.vn_head = v_new.stride_head;
+    a.new_positions = new_positions;
+    a.out = static_cast<__nv_bfloat16*>(out.ptr); a.out_seq = out.stride_seq; a.out_head = out.stride_head;
+    a.lse = lse_out;
+    a.g = options->q_per_kv; a.groups = l.groups; a.gs = l.gs; a.capacity = l.capacity; a.workers = l.workers;
+    a.accumulate = options->accumulate != 0; a.scale = options->scale; a.softcap = options->softcap;
+    a.prefix = reinterpret_cast<int*>(ws);
+    a.ml = reinterpret_cast<float*>(ws + l.off_ml);
+    a.o = reinterpret_cast<float*>(ws + l.off_o);
+    a.scores = reinterpret_cast<float*>(ws + l.off_scores);
+    compactor::set_chain_for(0);                             // two dependent kernels: always chained
+    if (status != nullptr) CK(cudaMemsetAsync(a.status, 0, sizeof(int32_t) * a.units, st));
+    CK(launch_paged_attention(a, sm_count(), st));
+    return COMPACTOR_OK;
+}
+
+extern "C" int compactor_paged_evict(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* lengths,
+                                     const int32_t* budgets, const int32_t* next_position, int32_t recent, int32_t max_length,
+                                     int32_t* lengths_out, int32_t* status, void* stream) {
+    int err = 0;
+    if (!cache_ok(cache, &err)) return err;
+    if (layers < 1 || first_layer < 0 || first_layer > cache->layers - layers || lengths == nullptr || budgets == nullptr ||
+        lengths_out == nullptr || recent < 0 || max_length < 1 || cache->mass == nullptr ||
+        (recent > 0 && (cache->positions == nullptr || next_position == nullptr)))
+        return COMPACTOR_E_INVALID_ARGUMENT;
+    max_length = (int)std::min<long long>(max_length, (long long)cache->max_pages * cache->page_tokens);
+    if (max_length > evict_max_tokens()) return COMPACTOR_E_TOO_LARGE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const size_t per_layer = (size_t)cache->heads * cache->batch;
+    EvictArgs a;
+    memset(&a, 0, sizeof(a));
+    a.c = to_paged(cache);
+    a.first_unit = (int)(first_layer * per_layer); a.units = (int)(layers * per_layer);
+    if (a.units > 0x7fffffff / 8) return COMPACTOR_E_TOO_LARGE;          // grid size with clusters of 8
+    a.lengths = lengths; a.budgets = budgets; a.next_position = next_position;
+    a.recent = recent; a.max_length = max_length; a.lengths_out = lengths_out; a.status = status;
+    if (status != nullptr) CK(cudaMemsetAsync(status + a.first_unit, 0, sizeof(int32_t) * a.units, st));
+    CK(launch_paged_evict(a, sm_count(), st));
     return COMPACTOR_OK;
 }
