@@ -1139,7 +1139,7 @@ bool decode_layout(const compactor_paged_cache* c, const compactor_decode_option
     l->groups = (o->q_per_kv + kDecodeHeads - 1) / kDecodeHeads;
     l->gs = (o->q_per_kv + 1) / 2 * 2;
     const long long tiles = units * ((l->capacity + kDecodeTile - 1) / kDecodeTile);
-    if (tiles * l->groups > 0x7fffffffLL || units * o->q_per_kv > 0x7ff00000LL) { *err = COMPACTOR_E_TOO_LARGE; return false; }
+    if ((tiles + units * kDecodeUnitCost) * l->groups > 0x7fffffffLL || units * o->q_per_kv > 0x3fffffffLL) { *err = COMPACTOR_E_TOO_LARGE; return false; }
     l->workers = (int)std::min<long long>(sm_count(), tiles * l->groups) * kDecodeWarps;
     const size_t slots = (size_t)l->workers + (size_t)units * l->groups;
     size_t off = align_up(sizeof(int) * ((size_t)units + 1));
@@ -1232,6 +1232,7 @@ extern "C" int compactor_paged_attention(const compactor_paged_cache* cache, int
     a.ml = reinterpret_cast<float*>(ws + l.off_ml);
     a.o = reinterpret_cast<float*>(ws + l.off_o);
     a.scores = reinterpret_cast<float*>(ws + l.off_scores);
+    a.unit_rows = (l.capacity + kDecodeTile - 1) / kDecodeTile * kDecodeTile;
     compactor::set_chain_for(0);                             // two dependent kernels: always chained
     if (status != nullptr) CK(cudaMemsetAsync(a.status, 0, sizeof(int32_t) * a.units, st));
     CK(launch_paged_attention(a, sm_count(), st));

@@ -32,6 +32,8 @@ constexpr int kStages = 3;
 constexpr int kRowBytes = kD * 2;
 constexpr int kStageBytes = 2 * kTile * kRowBytes;     // K tile, V tile
 constexpr size_t kSmemBytes = (size_t)kWarps * kStages * kStageBytes;
+constexpr int kUnitCost = kDecodeUnitCost;
+constexpr int kUnitsInSmem = 2048;                     // units whose token counts every CTA keeps at hand
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -78,29 +80,65 @@ __device__ __forceinline__ int live_tokens(const DecodeArgs& a, int unit) {
     return t > a.capacity ? 0 : (int)t;
 }
 __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + kTile - 1) / kTile; }
+// What a (unit, group) counts for when the work is shared out: its tiles and kUnitCost more, since a warp that enters
+// a unit waits for its queries, page ids and row of results (with 0 the warps that got many short units of a padded batch ended
+// last: 32 against 20 us).
+__device__ __forceinline__ int cost_of(int tokens) { return tokens == 0 ? 0 : tiles_of(tokens) + kUnitCost; }
 
-// Worker that owns tile t of `total` tiles shared by `workers` workers, worker w having [w total / workers, (w+1) total / workers).
-__device__ __forceinline__ int owner(long long t, long long total, long long workers) {
-    return (int)(((t + 1) * workers - 1) / total);
-}
+// `total` cost shared by `workers`: the first total % workers get one more than the others.
+struct Share {
+    int q, r;
+    __device__ __forceinline__ Share(int total, int workers) : q(total / workers), r(total - total / workers * workers) {}
+    __device__ __forceinline__ int begin(int w) const { return w * q + min(w, r); }
+    __device__ __forceinline__ int size(int w) const { return q + (w < r ? 1 : 0); }
+    __device__ __forceinline__ int owner(int at) const {
+        const int longer = r * (q + 1);
+        return at < longer ? at / (q + 1) : r + (at - longer) / q;
+    }
+};
+__device__ __forceinline__ int active_workers(const DecodeArgs& a, int total) { return min(a.workers, total); }
 
 // A place in the order of all tiles: unit by unit, within a unit group by group.
 struct Cursor {
     int unit, grp, tile, tiles, tokens;
-    int before;                                              // tiles of the units before this one
-    // Next (unit, group) that has tiles.  Only called while tiles remain, so it ends.
-    __device__ __forceinline__ void next_unit(const DecodeArgs& a) {
+    // Next (unit, group) that has tiles; false if there is none.
+    __device__ __forceinline__ bool next_unit(const DecodeArgs& a, const int* live) {
         tile = 0;
-        if (grp + 1 < a.groups) { ++grp; return; }
+        if (grp + 1 < a.groups) { ++grp; return true; }
         grp = 0;
-        before += tiles;
         do {
-            ++unit;
-            tokens = unit < a.units ? live_tokens(a, unit) : 1;
+            if (++unit >= a.units) return false;
+            tokens = unit < kUnitsInSmem ? live[unit] : live_tokens(a, unit);
         } while (tokens == 0);
         tiles = tiles_of(tokens);
+        return true;
     }
 };
+
+// Page ids of a unit, entry `e0 + lane` of its row of the table (-1 behind its last token's).
+__device__ __forceinline__ int page_ids(const DecodeArgs& a, const Cursor& c, int e0, int lane) {
+    const int e = e0 + lane;
+    return e <= (c.tokens - 1) >> a.c.page_shift ? __ldg(a.c.table + (long long)c.unit * a.c.max_pages + e) : -1;
+}
+
+// Query fragments (B operand) of a unit's group: head t * 8 + gid, channels 16 s + 2 tig, + 1 and + 8, + 9.
+template <int NG>
+__device__ __forceinline__ void load_queries(const DecodeArgs& a, const Cursor& c, uint32_t (&qf)[NG][8][2], int lane) {
+    const int gid = lane >> 2, tig = lane & 3;
+    const int h = c.unit / a.c.batch, b = c.unit - h * a.c.batch;
+    const int head0 = h * a.g + c.grp * kDecodeHeads, heads = min(kDecodeHeads, a.g - c.grp * kDecodeHeads);
+#pragma unroll
+    for (int t = 0; t < NG; ++t) {
+        const bool on = t * 8 + gid < heads;
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + b * a.q_seq + (long long)(head0 + (on ? t * 8 + gid : 0)) * a.q_head);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const uint32_t x0 = __ldg(q + s * 8 + tig), x1 = __ldg(q + s * 8 + tig + 4);
+            qf[t][s][0] = on ? x0 : 0u;
+            qf[t][s][1] = on ? x1 : 0u;
+        }
+    }
+}
 
 template <int NG>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -109,15 +147,22 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
     __shared__ int cum[kThreads + 1];
     __shared__ int warp_sum[kWarps];
     __shared__ int bad[kWarps][kStages];
+    __shared__ int new_page[kWarps][kStages];
+    __shared__ int live[kUnitsInSmem];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int gid = lane >> 2, tig = lane & 3;
     pdl_trigger();
+    pdl_wait();
 
-    // tiles before each thread's run of units
+    // cost before each thread's run of units
     const int per = (a.units + kThreads - 1) / kThreads;
     const int u0 = tid * per, u1 = min(a.units, u0 + per);
     int mine = 0;
-    for (int u = u0; u < u1; ++u) mine += tiles_of(live_tokens(a, u));
+    for (int u = u0; u < u1; ++u) {
+        const int n = live_tokens(a, u);
+        if (u < kUnitsInSmem) live[u] = n;
+        mine += cost_of(n);
+    }
     int incl = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -132,111 +177,134 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
     cum[tid + 1] = before + incl;
     if (tid == 0) cum[0] = 0;
     __syncthreads();
-    const int real_tiles = cum[kThreads];
+    const int all = cum[kThreads];
     if (blockIdx.x == 0) {                                   // for the second kernel, and the units that are refused
         int at = cum[tid];
         for (int u = u0; u < u1; ++u) {
             a.prefix[u] = at;
-            at += tiles_of(live_tokens(a, u));
+            at += cost_of(live_tokens(a, u));
             const int n = __ldg(a.lengths + u);
             if (a.status != nullptr && n >= 0 && (long long)n + (a.k_new != nullptr) > a.capacity)
                 atomicOr(a.status + u, COMPACTOR_STATUS_CAPACITY);
         }
-        if (tid == 0) a.prefix[a.units] = real_tiles;
+        if (tid == 0) a.prefix[a.units] = all;
     }
-    const long long total = (long long)real_tiles * a.groups;
-    const int workers = (int)min((long long)a.workers, total);
+    const int total = all * a.groups;
+    const int workers = active_workers(a, total);
     const int worker = warp * gridDim.x + blockIdx.x;        // neighbouring workers on different SMs: a small call uses them all
     if (worker >= workers) return;
-    const long long t0 = worker * total / workers, t1 = (worker + 1) * total / workers;
-    const int count = (int)(t1 - t0);
+    const Share share(total, workers);
+    const int begin = share.begin(worker);
+    int left_p = share.size(worker);                         // cost that the producer has not passed yet
 
-    // the unit that holds tile t0
+    // the unit that holds place `begin`
     Cursor start;
     {
-        int lo = 0, hi = kThreads;                           // cum[lo] * groups <= t0 < cum[hi] * groups
+        int lo = 0, hi = kThreads;                           // cum[lo] * groups <= begin < cum[hi] * groups
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if ((long long)cum[mid] * a.groups <= t0) lo = mid; else hi = mid;
+            if (cum[mid] * a.groups <= begin) lo = mid; else hi = mid;
         }
-        long long left = t0 - (long long)cum[lo] * a.groups;
-        int u = lo * per, n = live_tokens(a, u);
-        while (left >= (long long)tiles_of(n) * a.groups) {
-            left -= (long long)tiles_of(n) * a.groups;
-            n = live_tokens(a, ++u);
+        int left = begin - cum[lo] * a.groups;
+        auto tokens_of = [&](int unit) { return unit < kUnitsInSmem ? live[unit] : live_tokens(a, unit); };
+        int u = lo * per, n = tokens_of(u);
+        while (left >= cost_of(n) * a.groups) {
+            left -= cost_of(n) * a.groups;
+            n = tokens_of(++u);
         }
         start.unit = u; start.tokens = n; start.tiles = tiles_of(n);
-        start.before = (int)((t0 - left) / a.groups);
-        start.grp = (int)(left / start.tiles);
-        start.tile = (int)(left - (long long)start.grp * start.tiles);
+        start.grp = left / cost_of(n);
+        start.tile = left - start.grp * cost_of(n) - kUnitCost;
+        if (start.tile < 0) {                                // within the unit's head: the first tile is the next
+            left_p += start.tile;
+            start.tile = 0;
+            if (left_p <= 0) return;
+        }
     }
+    int left_c = left_p;                                     // cost that the consumer has not passed yet
 
     unsigned char* my_ring = ring + (size_t)warp * kStages * kStageBytes;
     const uint32_t ring_s = smem_u32(my_ring);
 
-    // ---- producer: one tile into a stage.  Lane l copies 16-byte piece l & 15 of rows (l >> 4) + 2 i.
-    Cursor pc = start;
-    int issued = 0;
+    // ---- producer: one tile into a stage.  Lane l copies 16-byte piece l & 15 of rows (l >> 4) + 2 i.  What the next tiles
+    // need is asked for early: 64 page ids of the unit (lane l holds entries e0 + l and e0 + 32 + l), the first 32 of the unit
+    // after it, and the queries of a unit when its first tile is issued.
+    Cursor pc = start, nc = start;
     const int piece = lane & 15, row_hi = lane >> 4;
+    int e0 = (pc.tile * kTile) >> a.c.page_shift;
+    int ids = page_ids(a, pc, e0, lane), ids_after = page_ids(a, pc, e0 + 32, lane), ids_next_unit = -1;
+    uint32_t qn[NG][8][2];
+    int q_unit = pc.unit, q_grp = pc.grp;                    // whose queries qn holds
+    bool q_waiting = true;
+    load_queries<NG>(a, pc, qn, lane);
+    if (nc.next_unit(a, live)) ids_next_unit = page_ids(a, nc, 0, lane);
+    int in_stage = 0;
     auto issue = [&]() {
-        if (issued < count) {
-            const int stage = issued % kStages;
+        if (left_p > 0) {
+            const int stage = in_stage;
             const int unit = pc.unit, n = pc.tokens, base = pc.tile * kTile;
             const int cached = n - (a.k_new != nullptr);     // tokens whose rows are in pages
-            const int p0 = page_of(a.c, unit, base);
-            const int p1 = base + 8 < n ? page_of(a.c, unit, base + 8) : -1;
+            const int e = base >> a.c.page_shift;
+            if (e + 1 >= e0 + 32) {                          // (pages of 8 tokens: a tile has two)
+                e0 += 32;
+                if (e < e0) {                                // a tile on the seam keeps one entry of the old run
+                    const int seam = __shfl_sync(0xffffffffu, ids, 31);
+                    const int rest = __shfl_up_sync(0xffffffffu, ids_after, 1);
+                    ids = lane == 0 ? seam : rest;
+                    e0 -= 1;
+                    ids_after = page_ids(a, pc, e0 + 32, lane);
+                } else {
+                    ids = ids_after;
+                    ids_after = page_ids(a, pc, e0 + 32, lane);
+                }
+            }
+            int p0 = __shfl_sync(0xffffffffu, ids, e - e0), p1 = __shfl_sync(0xffffffffu, ids, ((base + 8) >> a.c.page_shift) - e0);
+            if ((unsigned)p0 >= (unsigned)a.c.n_pages) p0 = -1;
+            if ((unsigned)p1 >= (unsigned)a.c.n_pages || base + 8 >= n) p1 = -1;
             const uint32_t ks = ring_s + stage * kStageBytes, vs = ks + kTile * kRowBytes;
-            const int batch = a.c.batch, h = unit / batch, b = unit - h * batch;
+            const __nv_bfloat16* kn = a.c.k;
+            const __nv_bfloat16* vn = a.c.v;
+            const int fresh_row = cached < n ? cached - base : -1;           // the new token's row of this tile, if it has it
+            if (fresh_row >= 0 && fresh_row < kTile) {
+                const int h = unit / a.c.batch, b = unit - h * a.c.batch;
+                kn = a.k_new + b * a.kn_seq + h * a.kn_head + piece * 8;
+                vn = a.v_new + b * a.vn_seq + h * a.vn_head + piece * 8;
+            }
 #pragma unroll
             for (int i = 0; i < kTile / 2; ++i) {
                 const int row = 2 * i + row_hi, tok = base + row;
                 const int page = i < kTile / 4 ? p0 : p1;
-                const __nv_bfloat16* ksrc = a.c.k;
-                const __nv_bfloat16* vsrc = a.c.v;
-                int bytes = 0;
-                if (tok < cached) {
-                    if (page >= 0) {
-                        const long long off = row_in_pool(a.c, page, tok) + piece * 8;
-                        ksrc += off; vsrc += off; bytes = 16;
-                    }
-                } else if (tok < n) {                        // the new token
-                    ksrc = a.k_new + b * a.kn_seq + h * a.kn_head + piece * 8;
-                    vsrc = a.v_new + b * a.vn_seq + h * a.vn_head + piece * 8;
-                    bytes = 16;
-                }
+                const bool is_new = row == fresh_row, on = is_new || (tok < cached && page >= 0);
+                const long long off = on && !is_new ? row_in_pool(a.c, page, tok) + piece * 8 : 0;
                 const uint32_t dst = row * kRowBytes + ((piece ^ (row & 7)) << 4);
-                cp_async16(ks + dst, ksrc, bytes);
-                cp_async16(vs + dst, vsrc, bytes);
+                cp_async16(ks + dst, is_new ? kn : a.c.k + off, on ? 16 : 0);
+                cp_async16(vs + dst, is_new ? vn : a.c.v + off, on ? 16 : 0);
             }
             if (lane == 0) {
                 const int bits = (p0 < 0 && base < cached ? 1 : 0) | (p1 < 0 && base + 8 < cached ? 2 : 0);
+                const int np = fresh_row < 8 ? p0 : p1;
                 bad[warp][stage] = bits;
-                if (bits != 0 && a.status != nullptr) atomicOr(a.status + unit, COMPACTOR_STATUS_PAGE);
-            }
-            if (cached < n && pc.grp == 0 && cached >= base && cached < base + kTile) {      // append the new token
-                const int page = cached < base + 8 ? p0 : p1;
-                if (page >= 0) {
-                    const long long off = row_in_pool(a.c, page, cached) + piece * 8;
-                    if (row_hi == 0)
-                        *reinterpret_cast<uint4*>(a.c.k + off) =
-                            *reinterpret_cast<const uint4*>(a.k_new + b * a.kn_seq + h * a.kn_head + piece * 8);
-                    else
-                        *reinterpret_cast<uint4*>(a.c.v + off) =
-                            *reinterpret_cast<const uint4*>(a.v_new + b * a.vn_seq + h * a.vn_head + piece * 8);
-                    const long long at = slot_in_pool(a.c, page, cached);
-                    if (lane == 0 && a.c.positions != nullptr)
-                        a.c.positions[at] = a.new_positions != nullptr ? a.new_positions[b] : cached;
-                    if (lane == 0 && a.c.mass != nullptr && !a.accumulate) a.c.mass[at] = 0.f;
-                } else if (lane == 0 && a.status != nullptr) {
+                new_page[warp][stage] = np;
+                if (a.status != nullptr && (bits != 0 || (fresh_row >= 0 && fresh_row < kTile && np < 0)))
                     atomicOr(a.status + unit, COMPACTOR_STATUS_PAGE);
+            }
+            in_stage = stage + 1 == kStages ? 0 : stage + 1;
+            --left_p;
+            if (++pc.tile == pc.tiles && (left_p -= kUnitCost) > 0) {
+                pc = nc;
+                e0 = 0;
+                ids = ids_next_unit;
+                ids_after = page_ids(a, pc, 32, lane);
+                if (nc.next_unit(a, live)) ids_next_unit = page_ids(a, nc, 0, lane);
+                if (!q_waiting) {
+                    load_queries<NG>(a, pc, qn, lane);
+                    q_unit = pc.unit; q_grp = pc.grp; q_waiting = true;
                 }
             }
-            ++issued;
-            if (++pc.tile == pc.tiles && issued < count) pc.next_unit(a);
         }
         cp_commit();
     };
-#pragma unroll
+#pragma unroll 1
     for (int s = 0; s < kStages; ++s) issue();
 
     // ---- consumer
@@ -247,34 +315,33 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
     float o[NG][8][4];
     float mx[NG][2], sum[NG][2];
     bool fresh = true;
-    int first_tile = 0, head0 = 0, heads = 0;
+    int first_tile = 0, head0 = 0, heads = 0, stage = 0;
 
-    for (int i = 0; i < count; ++i) {
+    while (true) {
         if (fresh) {                                         // a new unit or group: its queries
             fresh = false;
             first_tile = cc.tile;
-            const int h = cc.unit / a.c.batch, b = cc.unit - h * a.c.batch;
-            head0 = h * a.g + cc.grp * kDecodeHeads;
+            head0 = cc.unit / a.c.batch * a.g + cc.grp * kDecodeHeads;
             heads = min(kDecodeHeads, a.g - cc.grp * kDecodeHeads);
-            const __nv_bfloat16* q = a.q + b * a.q_seq;
+            if (q_waiting && q_unit == cc.unit && q_grp == cc.grp) {
+                q_waiting = false;
+#pragma unroll
+                for (int t = 0; t < NG; ++t)
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) { qf[t][s][0] = qn[t][s][0]; qf[t][s][1] = qn[t][s][1]; }
+            } else {
+                load_queries<NG>(a, cc, qf, lane);
+            }
 #pragma unroll
             for (int t = 0; t < NG; ++t) {
-                const bool live = t * 8 + gid < heads;
-                const uint32_t* qh = reinterpret_cast<const uint32_t*>(q + (long long)(head0 + (live ? t * 8 + gid : 0)) * a.q_head);
 #pragma unroll
-                for (int s = 0; s < 8; ++s) {
-                    const uint32_t x0 = __ldg(qh + s * 8 + tig), x1 = __ldg(qh + s * 8 + tig + 4);
-                    qf[t][s][0] = live ? x0 : 0u;
-                    qf[t][s][1] = live ? x1 : 0u;
-                    o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.f;
-                }
+                for (int s = 0; s < 8; ++s) o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.f;
                 mx[t][0] = mx[t][1] = -INFINITY;
                 sum[t][0] = sum[t][1] = 0.f;
             }
         }
         cp_wait<kStages - 1>();
         __syncwarp();
-        const int stage = i % kStages;
         const uint32_t ks = ring_s + stage * kStageBytes, vs = ks + kTile * kRowBytes;
         const int base = cc.tile * kTile;
 
@@ -328,7 +395,7 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
             }
         }
         if (a.accumulate) {                                  // kept until the sum over the whole unit is known
-            float* row = a.scores + ((long long)(cc.before + cc.tile) * kTile + gid) * a.gs + cc.grp * kDecodeHeads + 2 * tig;
+            float* row = a.scores + ((long long)cc.unit * a.unit_rows + base + gid) * a.gs + cc.grp * kDecodeHeads + 2 * tig;
 #pragma unroll
             for (int t = 0; t < NG; ++t)
                 if (t * 8 + 2 * tig < heads) {
@@ -356,11 +423,28 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
                 for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pf[t][0], pf[t][1]);
             }
         }
+        // the new token's row goes from the ring to its page
+        const int fresh_row = cached < cc.tokens && cc.grp == 0 ? cached - base : -1;
+        if (fresh_row >= 0 && fresh_row < kTile) {
+            const int page = new_page[warp][stage];
+            if (page >= 0) {
+                const uint4 x = *reinterpret_cast<const uint4*>(my_ring + stage * kStageBytes + row_hi * (kTile * kRowBytes) +
+                                                                fresh_row * kRowBytes + ((piece ^ (fresh_row & 7)) << 4));
+                *reinterpret_cast<uint4*>((row_hi == 0 ? a.c.k : a.c.v) + row_in_pool(a.c, page, cached) + piece * 8) = x;
+                const long long at = slot_in_pool(a.c, page, cached);
+                if (lane == 0 && a.c.positions != nullptr)
+                    a.c.positions[at] = a.new_positions != nullptr ? __ldg(a.new_positions + cc.unit % a.c.batch) : cached;
+                if (lane == 0 && a.c.mass != nullptr && !a.accumulate) a.c.mass[at] = 0.f;
+            }
+        }
         __syncwarp();
         issue();
 
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        --left_c;
         const bool unit_ends = ++cc.tile == cc.tiles;
-        if (unit_ends || i + 1 == count) {                   // hand over what this warp has of the unit
+        if (unit_ends) left_c -= kUnitCost;
+        if (unit_ends || left_c <= 0) {                   // hand over what this warp has of the unit
             const long long slot = (long long)worker + cc.unit * a.groups + cc.grp;
             const bool whole = unit_ends && first_tile == 0;
             const int b = cc.unit % a.c.batch, gg = min(a.g, kDecodeHeads);
@@ -397,8 +481,9 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
                         }
                     }
                 }
+            if (left_c <= 0) return;
             fresh = true;
-            if (unit_ends && i + 1 < count) cc.next_unit(a);
+            cc.next_unit(a, live);
         }
     }
 }
@@ -411,128 +496,161 @@ __device__ __forceinline__ void merge(float& m, float& l, float mo, float lo) {
     m = mm;
 }
 
-// The pieces of a unit's group: partial slots [first, first + n).
+// The pieces of a unit's group: partial slots [first, first + n).  `at`, `cost`: the unit's place and its cost per group.
 struct Pieces { long long first; int n; };
-__device__ __forceinline__ Pieces pieces_of(const DecodeArgs& a, int unit, int grp) {
-    const int p = a.prefix[unit], tiles = a.prefix[unit + 1] - p;
-    const long long total = (long long)a.prefix[a.units] * a.groups;
-    const long long workers = min((long long)a.workers, total);
-    const long long v = (long long)p * a.groups + (long long)grp * tiles;
-    const int w0 = owner(v, total, workers), w1 = owner(v + tiles - 1, total, workers);
+__device__ __forceinline__ Pieces pieces_of(const DecodeArgs& a, int unit, int grp, int at, int cost, int all) {
+    const int total = all * a.groups;
+    const Share share(total, active_workers(a, total));
+    const int v = at * a.groups + grp * cost;
+    const int w0 = share.owner(v + kUnitCost), w1 = share.owner(v + cost - 1);
     return {(long long)w0 + (long long)unit * a.groups + grp, w1 - w0 + 1};
 }
 
 // Blocks [0, units * g): one (unit, query head) each; its pieces are joined: o = sum_i e_i o_i / sum_i e_i l_i with
-// e_i = 2^(m_i - m).  The blocks behind them add the weights; each takes an equal run of tiles.
-__global__ void __launch_bounds__(kThreads)
-join_kernel(const __grid_constant__ DecodeArgs a, int join_blocks) {
+// e_i = 2^(m_i - m).  The blocks behind them add the weights, `chunk` tokens of one unit each.  Both are chains of a few
+// dependent reads from L2 (about 0.7 us each), so every step asks for all it needs at once.
+constexpr int kJoinBatch = 8;              // pieces per warp in flight
+constexpr int kTokenBatch = 4;             // tokens per thread in flight
+
+template <int kWarps>
+__global__ void __launch_bounds__(kWarps * 32)
+join_kernel(const __grid_constant__ DecodeArgs a, int join_blocks, int chunk, int chunks) {
+    constexpr int kThreads = kWarps * 32;
     __shared__ float part[kWarps][kD];
-    __shared__ float red_m[16][17], red_l[16][17];
+    __shared__ float red_m[kWarps][16], red_l[kWarps][16];
     __shared__ float lse2[64];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_trigger();
     pdl_wait();
+    const int all = a.prefix[a.units];
     if ((int)blockIdx.x < join_blocks) {
         const int unit = blockIdx.x / a.g, head = blockIdx.x - unit * a.g;
         const int grp = head / kDecodeHeads, hh = head - grp * kDecodeHeads, gg = min(a.g, kDecodeHeads);
         const int h = unit / a.c.batch, b = unit - h * a.c.batch;
+        const int at = a.prefix[unit], cost = a.prefix[unit + 1] - at;
         __nv_bfloat16* dst = a.out + b * a.out_seq + (long long)(h * a.g + head) * a.out_head;
         float* lse = a.lse != nullptr ? a.lse + (long long)b * (a.c.heads * a.g) + h * a.g + head : nullptr;
-        if (live_tokens(a, unit) == 0) {
+        if (cost == 0) {
             if (tid < kD) dst[tid] = __float2bfloat16_rn(0.f);
             if (tid == 0 && lse != nullptr) *lse = -INFINITY;
             return;
         }
-        const Pieces ps = pieces_of(a, unit, grp);
+        const Pieces ps = pieces_of(a, unit, grp, at, cost, all);
         if (ps.n == 1) return;                               // written by the warp that had it whole
         float m = -INFINITY, l = 0.f;
-        for (int i = lane; i < ps.n; i += 32) {
-            const float* ml = a.ml + (ps.first + i) * 32 + hh;
-            merge(m, l, ml[0], ml[16]);
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            const float mo = __shfl_xor_sync(0xffffffffu, m, d), lo = __shfl_xor_sync(0xffffffffu, l, d);
-            merge(m, l, mo, lo);
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int i = warp; i < ps.n; i += kWarps) {
-            const long long slot = ps.first + i;
-            const float e = ex2f(a.ml[slot * 32 + hh] - ref);
-            const float4 x = *reinterpret_cast<const float4*>(a.o + (slot * gg + hh) * kD + lane * 4);
-            acc.x += e * x.x; acc.y += e * x.y; acc.z += e * x.z; acc.w += e * x.w;
+        for (int i0 = warp; i0 < ps.n; i0 += kWarps * kJoinBatch) {
+            float pm[kJoinBatch], pl[kJoinBatch];
+            float4 x[kJoinBatch];
+#pragma unroll
+            for (int k = 0; k < kJoinBatch; ++k) {
+                const long long slot = ps.first + min(i0 + k * kWarps, ps.n - 1);
+                pm[k] = a.ml[slot * 32 + hh];
+                pl[k] = a.ml[slot * 32 + 16 + hh];
+                x[k] = *reinterpret_cast<const float4*>(a.o + (slot * gg + hh) * kD + lane * 4);
+            }
+            float top = m;
+#pragma unroll
+            for (int k = 0; k < kJoinBatch; ++k) {
+                if (i0 + k * kWarps >= ps.n) pm[k] = -INFINITY;
+                top = fmaxf(top, pm[k]);
+            }
+            const float ref = top == -INFINITY ? 0.f : top;
+            const float old = ex2f(m - ref);
+            l *= old; acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
+            m = top;
+#pragma unroll
+            for (int k = 0; k < kJoinBatch; ++k) {
+                if (i0 + k * kWarps >= ps.n) continue;
+                const float e = ex2f(pm[k] - ref);
+                l += e * pl[k];
+                acc.x += e * x[k].x; acc.y += e * x[k].y; acc.z += e * x[k].z; acc.w += e * x[k].w;
+            }
         }
         *reinterpret_cast<float4*>(&part[warp][lane * 4]) = acc;
+        if (lane == 0) { red_m[warp][0] = m; red_l[warp][0] = l; }
         __syncthreads();
         if (tid < kD) {
-            float x = 0.f;
+            float top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) x += part[w][tid];
-            dst[tid] = __float2bfloat16_rn(l == 0.f ? 0.f : x / l);
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, red_m[w][0]);
+            const float ref = top == -INFINITY ? 0.f : top;
+            float x = 0.f, z = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float e = ex2f(red_m[w][0] - ref);
+                x += e * part[w][tid];
+                z += e * red_l[w][0];
+            }
+            dst[tid] = __float2bfloat16_rn(z == 0.f ? 0.f : x / z);
+            if (tid == 0 && lse != nullptr) *lse = z == 0.f ? -INFINITY : kLn2 * (top + log2f(z));
         }
-        if (tid == 0 && lse != nullptr) *lse = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
         return;
     }
 
     // weights: w_j += sum over the unit's query heads of 2^(y_j - lse)
-    const long long tiles = a.prefix[a.units];
-    const int blk = blockIdx.x - join_blocks, blks = gridDim.x - join_blocks;
-    long long t = blk * tiles / blks;
-    const long long t1 = (blk + 1) * tiles / blks;
-    if (t >= t1) return;
-    int lo = 0, hi = a.units;                                // prefix[lo] <= t < prefix[hi]
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 31) / 32, at = lo + lane * step;
-        const bool below = at < hi && a.prefix[at] <= t;
-        const int k = 31 - __clz(__ballot_sync(0xffffffffu, below));
-        lo += k * step;
-        hi = min(hi, lo + step);
-    }
-    int unit = lo;
-    while (t < t1) {
-        while (a.prefix[unit + 1] <= t) ++unit;              // units without tiles
-        const int p = a.prefix[unit];
-        const int tok0 = (int)(t - p) * kTile;
-        const long long t_end = min(t1, (long long)a.prefix[unit + 1]);
-        const int n = live_tokens(a, unit), tok1 = min(n, (int)(t_end - p) * kTile);
-        const int cached = n - (a.k_new != nullptr);
-        for (int grp = 0; grp < a.groups; ++grp) {
-            const Pieces ps = pieces_of(a, unit, grp);
-            const int heads = min(kDecodeHeads, a.g - grp * kDecodeHeads);
-            const int hh = tid & 15, st = tid >> 4;
-            float m = -INFINITY, l = 0.f;
-            if (hh < heads)
-                for (int i = st; i < ps.n; i += 16) {
-                    const float* ml = a.ml + (ps.first + i) * 32 + hh;
-                    merge(m, l, ml[0], ml[16]);
-                }
-            red_m[st][hh] = m; red_l[st][hh] = l;
-            __syncthreads();
-            if (tid < heads) {
-                m = red_m[0][tid]; l = red_l[0][tid];
+    const int item = blockIdx.x - join_blocks, unit = item / chunks, tok0 = (item - unit * chunks) * chunk;
+    const int n = live_tokens(a, unit), tok1 = min(n, tok0 + chunk);
+    const int at = a.prefix[unit], cost = a.prefix[unit + 1] - at;
+    if (tok0 >= n) return;
+    const int cached = n - (a.k_new != nullptr);
+    int page[kTokenBatch];
+    auto ask_pages = [&](int first) {
 #pragma unroll
-                for (int i = 1; i < 16; ++i) merge(m, l, red_m[i][tid], red_l[i][tid]);
-                lse2[grp * kDecodeHeads + tid] = l == 0.f ? INFINITY : m + log2f(l);
+        for (int k = 0; k < kTokenBatch; ++k) page[k] = page_of(a.c, unit, min(first + k * kThreads, tok1 - 1));
+    };
+    ask_pages(tok0 + tid);
+    int hp = 1;                                              // lanes side by side for the heads of a group
+    while (hp < min(a.g, kDecodeHeads)) hp *= 2;
+    const int hh = lane & (hp - 1), st = tid / hp, streams = kThreads / hp;
+    for (int grp = 0; grp < a.groups; ++grp) {
+        const Pieces ps = pieces_of(a, unit, grp, at, cost, all);
+        const int heads = min(kDecodeHeads, a.g - grp * kDecodeHeads);
+        float m = -INFINITY, l = 0.f;
+        if (hh < heads) {
+#pragma unroll 4
+            for (int i = st; i < ps.n; i += streams) {
+                const float* ml = a.ml + (ps.first + i) * 32 + hh;
+                merge(m, l, ml[0], ml[16]);
             }
-            __syncthreads();
         }
-        for (int tok = tok0 + tid; tok < tok1; tok += kThreads) {
-            const float2* row = reinterpret_cast<const float2*>(a.scores + ((long long)p * kTile + tok) * a.gs);
-            float w = 0.f;
-            for (int i = 0; i < a.g; i += 2) {
-                const float2 y = row[i >> 1];
-                w += ex2f(y.x - lse2[i]);
-                if (i + 1 < a.g) w += ex2f(y.y - lse2[i + 1]);
-            }
-            const int page = page_of(a.c, unit, tok);
-            if (page >= 0) {
-                const long long at = slot_in_pool(a.c, page, tok);
-                a.c.mass[at] = tok < cached ? a.c.mass[at] + w : w;
-            }
+        for (int d = hp; d < 32; d *= 2) {
+            const float mo = __shfl_xor_sync(0xffffffffu, m, d), lo = __shfl_xor_sync(0xffffffffu, l, d);
+            merge(m, l, mo, lo);
+        }
+        if (lane < hp) { red_m[warp][lane] = m; red_l[warp][lane] = l; }
+        __syncthreads();
+        if (tid < heads) {
+            m = red_m[0][tid]; l = red_l[0][tid];
+#pragma unroll
+            for (int i = 1; i < kWarps; ++i) merge(m, l, red_m[i][tid], red_l[i][tid]);
+            lse2[grp * kDecodeHeads + tid] = l == 0.f ? INFINITY : m + log2f(l);
         }
         __syncthreads();
-        t = t_end;
+    }
+    for (int first = tok0 + tid; first < tok1; first += kThreads * kTokenBatch) {
+        float w[kTokenBatch], old[kTokenBatch];
+#pragma unroll
+        for (int k = 0; k < kTokenBatch; ++k)
+            old[k] = a.c.mass[slot_in_pool(a.c, max(page[k], 0), min(first + k * kThreads, tok1 - 1))];
+#pragma unroll
+        for (int k = 0; k < kTokenBatch; ++k) {
+            const int tok = min(first + k * kThreads, tok1 - 1);
+            w[k] = 0.f;
+            const float2* row = reinterpret_cast<const float2*>(a.scores + ((long long)unit * a.unit_rows + tok) * a.gs);
+            for (int i = 0; i < a.g; i += 2) {
+                const float2 y = row[i >> 1];
+                w[k] += ex2f(y.x - lse2[i]);
+                if (i + 1 < a.g) w[k] += ex2f(y.y - lse2[i + 1]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kTokenBatch; ++k) {
+            const int tok = first + k * kThreads;
+            if (tok < tok1 && page[k] >= 0)
+                a.c.mass[slot_in_pool(a.c, page[k], tok)] = tok < cached ? old[k] + w[k] : w[k];
+        }
+        if (first + kThreads * kTokenBatch < tok1) ask_pages(first + kThreads * kTokenBatch);
     }
 }
 
@@ -543,15 +661,18 @@ cudaError_t launch_paged_attention(const DecodeArgs& a, int sm_count, cudaStream
     auto kernel = a.g <= 8 ? decode_kernel<1> : decode_kernel<2>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
     if (e != cudaSuccess) return e;
-    kernel<<<grid, kThreads, kSmemBytes, stream>>>(a);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_chained(kPdlOther, kernel, dim3(grid), dim3(kThreads), kSmemBytes, stream, a)) != cudaSuccess) return e;
+    // the second kernel: 16 warps a block where its blocks do not fill the GPU anyway
     const int join_blocks = a.units * a.g;
-    int mass_blocks = 0;
-    if (a.accumulate) {
-        const long long tokens = (long long)a.units * a.capacity;
-        mass_blocks = (int)min(4LL * sm_count, (tokens + kThreads - 1) / kThreads);
+    const int warps = join_blocks <= 2 * sm_count ? 16 : 8;
+    int chunk = warps * 32 * kTokenBatch, chunks = 0;
+    if (a.accumulate) {                                      // one round of a block's threads, more where that gives more blocks than fit at once
+        while ((long long)a.units * ((a.capacity + chunk - 1) / chunk) > 16LL * sm_count && chunk < a.capacity) chunk *= 2;
+        chunks = (a.capacity + chunk - 1) / chunk;
     }
-    e = launch_chained(kPdlOther, join_kernel, dim3(join_blocks + mass_blocks), dim3(kThreads), 0, stream, a, join_blocks);
+    const dim3 blocks(join_blocks + a.units * chunks);
+    e = warps == 16 ? launch_chained(kPdlOther, join_kernel<16>, blocks, dim3(512), 0, stream, a, join_blocks, chunk, chunks)
+                    : launch_chained(kPdlOther, join_kernel<8>, blocks, dim3(256), 0, stream, a, join_blocks, chunk, chunks);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -594,3 +594,24 @@ def test_compress_fill_decode_evict(across):
     same_bits(got, host, "evict")
     np.testing.assert_array_equal(got["mass"].view(np.uint32), host["mass"].view(np.uint32))
     np.testing.assert_array_equal(len_d.cpu().numpy(), budgets)
+
+
+def test_attention_captured_behind_copies_and_memsets():
+    # what stands before the call in a graph need not be a kernel: a copy, the clearing of the status words
+    from paper_2507_08143_b200 import binding as B
+    _, cache, len_d = make_cache([[[100, 7]]], 16, 4, 13)
+    q, q2 = torch.randn(2, 4, 128, device="cuda").bfloat16(), torch.randn(2, 4, 128, device="cuda").bfloat16()
+    opt = B.decode_options(4, 104)
+    ws, out, want = B.alloc_paged_attention_workspace(cache, opt), torch.empty_like(q), torch.empty_like(q)
+    st = torch.full((1, 1, 2), 5, dtype=torch.int32, device="cuda")
+    B.paged_attention(cache, 0, opt, q2, len_d, want, ws, status=st)
+    torch.cuda.synchronize()
+    for status in (None, st):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            q.copy_(q2)
+            B.paged_attention(cache, 0, opt, q, len_d, out, ws, status=status)
+        q.zero_(); out.zero_(); st.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and st.unique().tolist() == [5 if status is None else 0]
