@@ -370,8 +370,8 @@ int compactor_compress_full(const compactor_shape* shape, const compactor_option
  *   k_pages, v_pages  device bf16; row (page p, slot s) is the d elements at p * stride_page + s * stride_token
  *                     of either pool.  16-byte aligned; strides in elements, multiples of 8, stride_token >= d,
  *                     stride_page >= page_tokens * stride_token.  A pool may exceed 2^32 elements.
- *   mass              device fp32 [n_pages][page_tokens] or NULL: accumulated attention weight per slot.
- *   positions         device int32 [n_pages][page_tokens] or NULL: position of the slot's token.
+ *   mass              device fp32 [n_pages][page_tokens] or NULL: accumulated attention weight per slot; 16-byte aligned.
+ *   positions         device int32 [n_pages][page_tokens] or NULL: position of the slot's token; 16-byte aligned.
  *   page_table        device int32 [layers*heads*batch][max_pages]: token t of unit u lies in slot
  *                     t % page_tokens of page page_table[u][t / page_tokens].  Entries behind a unit's
  *                     last token are not read.  A page that is written (filled, appended to, accumulated

@@ -1093,8 +1093,8 @@ bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; 
 bool cache_ok(const compactor_paged_cache* c, int* err) {
     *err = COMPACTOR_E_INVALID_ARGUMENT;
     if (c == nullptr || c->k_pages == nullptr || c->v_pages == nullptr || c->page_table == nullptr) return false;
-    if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16) || !aligned(c->page_table, 4) || !aligned(c->mass, 4) ||
-        !aligned(c->positions, 4)) return false;
+    if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16) || !aligned(c->page_table, 4) || !aligned(c->mass, 16) ||
+        !aligned(c->positions, 16)) return false;
     if (c->d != kD) { *err = COMPACTOR_E_UNSUPPORTED; return false; }
     if (c->layers < 1 || c->heads < 1 || c->batch < 1 || c->n_pages < 1 || c->max_pages < 1) return false;
     if ((long long)c->layers * c->heads > 65535 || (long long)c->layers * c->heads * c->batch > 0x7fffffffLL) return false;

@@ -103,30 +103,37 @@ __global__ void fill_lengths_kernel(const __grid_constant__ FillArgs a, const __
 }
 
 // ------------------------------------------------------------------------------------------ evict
-// One cluster of 1 to 8 CTAs per unit; each CTA holds the sort keys of a slice of the unit's slots in shared memory.
+// A cluster of up to 8 CTAs per unit, of which as many work as the unit's length asks for; each holds the sort keys of a
+// slice of the unit's slots in shared memory.
 //   key      the weight as an ordered 32-bit integer; the largest key for a recent token (never below a weight)
 //   1. radix selection of the E-th smallest key, E = n - budget: digits of 11, 11 and 10 bits, one histogram per CTA,
-//      summed over the cluster through distributed shared memory by every CTA alike
+//      summed over the cluster through distributed shared memory by every CTA alike; it ends as soon as all keys of the digit go
 //   2. a bit per slot: evicted or not (of equal keys the higher slots go first)
 //   3. lists of the holes (evicted, below the budget) and the movers (kept, at or above it), both ascending; there are as
 //      many of one as of the other, and the j-th mover's row goes to the j-th hole.  Sources and targets never overlap, so the
 //      rows move in any order, and no more than min(E, budget) of them move: compaction that kept the slots' order
 //      would rewrite nearly the whole unit for one evicted token.
-// Bound by HBM (8 bytes per slot, 1 KB per moved row) for many units; for few or small ones by the chain of block-wide steps.
-constexpr int kEvictThreads = 512;
-constexpr int kEvictWarps = kEvictThreads / 32;
+// The bytes are few (8 per slot, 1 KB per moved row); what bounds it is the chain of block-wide steps, about 8 us per unit
+// whatever its length.  So several small CTAs share an SM and hide each other's waits.
 constexpr int kBins = 2048;
 constexpr int kMaxCluster = 8;
-constexpr int kMaxSlice = 49152;                // slots per CTA: 192 KB of keys
-constexpr int kMaxWords = kMaxSlice / 32;
+constexpr int kSmallThreads = 256, kLargeThreads = 512;
+constexpr int kSmallSlice = 8256, kLargeSlice = 49152;   // most slots per CTA: 33 KB of keys, four CTAs to an SM; 192 KB, one
+constexpr int kLoadBatch = 4;                   // groups of four slots per thread whose weights are in flight together
+constexpr int kRowBatch = 4;                    // rows per warp in flight
 constexpr uint32_t kKeyRecent = 0xffffffffu, kKeyNan = 0xfffffffeu;
 
+template <int kThreads>
 struct EvictShared {
-    int hist[kBins];
-    uint32_t evicted[kMaxWords];                // bit per slot of the slice
-    uint32_t same[kMaxWords];                   // bit per slot whose key cannot be told from the E-th smallest
-    int warp_a[kEvictWarps], warp_b[kEvictWarps];
+    static constexpr int kWords = (kThreads == kSmallThreads ? kSmallSlice : kLargeSlice) / 32;
+    int hist[2][kBins];                         // passes take turns
+    int coarse[2][kBins / 32];
+    uint32_t evicted[kWords];                   // bit per slot of the slice
+    uint32_t same[kWords];                      // bit per slot whose key cannot be told from the E-th smallest
+    uint16_t holes_before[kWords], movers_before[kWords];     // per word of slots
+    int warp_a[kThreads / 32], warp_b[kThreads / 32];
     int holes, movers, ties, bad;               // of this CTA's slice
+    int rank_holes[kMaxCluster], rank_movers[kMaxCluster];
     int digit, left, in_bin;
 };
 
@@ -137,7 +144,8 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 
 // Exclusive prefix over the block of two counts per thread, and their totals.
-__device__ __forceinline__ void block_prefix2(EvictShared& s, int& x, int& y, int& total_x, int& total_y) {
+template <int kThreads>
+__device__ __forceinline__ void block_prefix2(EvictShared<kThreads>& s, int& x, int& y, int& total_x, int& total_y) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int ix = x, iy = y;
 #pragma unroll
@@ -151,7 +159,7 @@ __device__ __forceinline__ void block_prefix2(EvictShared& s, int& x, int& y, in
     int bx = 0, by = 0;
     total_x = total_y = 0;
 #pragma unroll
-    for (int w = 0; w < kEvictWarps; ++w) {
+    for (int w = 0; w < kThreads / 32; ++w) {
         const int cx = s.warp_a[w], cy = s.warp_b[w];
         if (w < warp) { bx += cx; by += cy; }
         total_x += cx; total_y += cy;
@@ -159,14 +167,17 @@ __device__ __forceinline__ void block_prefix2(EvictShared& s, int& x, int& y, in
     x = bx + ix - x; y = by + iy - y;
 }
 
-__global__ void __launch_bounds__(kEvictThreads, 1)
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
+    constexpr int kWarps = kThreads / 32;
     extern __shared__ __align__(16) uint32_t key[];          // [slice_cap]; afterwards the two lists
-    __shared__ __align__(16) EvictShared s;
+    __shared__ __align__(16) EvictShared<kThreads> s;
+    int4* move = reinterpret_cast<int4*>(s.hist[0]);         // a batch of moves, when the histograms are done with: page and slot from, page and slot to
     cg::cluster_group cluster = cg::this_cluster();
-    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int cluster_size = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int unit = a.first_unit + (int)(blockIdx.x / ranks);
+    const int unit = a.first_unit + (int)(blockIdx.x / cluster_size);
     const int n = a.lengths[unit], budget = a.budgets[unit];
     const long long capacity = min((long long)a.max_length, (long long)a.c.max_pages << a.c.page_shift);
     // nothing to do: the same decision in every CTA of the cluster, before any barrier between them
@@ -178,38 +189,76 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
         }
         return;
     }
-    const int slice = ((n + ranks - 1) / ranks + 31) / 32 * 32;              // at most slice_cap: n <= max_length
+    int ranks = 1;                                           // CTAs that this unit needs; a barrier of the cluster waits for those that have not ended
+    while (ranks * slice_cap < n) ++ranks;
+    if (rank >= ranks) return;
+    auto sync_ranks = [&]() {
+        if (ranks == 1) __syncthreads();
+        else cluster.sync();
+    };
+    const int slice = ((n + ranks - 1) / ranks + 31) / 32 * 32;              // at most slice_cap
     const int lo = min(n, rank * slice), count = min(n, lo + slice) - lo;
     const int recent_from = a.recent > 0 ? a.next_position[unit % a.c.batch] - min(a.recent, budget) : 0;
 
     if (tid == 0) s.bad = 0;
+    for (int i = tid; i < 2 * kBins; i += kThreads) s.hist[0][i] = 0;
     __syncthreads();
-    for (int i = tid; i < count; i += kEvictThreads) {
-        const int page = page_of(a.c, unit, lo + i);
-        uint32_t k = 0;
-        if (page < 0) s.bad = 1;
-        else {
-            const long long at = slot_in_pool(a.c, page, lo + i);
-            k = weight_key(a.c.mass[at]);
-            if (a.recent > 0 && a.c.positions[at] >= recent_from) k = kKeyRecent;
+    const int quads = (count + 3) / 4;                       // four slots share a page: one id, one 16-byte load of each pool
+    for (int q0 = tid; q0 < quads; q0 += kThreads * kLoadBatch) {
+        int page[kLoadBatch];
+        int4 pos[kLoadBatch];
+        float4 w[kLoadBatch];
+#pragma unroll
+        for (int k = 0; k < kLoadBatch; ++k) page[k] = page_of(a.c, unit, lo + 4 * min(q0 + k * kThreads, quads - 1));
+#pragma unroll
+        for (int k = 0; k < kLoadBatch; ++k) {
+            const long long at = slot_in_pool(a.c, max(page[k], 0), lo + 4 * min(q0 + k * kThreads, quads - 1));
+            w[k] = *reinterpret_cast<const float4*>(a.c.mass + at);
+            pos[k] = a.recent > 0 ? *reinterpret_cast<const int4*>(a.c.positions + at) : make_int4(0, 0, 0, 0);
         }
-        key[i] = k;
+#pragma unroll
+        for (int k = 0; k < kLoadBatch; ++k) {
+            const int q = q0 + k * kThreads;
+            if (q >= quads) break;
+            if (page[k] < 0) s.bad = 1;
+            const float wk[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+            const int pk[4] = {pos[k].x, pos[k].y, pos[k].z, pos[k].w};
+            uint32_t x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[j] = a.recent > 0 && pk[j] >= recent_from ? kKeyRecent : weight_key(wk[j]);
+                if (4 * q + j < count) atomicAdd(&s.hist[0][x[j] >> 21], 1);
+            }
+            *reinterpret_cast<uint4*>(key + 4 * q) = make_uint4(x[0], x[1], x[2], x[3]);
+        }
     }
 
     // ---- the E-th smallest key
     int left = n - budget;                                   // how many go, among the keys that match `prefix` so far
     uint32_t prefix = 0;
     int shift = 32, in_bin = 0;
-    bool whole_bin = false;
-    for (int pass = 0; pass < 3 && !whole_bin; ++pass) {
+    for (int pass = 0; pass < 3; ++pass) {
         const int bits = pass < 2 ? 11 : 10, next = shift - bits;
-        for (int i = tid; i < kBins; i += kEvictThreads) s.hist[i] = 0;
+        int (&hist)[kBins] = s.hist[pass & 1];
+        if (pass > 0)                                        // (the first digit was counted as the keys came in)
+            for (int q = tid; q < quads; q += kThreads) {
+                const uint4 v = *reinterpret_cast<const uint4*>(key + 4 * q);
+                const uint32_t k[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if ((k[j] >> shift) == prefix && 4 * q + j < count) atomicAdd(&hist[(k[j] >> next) & ((1u << bits) - 1u)], 1);
+            }
         __syncthreads();
-        for (int i = tid; i < count; i += kEvictThreads) {
-            const uint32_t k = key[i];
-            if (pass == 0 || (k >> shift) == prefix) atomicAdd(&s.hist[(k >> next) & ((1u << bits) - 1u)], 1);
+        {                                                    // sums of 32 bins, so that the cluster reads few of them
+            constexpr int kPer = kBins / kThreads, kLanes = 32 / kPer;
+            int sum = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) sum += hist[tid * kPer + i];
+#pragma unroll
+            for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if (tid % kLanes == 0) s.coarse[pass & 1][tid / kLanes] = sum;
         }
-        cluster.sync();
+        sync_ranks();
         if (pass == 0) {                                     // a page that is none: the unit stays as it is
             int bad = 0;
             for (int r = 0; r < ranks; ++r) bad |= cluster.map_shared_rank(&s, r)->bad;
@@ -218,54 +267,69 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
                     if (a.status != nullptr) atomicOr(a.status + unit, COMPACTOR_STATUS_PAGE);
                     a.lengths_out[unit] = n;
                 }
-                cluster.sync();                              // nobody leaves while its shared memory is read
+                sync_ranks();                                // nobody leaves while its shared memory is read
                 return;
             }
         }
-        constexpr int kPer = kBins / kEvictThreads;
-        int c[kPer], sum = 0, dummy = 0, tot, tot2;
+        if (warp == 0) {                                     // the group of 32 bins, then the bin: summed over the cluster, prefix by shuffles
+            int x = 0, y = 0;
+#pragma unroll 4
+            for (int r = 0; r < ranks; ++r) {
+                const int2 v = reinterpret_cast<const int2*>(cluster.map_shared_rank(&s, r)->coarse[pass & 1])[lane];
+                x += v.x; y += v.y;
+            }
+            int upto = x + y;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) c[i] = 0;
-        for (int r = 0; r < ranks; ++r) {
-            const int4 v = *reinterpret_cast<const int4*>(&cluster.map_shared_rank(&s, r)->hist[tid * kPer]);
-            c[0] += v.x; c[1] += v.y; c[2] += v.z; c[3] += v.w;
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, upto, d);
+                if (lane >= d) upto += o;
+            }
+            const int pair = __ffs(__ballot_sync(0xffffffffu, upto >= left)) - 1;         // the last lane's is the number of all that match
+            const int before_pair = __shfl_sync(0xffffffffu, upto - x - y, pair), first = __shfl_sync(0xffffffffu, x, pair);
+            const bool second = before_pair + first < left;
+            const int group = 2 * pair + (second ? 1 : 0), before = before_pair + (second ? first : 0);
+            int c = 0;
+#pragma unroll 4
+            for (int r = 0; r < ranks; ++r) c += cluster.map_shared_rank(&s, r)->hist[pass & 1][group * 32 + lane];
+            upto = c;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, upto, d);
+                if (lane >= d) upto += o;
+            }
+            if (before + upto - c < left && left <= before + upto) { s.digit = group * 32 + lane; s.left = left - (before + upto - c); s.in_bin = c; }
         }
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) sum += c[i];
-        int before = sum;
-        block_prefix2(s, before, dummy, tot, tot2);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (before < left && left <= before + c[i]) { s.digit = tid * kPer + i; s.left = left - before; s.in_bin = c[i]; }
-            before += c[i];
-        }
-        cluster.sync();                                      // the histograms have been read everywhere; s.digit is there
+        __syncthreads();
         prefix = (prefix << bits) | (uint32_t)s.digit;
         left = s.left; in_bin = s.in_bin;
         shift = next;
-        whole_bin = left == in_bin;                          // the rest of the digits decides nothing
-        __syncthreads();
+        if (left == in_bin) break;                           // all keys of the digit go: the rest of the bits decides nothing
+        // the third pass takes the first one's histogram: everybody has read it, or nobody could have passed the second's barrier
+        if (pass == 1) {
+            for (int i = tid; i < kBins; i += kThreads) s.hist[0][i] = 0;
+            __syncthreads();
+        }
     }
 
     // ---- which slots go.  A key whose top bits are below `prefix` goes, one above stays; of those that match, the last `left`.
     const int words = (count + 31) / 32;
-    const int per = (words + kEvictThreads - 1) / kEvictThreads;             // a run of words per thread, so that its prefix is its run's
+    const int per = (words + kThreads - 1) / kThreads;       // a run of words per thread, so that its prefix is its run's
     const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
     const int stay = in_bin - left;                          // matching slots that stay: the lowest ones
-    for (int w = warp; w < words; w += kEvictWarps) {
+    for (int w = warp; w < words; w += kWarps) {
         const int i = w * 32 + lane;
-        const uint32_t top = i < count ? (shift == 0 ? key[i] : key[i] >> shift) : 0xffffffffu;
+        const uint32_t top = i < count ? key[i] >> shift : 0xffffffffu;
         const uint32_t less = __ballot_sync(0xffffffffu, i < count && top < prefix);
         const uint32_t same = __ballot_sync(0xffffffffu, i < count && top == prefix);
         if (lane == 0) { s.evicted[w] = stay == 0 ? less | same : less; s.same[w] = same; }
     }
-    __syncthreads();
     if (stay > 0) {                                          // equal keys on both sides of the line: rank them by slot
+        __syncthreads();
         int at = 0, dummy = 0, tot, tot2;
         for (int w = w0; w < w1; ++w) at += __popc(s.same[w]);
-        block_prefix2(s, at, dummy, tot, tot2);
+        block_prefix2<kThreads>(s, at, dummy, tot, tot2);
         if (tid == 0) s.ties = tot;
-        cluster.sync();
+        sync_ranks();
         for (int r = 0; r < rank; ++r) at += cluster.map_shared_rank(&s, r)->ties;
         for (int w = w0; w < w1; ++w) {
             uint32_t m = s.same[w];
@@ -273,11 +337,10 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
             at += __popc(m);
             s.evicted[w] |= m;
         }
-        __syncthreads();
     }
+    __syncthreads();
 
     // ---- lists, in the place of the keys: this slice's holes, then its movers
-    int holes = 0, movers = 0, n_holes, n_movers;
     auto split = [&](int w, uint32_t& hole, uint32_t& mover) {
         const int first = lo + w * 32;                       // slots [first, first + 32) against the budget
         const uint32_t front = budget >= first + 32 ? 0xffffffffu : budget <= first ? 0u : (1u << (budget - first)) - 1u;
@@ -285,64 +348,96 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
         hole = s.evicted[w] & front & live;
         mover = ~s.evicted[w] & ~front & live;
     };
+    int holes = 0, movers = 0, n_holes, n_movers;
     for (int w = w0; w < w1; ++w) {
         uint32_t h, m;
         split(w, h, m);
         holes += __popc(h); movers += __popc(m);
     }
-    block_prefix2(s, holes, movers, n_holes, n_movers);
+    block_prefix2<kThreads>(s, holes, movers, n_holes, n_movers);
     for (int w = w0; w < w1; ++w) {
         uint32_t h, m;
         split(w, h, m);
-        for (; h != 0u; h &= h - 1u) key[holes++] = lo + w * 32 + __ffs(h) - 1;
-        for (; m != 0u; m &= m - 1u) key[n_holes + movers++] = lo + w * 32 + __ffs(m) - 1;
+        s.holes_before[w] = (uint16_t)holes; s.movers_before[w] = (uint16_t)movers;      // at most kLargeSlice
+        holes += __popc(h); movers += __popc(m);
     }
     if (tid == 0) { s.holes = n_holes; s.movers = n_movers; }
-    cluster.sync();
+    __syncthreads();
+    for (int w = warp; w < words; w += kWarps) {
+        uint32_t h, m;
+        split(w, h, m);
+        const uint32_t below = (1u << lane) - 1u;
+        if (h >> lane & 1u) key[s.holes_before[w] + __popc(h & below)] = lo + w * 32 + lane;
+        if (m >> lane & 1u) key[n_holes + s.movers_before[w] + __popc(m & below)] = lo + w * 32 + lane;
+    }
+    sync_ranks();
+    if (tid < ranks) {
+        const EvictShared<kThreads>* o = cluster.map_shared_rank(&s, tid);
+        s.rank_holes[tid] = o->holes; s.rank_movers[tid] = o->movers;
+    }
+    __syncthreads();
 
-    // ---- rows: the cluster's CTAs share the unit's moves
+    // ---- rows: the cluster's CTAs share the unit's moves.  Batch by batch the threads look up one move each (and move its weight
+    // and position), then the warps copy the rows.
     int total = 0;
-    for (int r = 0; r < ranks; ++r) total += cluster.map_shared_rank(&s, r)->holes;
+    for (int r = 0; r < ranks; ++r) total += s.rank_holes[r];
     const int j0 = (int)((long long)rank * total / ranks), j1 = (int)((long long)(rank + 1) * total / ranks);
-    auto lookup = [&](int j, bool hole) {
-        for (int r = 0; r < ranks; ++r) {
-            const EvictShared* o = cluster.map_shared_rank(&s, r);
-            const int have = hole ? o->holes : o->movers;
-            if (j < have) return (int)cluster.map_shared_rank(key, r)[(hole ? 0 : o->holes) + j];
-            j -= have;
-        }
-        return 0;
-    };
     const int piece = lane & 15;
     __nv_bfloat16* pool = lane < 16 ? a.c.k : a.c.v;
-    constexpr int kInFlight = 4;
-    for (int j = j0 + warp * kInFlight; j < j1; j += kEvictWarps * kInFlight) {
-        uint4 x[kInFlight];
-        long long to[kInFlight], at[kInFlight];
-        float w[kInFlight];
-        int pos[kInFlight];
-#pragma unroll
-        for (int i = 0; i < kInFlight; ++i) {
-            const int jj = min(j + i, j1 - 1);               // loads without a condition stay in flight together
-            const int from_slot = lookup(jj, false), to_slot = lookup(jj, true);
-            const int from_page = page_of(a.c, unit, from_slot), to_page = page_of(a.c, unit, to_slot);
-            x[i] = *(reinterpret_cast<const uint4*>(pool + row_in_pool(a.c, from_page, from_slot)) + piece);
-            to[i] = row_in_pool(a.c, to_page, to_slot);
-            at[i] = slot_in_pool(a.c, to_page, to_slot);
-            const long long from = slot_in_pool(a.c, from_page, from_slot);
-            w[i] = a.c.mass[from];
-            pos[i] = a.c.positions != nullptr ? a.c.positions[from] : 0;
+    for (int jb = j0; jb < j1; jb += kThreads) {
+        const int batch = min(kThreads, j1 - jb);
+        if (tid < batch) {
+            int jh = jb + tid, jm = jh, rh = 0, rm = 0;
+            while (jh >= s.rank_holes[rh]) jh -= s.rank_holes[rh++];
+            while (jm >= s.rank_movers[rm]) jm -= s.rank_movers[rm++];
+            const int to = (int)cluster.map_shared_rank(key, rh)[jh];
+            const int from = (int)cluster.map_shared_rank(key, rm)[s.rank_holes[rm] + jm];
+            const int from_page = page_of(a.c, unit, from), to_page = page_of(a.c, unit, to);
+            move[tid] = make_int4(from_page, from, to_page, to);
+            const long long f = slot_in_pool(a.c, from_page, from), t = slot_in_pool(a.c, to_page, to);
+            const float w = a.c.mass[f];
+            const int pos = a.c.positions != nullptr ? a.c.positions[f] : 0;
+            a.c.mass[t] = w;
+            if (a.c.positions != nullptr) a.c.positions[t] = pos;
         }
+        __syncthreads();
+        for (int i = warp * kRowBatch; i < batch; i += kWarps * kRowBatch) {
+            uint4 x[kRowBatch];
+            long long to[kRowBatch];
 #pragma unroll
-        for (int i = 0; i < kInFlight; ++i) {
-            if (j + i >= j1) break;
-            *(reinterpret_cast<uint4*>(pool + to[i]) + piece) = x[i];
-            if (lane == 0) a.c.mass[at[i]] = w[i];
-            if (lane == 1 && a.c.positions != nullptr) a.c.positions[at[i]] = pos[i];
+            for (int k = 0; k < kRowBatch; ++k) {
+                const int4 mv = move[min(i + k, batch - 1)];       // loads without a condition stay in flight together
+                x[k] = *(reinterpret_cast<const uint4*>(pool + row_in_pool(a.c, mv.x, mv.y)) + piece);
+                to[k] = row_in_pool(a.c, mv.z, mv.w);
+            }
+#pragma unroll
+            for (int k = 0; k < kRowBatch; ++k) {
+                if (i + k >= batch) break;
+                *(reinterpret_cast<uint4*>(pool + to[k]) + piece) = x[k];
+            }
         }
+        __syncthreads();
     }
     if (rank == 0 && tid == 0) a.lengths_out[unit] = budget;
-    cluster.sync();                                          // the lists are read across the cluster until here
+    sync_ranks();                                            // the lists are read across the cluster until here
+}
+
+template <int kThreads>
+cudaError_t launch_evict(const EvictArgs& a, int ranks, cudaStream_t stream) {
+    const int slice_cap = ((a.max_length + ranks - 1) / ranks + 31) / 32 * 32;
+    cudaError_t e = cudaFuncSetAttribute(evict_kernel<kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         (kThreads == kSmallThreads ? kSmallSlice : kLargeSlice) * (int)sizeof(uint32_t));
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.units * ranks)); cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(uint32_t) * (size_t)slice_cap; cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, evict_kernel<kThreads>, a, slice_cap);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
@@ -363,28 +458,18 @@ cudaError_t launch_paged_fill_lengths(const FillArgs& a, const FillTables& t, cu
     return cudaGetLastError();
 }
 
-int evict_max_tokens() { return kMaxCluster * kMaxSlice; }
+int evict_max_tokens() { return kMaxCluster * kLargeSlice; }
 
 cudaError_t launch_paged_evict(const EvictArgs& a, int sm_count, cudaStream_t stream) {
-    // CTAs per unit: enough for their slices to fit, more while the GPU is not full and a slice still has 2048 slots
+    // CTAs of 256 threads, four to an SM, while their slices do and there are many units; else of 512.  More CTAs per unit while the GPU is not full and a
+    // slice still has 2048 slots.
+    const bool small = a.max_length <= kMaxCluster * kSmallSlice && (long long)a.units * kMaxCluster > 2 * sm_count;
+    const int good = small ? kSmallSlice : 12288, resident = small ? 4 * sm_count : 2 * sm_count;
     int ranks = 1;
-    while (ranks < kMaxCluster && (a.max_length > (long long)ranks * kMaxSlice ||
-                                   ((long long)a.units * ranks * 2 <= sm_count && a.max_length > 4096LL * ranks)))
+    while (ranks < kMaxCluster && (a.max_length > (long long)ranks * good ||
+                                   ((long long)a.units * ranks * 2 <= resident && a.max_length > 4096LL * ranks)))
         ranks *= 2;
-    const int slice_cap = ((a.max_length + ranks - 1) / ranks + 31) / 32 * 32;
-    const size_t smem = sizeof(uint32_t) * (size_t)slice_cap;
-    cudaError_t e = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice * (int)sizeof(uint32_t));
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.units * ranks)); cfg.blockDim = dim3(kEvictThreads);
-    cfg.dynamicSmemBytes = smem; cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, evict_kernel, a, slice_cap);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return small ? launch_evict<kSmallThreads>(a, ranks, stream) : launch_evict<kLargeThreads>(a, ranks, stream);
 }
 
 }  // namespace compactor
