@@ -1179,6 +1179,7 @@ extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t 
     a.lengths = lengths; a.lengths_out = lengths_out; a.status = status;
     const size_t per_layer = (size_t)cache->heads * cache->batch;
     if (status != nullptr) CK(cudaMemsetAsync(status + first_layer * per_layer, 0, sizeof(int32_t) * per_layer * shape->layers, st));
+    compactor::set_chain_for(0);
     int done = 0;
     for (a.b0 = 0; a.b0 < shape->batch; a.b0 += kFillSeqs) {
         a.nb = std::min(kFillSeqs, shape->batch - a.b0);
@@ -1260,6 +1261,7 @@ extern "C" int compactor_paged_evict(const compactor_paged_cache* cache, int32_t
     a.lengths = lengths; a.budgets = budgets; a.next_position = next_position;
     a.recent = recent; a.max_length = max_length; a.lengths_out = lengths_out; a.status = status;
     if (status != nullptr) CK(cudaMemsetAsync(status + a.first_unit, 0, sizeof(int32_t) * a.units, st));
+    compactor::set_chain_for(0);
     CK(launch_paged_evict(a, sm_count(), st));
     return COMPACTOR_OK;
 }

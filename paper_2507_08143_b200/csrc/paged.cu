@@ -10,13 +10,14 @@ namespace compactor {
 namespace {
 
 // ------------------------------------------------------------------------------------------ fill
-// 16 threads per row as in the dense gather (compact.cu); what is new is where a row goes: slot lengths[unit] + j of
-// its unit, j its place among the unit's kept rows, found through the page table.  Bound by HBM: 512 bytes read and
-// written per row.
+// Where a row goes: slot lengths[unit] + j of its unit, j its place among the unit's kept rows, found through the page table.  A block
+// moves 128 rows: first a thread per row finds source and target (index, length and page id are three dependent reads,
+// made once per row and not once per 16-byte piece) and moves weight and position, then 16 threads per row move K and V.
+// Bound by HBM: 512 bytes read and written per row.
 constexpr int kFillThreads = 256;
+constexpr int kFillRows = 128;
 constexpr int kFillRowsPerIter = kFillThreads / 16;
-constexpr int kFillSteps = 8;
-constexpr int kFillRows = kFillRowsPerIter * kFillSteps;
+constexpr int kFillBatch = 2;                   // rows per thread in flight
 
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
     uint4 v;
@@ -41,51 +42,74 @@ __device__ __forceinline__ int first_slot(const FillArgs& a, int unit, int rows)
 template <bool ACROSS>
 __global__ void __launch_bounds__(kFillThreads)
 fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTables t) {
-    const int piece = threadIdx.x & 15, sub = threadIdx.x >> 4;
+    __shared__ long long src_k[kFillRows], src_v[kFillRows], dst[kFillRows];       // elements; dst < 0: the row is skipped
+    const int tid = threadIdx.x;
+    pdl_trigger();
+    pdl_wait();
     const int layer = ACROSS ? blockIdx.y : blockIdx.y / a.c.heads;
     const long long per_outer = ACROSS ? (long long)a.c.heads * a.total_keep : a.total_keep;     // rows per layer or (layer, head)
-    const long long scale = ACROSS ? a.c.heads : 1;
-    const long long end = scale * t.cu_keep[a.nb];
-    const long long row0 = scale * t.cu_keep[0] + (long long)blockIdx.x * kFillRows;
+    const int scale = ACROSS ? a.c.heads : 1;
+    const long long end = (long long)scale * t.cu_keep[a.nb];
+    const long long row0 = (long long)scale * t.cu_keep[0] + (long long)blockIdx.x * kFillRows;
+    if (tid < kFillRows) {
+        const long long row = row0 + tid;
+        long long to = -1;
+        if (row < end) {
+            const int local0 = a.idx != nullptr ? __ldg(a.idx + (long long)blockIdx.y * per_outer + row) : 0;
+            const int b = find_segment(t.cu_keep, a.nb, (int)(row / scale));
+            int head, j;
+            if (ACROSS) {
+                const int* offs = a.head_offsets + ((long long)layer * a.c.batch + a.b0 + b) * (a.c.heads + 1);
+                j = (int)(row - (long long)scale * t.cu_keep[b]);
+                head = find_segment(offs, a.c.heads, j);
+                j -= offs[head];
+            } else {
+                head = blockIdx.y - layer * a.c.heads;
+                j = (int)row - t.cu_keep[b];
+            }
+            const int n = t.cu_seqlens[b + 1] - t.cu_seqlens[b];
+            const int local = a.idx != nullptr ? local0 : j;
+            const int unit = ((a.first_layer + layer) * a.c.heads + head) * a.c.batch + a.b0 + b;
+            const int rows = kept_rows(a, t, layer, head, b), first = first_slot(a, unit, rows);
+            if (first >= 0 && j >= 0 && j < rows && (unsigned)local < (unsigned)n) {
+                const int slot = first + j, page = page_of(a.c, unit, slot);
+                if (page >= 0) {
+                    const long long tok = (long long)t.cu_seqlens[b] + local;
+                    to = row_in_pool(a.c, page, slot);
+                    src_k[tid] = layer * a.k.stride_layer + head * a.k.stride_head + tok * a.k.stride_token;
+                    src_v[tid] = layer * a.v.stride_layer + head * a.v.stride_head + tok * a.v.stride_token;
+                    const long long at = slot_in_pool(a.c, page, slot);
+                    if (a.c.mass != nullptr)
+                        a.c.mass[at] = a.mass_in != nullptr ? a.mass_in[((long long)layer * a.c.heads + head) * a.total_tokens + tok] : 0.f;
+                    if (a.c.positions != nullptr)
+                        a.c.positions[at] = (a.first_position != nullptr ? a.first_position[a.b0 + b] : 0) + local;
+                } else if (a.status != nullptr) {
+                    atomicOr(a.status + unit, COMPACTOR_STATUS_PAGE);
+                }
+            }
+        }
+        dst[tid] = to;
+        if (to < 0) src_k[tid] = src_v[tid] = 0;             // read, not written: any address of the tensor will do
+    }
+    __syncthreads();
+    const int piece = tid & 15, sub = tid >> 4;
+    const int rows_here = (int)min((long long)kFillRows, end - row0);
+#pragma unroll 1
+    for (int r0 = sub; r0 < rows_here; r0 += kFillRowsPerIter * kFillBatch) {
+        uint4 kv[kFillBatch], vv[kFillBatch];
 #pragma unroll
-    for (int step = 0; step < kFillSteps; ++step) {
-        const long long row = row0 + step * kFillRowsPerIter + sub;
-        if (row >= end) return;
-        const int b = find_segment(t.cu_keep, a.nb, (int)(row / scale));
-        int head, j;
-        if (ACROSS) {
-            const int* offs = a.head_offsets + ((long long)layer * a.c.batch + a.b0 + b) * (a.c.heads + 1);
-            j = (int)(row - scale * t.cu_keep[b]);
-            head = find_segment(offs, a.c.heads, j);
-            j -= offs[head];
-        } else {
-            head = blockIdx.y - layer * a.c.heads;
-            j = (int)row - t.cu_keep[b];
+        for (int u = 0; u < kFillBatch; ++u) {               // without a condition, so that they are in flight together
+            const int r = min(r0 + u * kFillRowsPerIter, rows_here - 1);
+            kv[u] = ld_stream(reinterpret_cast<const uint4*>(a.k.ptr + src_k[r]) + piece);
+            vv[u] = ld_stream(reinterpret_cast<const uint4*>(a.v.ptr + src_v[r]) + piece);
         }
-        const int n = t.cu_seqlens[b + 1] - t.cu_seqlens[b];
-        const int local = a.idx != nullptr ? __ldg(a.idx + (long long)blockIdx.y * per_outer + row) : j;
-        const int unit = ((a.first_layer + layer) * a.c.heads + head) * a.c.batch + a.b0 + b;
-        const int rows = kept_rows(a, t, layer, head, b), first = first_slot(a, unit, rows);
-        if (first < 0 || j < 0 || j >= rows || (unsigned)local >= (unsigned)n) continue;
-        const int slot = first + j;
-        const int page = page_of(a.c, unit, slot);
-        if (page < 0) {
-            if (piece == 0 && a.status != nullptr) atomicOr(a.status + unit, COMPACTOR_STATUS_PAGE);
-            continue;
+#pragma unroll
+        for (int u = 0; u < kFillBatch; ++u) {
+            const int r = r0 + u * kFillRowsPerIter;
+            if (r >= rows_here || dst[r] < 0) continue;
+            *(reinterpret_cast<uint4*>(a.c.k + dst[r]) + piece) = kv[u];
+            *(reinterpret_cast<uint4*>(a.c.v + dst[r]) + piece) = vv[u];
         }
-        const long long tok = (long long)t.cu_seqlens[b] + local;
-        const long long to = row_in_pool(a.c, page, slot);
-        const uint4 kv = ld_stream(reinterpret_cast<const uint4*>(a.k.ptr + layer * a.k.stride_layer + head * a.k.stride_head +
-                                                                  tok * a.k.stride_token) + piece);
-        const uint4 vv = ld_stream(reinterpret_cast<const uint4*>(a.v.ptr + layer * a.v.stride_layer + head * a.v.stride_head +
-                                                                  tok * a.v.stride_token) + piece);
-        reinterpret_cast<uint4*>(a.c.k + to)[piece] = kv;
-        reinterpret_cast<uint4*>(a.c.v + to)[piece] = vv;
-        if (piece == 0 && a.c.mass != nullptr)
-            a.c.mass[slot_in_pool(a.c, page, slot)] =
-                a.mass_in != nullptr ? a.mass_in[((long long)layer * a.c.heads + head) * a.total_tokens + tok] : 0.f;
-        if (piece == 1 && a.c.positions != nullptr)
-            a.c.positions[slot_in_pool(a.c, page, slot)] = (a.first_position != nullptr ? a.first_position[a.b0 + b] : 0) + local;
     }
 }
 
@@ -93,6 +117,8 @@ fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTabl
 // fill reads.
 __global__ void fill_lengths_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTables t) {
     const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    pdl_trigger();
+    pdl_wait();
     if (i >= (long long)a.layers * a.c.heads * a.nb) return;
     const int b = (int)(i % a.nb), lh = (int)(i / a.nb), layer = lh / a.c.heads, head = lh - layer * a.c.heads;
     const int unit = ((a.first_layer + layer) * a.c.heads + head) * a.c.batch + a.b0 + b;
@@ -116,11 +142,10 @@ __global__ void fill_lengths_kernel(const __grid_constant__ FillArgs a, const __
 // The bytes are few (8 per slot, 1 KB per moved row); what bounds it is the chain of block-wide steps, about 8 us per unit
 // whatever its length.  So several small CTAs share an SM and hide each other's waits.
 constexpr int kBins = 2048;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;                 // 8 is what every launch may use
 constexpr int kSmallThreads = 256, kLargeThreads = 512;
 constexpr int kSmallSlice = 8256, kLargeSlice = 49152;   // most slots per CTA: 33 KB of keys, four CTAs to an SM; 192 KB, one
-constexpr int kLoadBatch = 4;                   // groups of four slots per thread whose weights are in flight together
-constexpr int kRowBatch = 4;                    // rows per warp in flight
+constexpr int kLoadBatch = 8;                   // groups of four slots per thread whose weights are in flight together
 constexpr uint32_t kKeyRecent = 0xffffffffu, kKeyNan = 0xfffffffeu;
 
 template <int kThreads>
@@ -130,7 +155,6 @@ struct EvictShared {
     int coarse[2][kBins / 32];
     uint32_t evicted[kWords];                   // bit per slot of the slice
     uint32_t same[kWords];                      // bit per slot whose key cannot be told from the E-th smallest
-    uint16_t holes_before[kWords], movers_before[kWords];     // per word of slots
     int warp_a[kThreads / 32], warp_b[kThreads / 32];
     int holes, movers, ties, bad;               // of this CTA's slice
     int rank_holes[kMaxCluster], rank_movers[kMaxCluster];
@@ -167,10 +191,12 @@ __device__ __forceinline__ void block_prefix2(EvictShared<kThreads>& s, int& x, 
     x = bx + ix - x; y = by + iy - y;
 }
 
+// One unit.  `part`: which units the launch is for.
+enum { kEvictAll, kEvictLong, kEvictShort };
 template <int kThreads>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
-evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
+__device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, int part) {
     constexpr int kWarps = kThreads / 32;
+    constexpr int kRowBatch = kThreads == kSmallThreads ? 4 : 8;     // rows per warp in flight
     extern __shared__ __align__(16) uint32_t key[];          // [slice_cap]; afterwards the two lists
     __shared__ __align__(16) EvictShared<kThreads> s;
     int4* move = reinterpret_cast<int4*>(s.hist[0]);         // a batch of moves, when the histograms are done with: page and slot from, page and slot to
@@ -180,6 +206,7 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
     const int unit = a.first_unit + (int)(blockIdx.x / cluster_size);
     const int n = a.lengths[unit], budget = a.budgets[unit];
     const long long capacity = min((long long)a.max_length, (long long)a.c.max_pages << a.c.page_shift);
+    if (part == kEvictLong ? n <= kSmallSlice : part == kEvictShort && n > kSmallSlice) return;
     // nothing to do: the same decision in every CTA of the cluster, before any barrier between them
     if (n < 0 || budget < 0 || n <= budget || n > capacity || budget == 0) {
         if (rank == 0 && tid == 0) {
@@ -201,27 +228,31 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
     const int recent_from = a.recent > 0 ? a.next_position[unit % a.c.batch] - min(a.recent, budget) : 0;
 
     if (tid == 0) s.bad = 0;
-    for (int i = tid; i < 2 * kBins; i += kThreads) s.hist[0][i] = 0;
+    for (int i = tid; i < 2 * kBins / 4; i += kThreads) reinterpret_cast<int4*>(s.hist)[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
+    const uint32_t key_s = (uint32_t)__cvta_generic_to_shared(key);
     const int quads = (count + 3) / 4;                       // four slots share a page: one id, one 16-byte load of each pool
     for (int q0 = tid; q0 < quads; q0 += kThreads * kLoadBatch) {
         int page[kLoadBatch];
         int4 pos[kLoadBatch];
-        float4 w[kLoadBatch];
 #pragma unroll
         for (int k = 0; k < kLoadBatch; ++k) page[k] = page_of(a.c, unit, lo + 4 * min(q0 + k * kThreads, quads - 1));
 #pragma unroll
-        for (int k = 0; k < kLoadBatch; ++k) {
-            const long long at = slot_in_pool(a.c, max(page[k], 0), lo + 4 * min(q0 + k * kThreads, quads - 1));
-            w[k] = *reinterpret_cast<const float4*>(a.c.mass + at);
+        for (int k = 0; k < kLoadBatch; ++k) {               // weights into the keys' place, positions into registers: all in flight at once
+            const int q = min(q0 + k * kThreads, quads - 1);
+            const long long at = slot_in_pool(a.c, max(page[k], 0), lo + 4 * q);
+            if (q0 + k * kThreads < quads)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(key_s + 16 * q), "l"(a.c.mass + at) : "memory");
             pos[k] = a.recent > 0 ? *reinterpret_cast<const int4*>(a.c.positions + at) : make_int4(0, 0, 0, 0);
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");     // each thread reads only what it copied itself
 #pragma unroll
         for (int k = 0; k < kLoadBatch; ++k) {
             const int q = q0 + k * kThreads;
             if (q >= quads) break;
             if (page[k] < 0) s.bad = 1;
-            const float wk[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+            const float4 w = *reinterpret_cast<const float4*>(key + 4 * q);
+            const float wk[4] = {w.x, w.y, w.z, w.w};
             const int pk[4] = {pos[k].x, pos[k].y, pos[k].z, pos[k].w};
             uint32_t x[4];
 #pragma unroll
@@ -316,14 +347,24 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
     const int per = (words + kThreads - 1) / kThreads;       // a run of words per thread, so that its prefix is its run's
     const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
     const int stay = in_bin - left;                          // matching slots that stay: the lowest ones
-    for (int w = warp; w < words; w += kWarps) {
-        const int i = w * 32 + lane;
-        const uint32_t top = i < count ? key[i] >> shift : 0xffffffffu;
-        const uint32_t less = __ballot_sync(0xffffffffu, i < count && top < prefix);
-        const uint32_t same = __ballot_sync(0xffffffffu, i < count && top == prefix);
-        if (lane == 0) { s.evicted[w] = stay == 0 ? less | same : less; s.same[w] = same; }
-    }
-    if (stay > 0) {                                          // equal keys on both sides of the line: rank them by slot
+    const uint32_t rest = shift == 0 ? 0u : (1u << shift) - 1u;
+    const uint32_t first_match = prefix << shift, last_match = first_match | rest;
+    if (stay == 0) {                                         // everything up to last_match goes
+#pragma unroll 4
+        for (int w = warp; w < words; w += kWarps) {
+            const uint32_t k = key[w * 32 + lane];           // (behind `count` up to a quad's end: masked below)
+            const uint32_t m = __ballot_sync(0xffffffffu, k <= last_match);
+            if (lane == 0) s.evicted[w] = m;
+        }
+        __syncthreads();
+    } else {                                                 // equal keys on both sides of the line: rank them by slot
+        for (int w = warp; w < words; w += kWarps) {
+            const uint32_t k = key[w * 32 + lane];
+            const bool in = w * 32 + lane < count;
+            const uint32_t less = __ballot_sync(0xffffffffu, in && k < first_match);
+            const uint32_t same = __ballot_sync(0xffffffffu, in && k >= first_match && k <= last_match);
+            if (lane == 0) { s.evicted[w] = less; s.same[w] = same; }
+        }
         __syncthreads();
         int at = 0, dummy = 0, tot, tot2;
         for (int w = w0; w < w1; ++w) at += __popc(s.same[w]);
@@ -338,7 +379,6 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
             s.evicted[w] |= m;
         }
     }
-    __syncthreads();
 
     // ---- lists, in the place of the keys: this slice's holes, then its movers
     auto split = [&](int w, uint32_t& hole, uint32_t& mover) {
@@ -354,22 +394,14 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
         split(w, h, m);
         holes += __popc(h); movers += __popc(m);
     }
-    block_prefix2<kThreads>(s, holes, movers, n_holes, n_movers);
+    block_prefix2<kThreads>(s, holes, movers, n_holes, n_movers);      // (its barriers also end the reading of the keys)
     for (int w = w0; w < w1; ++w) {
         uint32_t h, m;
         split(w, h, m);
-        s.holes_before[w] = (uint16_t)holes; s.movers_before[w] = (uint16_t)movers;      // at most kLargeSlice
-        holes += __popc(h); movers += __popc(m);
+        for (; h != 0u; h &= h - 1u) key[holes++] = lo + w * 32 + __ffs(h) - 1;
+        for (; m != 0u; m &= m - 1u) key[n_holes + movers++] = lo + w * 32 + __ffs(m) - 1;
     }
     if (tid == 0) { s.holes = n_holes; s.movers = n_movers; }
-    __syncthreads();
-    for (int w = warp; w < words; w += kWarps) {
-        uint32_t h, m;
-        split(w, h, m);
-        const uint32_t below = (1u << lane) - 1u;
-        if (h >> lane & 1u) key[s.holes_before[w] + __popc(h & below)] = lo + w * 32 + lane;
-        if (m >> lane & 1u) key[n_holes + s.movers_before[w] + __popc(m & below)] = lo + w * 32 + lane;
-    }
     sync_ranks();
     if (tid < ranks) {
         const EvictShared<kThreads>* o = cluster.map_shared_rank(&s, tid);
@@ -422,21 +454,45 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
     sync_ranks();                                            // the lists are read across the cluster until here
 }
 
+// kEvictShort runs beside a launch for the long units, which holds it back only from ending: what came before that launch is
+// complete when it lets this one start, and the two touch different units.  (A length that the other launch has already replaced,
+// where lengths_out is lengths, reads as a unit at its budget, which stays as it is.)
 template <int kThreads>
-cudaError_t launch_evict(const EvictArgs& a, int ranks, cudaStream_t stream) {
-    const int slice_cap = ((a.max_length + ranks - 1) / ranks + 31) / 32 * 32;
-    cudaError_t e = cudaFuncSetAttribute(evict_kernel<kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+__global__ void __launch_bounds__(kThreads, kThreads == kSmallThreads ? 4 : 1)
+evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap, int part) {
+    if (part != kEvictShort) pdl_wait();
+    pdl_trigger();
+    evict_unit<kThreads>(a, slice_cap, part);
+    if (part == kEvictShort) pdl_wait();
+}
+
+template <int kThreads>
+cudaError_t launch_evict(const EvictArgs& a, int ranks, int max_length, int part, cudaStream_t stream) {
+    const auto kernel = evict_kernel<kThreads>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          (kThreads == kSmallThreads ? kSmallSlice : kLargeSlice) * (int)sizeof(uint32_t));
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.units * ranks)); cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sizeof(uint32_t) * (size_t)slice_cap; cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.blockDim = dim3(kThreads); cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, evict_kernel<kThreads>, a, slice_cap);
+    cfg.numAttrs = pdl_enabled(kPdlOther) ? 2 : 1;
+    int slice_cap = 0;
+    for (;; ranks -= 2) {
+        slice_cap = ((max_length + ranks - 1) / ranks + 31) / 32 * 32;
+        cfg.gridDim = dim3((unsigned)(a.units * ranks));
+        cfg.dynamicSmemBytes = sizeof(uint32_t) * (size_t)slice_cap;
+        attr[0].val.clusterDim.x = ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        if (ranks <= 8) break;
+        int fit = 0;                                         // more than 8 CTAs pay if all units get theirs at once
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+            cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg) == cudaSuccess && fit >= a.units) break;
+        (void)cudaGetLastError();
+    }
+    e = cudaLaunchKernelEx(&cfg, kernel, a, slice_cap, part);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -447,29 +503,35 @@ cudaError_t launch_paged_fill(const FillArgs& a, const FillTables& t, cudaStream
     const long long rows = (long long)(t.cu_keep[a.nb] - t.cu_keep[0]) * (across ? a.c.heads : 1);
     if (rows == 0) return cudaSuccess;
     const dim3 grid((unsigned)((rows + kFillRows - 1) / kFillRows), across ? a.layers : a.layers * a.c.heads);
-    if (across) fill_kernel<true><<<grid, kFillThreads, 0, stream>>>(a, t);
-    else fill_kernel<false><<<grid, kFillThreads, 0, stream>>>(a, t);
-    return cudaGetLastError();
+    return launch_chained(kPdlOther, across ? fill_kernel<true> : fill_kernel<false>, grid, dim3(kFillThreads), 0, stream, a, t);
 }
 
 cudaError_t launch_paged_fill_lengths(const FillArgs& a, const FillTables& t, cudaStream_t stream) {
     const long long units = (long long)a.layers * a.c.heads * a.nb;
-    fill_lengths_kernel<<<(unsigned)((units + 255) / 256), 256, 0, stream>>>(a, t);
-    return cudaGetLastError();
+    return launch_chained(kPdlOther, fill_lengths_kernel, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, stream, a, t);
 }
 
-int evict_max_tokens() { return kMaxCluster * kLargeSlice; }
+int evict_max_tokens() { return 8 * kLargeSlice; }
 
 cudaError_t launch_paged_evict(const EvictArgs& a, int sm_count, cudaStream_t stream) {
-    // CTAs of 256 threads, four to an SM, while their slices do and there are many units; else of 512.  More CTAs per unit while the GPU is not full and a
-    // slice still has 2048 slots.
-    const bool small = a.max_length <= kMaxCluster * kSmallSlice && (long long)a.units * kMaxCluster > 2 * sm_count;
-    const int good = small ? kSmallSlice : 12288, resident = small ? 4 * sm_count : 2 * sm_count;
+    // Many units: CTAs of 256 threads, four to an SM; where some units may need several CTAs, those go in a launch of clusters, the others
+    // in one of single CTAs beside it (one launch of clusters for all left most of their CTAs without work: 128 of 512 ragged
+    // units of up to 32768 tokens 57 us against WHAT).  Few units or very long ones: CTAs of 512 threads, more of them per unit while
+    // the GPU is not full and a slice still has 2048 slots.
+    const int n = a.max_length;
+    cudaError_t e;
+    if (n <= 8 * kSmallSlice && (long long)a.units * 8 > 2 * sm_count) {
+        if (n <= kSmallSlice) return launch_evict<kSmallThreads>(a, 1, n, kEvictAll, stream);
+        int ranks = 2;
+        while (n > ranks * kSmallSlice) ranks *= 2;
+        e = launch_evict<kSmallThreads>(a, ranks, n, kEvictLong, stream);
+        return e != cudaSuccess ? e : launch_evict<kSmallThreads>(a, 1, kSmallSlice, kEvictShort, stream);
+    }
     int ranks = 1;
-    while (ranks < kMaxCluster && (a.max_length > (long long)ranks * good ||
-                                   ((long long)a.units * ranks * 2 <= resident && a.max_length > 4096LL * ranks)))
+    while ((ranks < 8 && n > (long long)ranks * 12288) ||
+           (ranks < kMaxCluster && (long long)a.units * ranks * 2 <= sm_count && n > 4096LL * ranks))
         ranks *= 2;
-    return small ? launch_evict<kSmallThreads>(a, ranks, stream) : launch_evict<kLargeThreads>(a, ranks, stream);
+    return launch_evict<kLargeThreads>(a, ranks, n, kEvictAll, stream);
 }
 
 }  // namespace compactor
