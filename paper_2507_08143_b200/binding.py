@@ -1,4 +1,5 @@
-"""ctypes binding of the C-ABI library: argument marshalling only.
+"""Binding of the C-ABI library: argument marshalling only, by ctypes, and for the calls of a decoding loop by the compiled
+`_fastcall` beside it.
 
 Function names mirror the C entry points of `include/compactor.h`.  Device buffers are torch
 CUDA tensors (torch is used for device memory and streams, nothing else); every step of the
@@ -113,6 +114,11 @@ def _load() -> ctypes.CDLL:
 
 LIB = _load()
 LIB_PATH = _build.LIB
+
+from . import _fastcall  # noqa: E402  (built with the library)
+
+_fastcall.bind(*[ctypes.cast(f, c_void_p).value for f in (LIB.compactor_paged_fill, LIB.compactor_paged_attention,
+                                                         LIB.compactor_paged_evict)])
 
 EXPORTS = ["compactor_version", "compactor_error_string", "compactor_make_sketch", "compactor_make_sketch_srht", "compactor_keep_count",
            "compactor_calibrated_ratio", "compactor_fit_calibration", "compactor_workspace_bytes", "compactor_score", "compactor_select",
@@ -389,34 +395,8 @@ class PagedCache:
                                      None if mass is None else mass.data_ptr(), None if positions is None else positions.data_ptr(),
                                      page_table.data_ptr(), self.n_pages, self.page_tokens, self.max_pages,
                                      self.layers, self.heads, self.batch, self.d)
-
-    def _stream(self) -> c_void_p:
-        if self.device.type != "cuda" or self.device.index != torch.cuda.current_device():
-            raise ValueError(f"the cache lives on {self.device}, which is not the current CUDA device")
-        return _stream()
-
-    def _per_unit(self, t: Optional[torch.Tensor], name: str) -> Optional[int]:
-        """Address of an int32 [layers, heads, batch] array (any shape of that many elements)."""
-        if t is None:
-            return None
-        if t.dtype != torch.int32 or t.numel() != self.units or not t.is_contiguous() or t.device != self.device:
-            raise ValueError(f"{name}: contiguous int32, one entry per (layer, head, sequence), on the cache's device")
-        return t.data_ptr()
-
-    def _per_sequence(self, t: Optional[torch.Tensor], name: str) -> Optional[int]:
-        if t is None:
-            return None
-        if t.dtype != torch.int32 or t.numel() != self.batch or not t.is_contiguous() or t.device != self.device:
-            raise ValueError(f"{name}: contiguous int32 [batch] on the cache's device")
-        return t.data_ptr()
-
-    def _rows(self, t: torch.Tensor, heads: int, name: str) -> CompactorRows:
-        if t.dtype != torch.bfloat16 or t.shape != (self.batch, heads, self.d) or t.stride(2) != 1 or t.device != self.device:
-            raise ValueError(f"{name}: bf16 [{self.batch}, {heads}, {self.d}], contiguous along the last axis, on the cache's device")
-        return CompactorRows(t.data_ptr(), t.stride(0), t.stride(1))
-
-
-_NO_ROWS = CompactorRows(None, 0, 0)
+        self._address = ctypes.addressof(self.c)
+        self._device = self.device.index if self.device.type == "cuda" else -1
 
 
 def paged_fill(cache: PagedCache, shape: Shape, k_cache: torch.Tensor, v_cache: torch.Tensor, keep_counts: Sequence[int],
@@ -426,24 +406,8 @@ def paged_fill(cache: PagedCache, shape: Shape, k_cache: torch.Tensor, v_cache: 
                status: Optional[torch.Tensor] = None) -> None:
     """Compaction into pages: the kept rows (`idx`, and `head_offsets` after a selection across heads; without `idx` the first
     keep_counts[b] rows of every sequence) of k_cache / v_cache [layers, heads, tokens, d] go behind `lengths`."""
-    stream = cache._stream()
-    total, kept = shape.total_tokens, sum(int(k) for k in keep_counts)
-    want = (shape.layers, shape.heads, total, shape.d)
-    if len(keep_counts) != shape.batch:
-        raise ValueError("keep_counts: one per sequence")
-    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if t.shape != want or t.device != cache.device:
-            raise ValueError(f"{name}: {want} on the cache's device")
-    for t, dtype, n, name in ((idx, torch.int32, shape.layers * shape.heads * kept, "idx"),
-                              (head_offsets, torch.int32, shape.layers * shape.batch * (shape.heads + 1), "head_offsets"),
-                              (mass_in, torch.float32, shape.layers * shape.heads * total, "mass_in")):
-        if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != cache.device):
-            raise ValueError(f"{name}: contiguous {dtype} of {n} elements on the cache's device")
-    _check(LIB.compactor_paged_fill(byref(cache.c), first_layer, byref(shape.c), mat(k_cache), mat(v_cache), _ptr(idx),
-                                    _ptr(head_offsets), _keep_array(keep_counts), _ptr(mass_in),
-                                    cache._per_sequence(first_position, "first_position"), cache._per_unit(lengths, "lengths"),
-                                    cache._per_unit(lengths_out, "lengths_out"), cache._per_unit(status, "status"), stream),
-           "compactor_paged_fill")
+    _check(_fastcall.fill(cache._address, cache._device, first_layer, ctypes.addressof(shape.c), k_cache, v_cache, keep_counts, idx,
+                          head_offsets, mass_in, first_position, lengths, lengths_out, status), "compactor_paged_fill")
 
 
 def decode_options(q_per_kv: int, max_length: int, scale: float = 128 ** -0.5, softcap: float = 0.0,
@@ -465,22 +429,8 @@ def paged_attention(cache: PagedCache, layer: int, opt: CompactorDecodeOptions, 
                     lse_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
     """Attention of one new token per sequence: q, out [batch, heads * q_per_kv, d], k_new, v_new [batch, heads, d],
     lse_out fp32 [batch, heads * q_per_kv]; `lengths` [layers, heads, batch] without the new token, left as it is."""
-    stream = cache._stream()
-    q_heads = cache.heads * opt.q_per_kv
-    if lse_out is not None and (lse_out.dtype != torch.float32 or lse_out.numel() != cache.batch * q_heads or
-                                not lse_out.is_contiguous() or lse_out.device != cache.device):
-        raise ValueError("lse_out: contiguous fp32 [batch, heads * q_per_kv] on the cache's device")
-    if workspace.device != cache.device or not workspace.is_contiguous():
-        raise ValueError("workspace: contiguous, on the cache's device")
-    if (k_new is None) != (v_new is None):
-        raise ValueError("k_new and v_new come together")
-    _check(LIB.compactor_paged_attention(byref(cache.c), layer, byref(opt), cache._rows(q, q_heads, "q"),
-                                         _NO_ROWS if k_new is None else cache._rows(k_new, cache.heads, "k_new"),
-                                         _NO_ROWS if v_new is None else cache._rows(v_new, cache.heads, "v_new"),
-                                         cache._per_sequence(new_positions, "new_positions"), cache._per_unit(lengths, "lengths"),
-                                         cache._rows(out, q_heads, "out"), None if lse_out is None else lse_out.data_ptr(),
-                                         cache._per_unit(status, "status"), workspace.data_ptr(), workspace.nbytes, stream),
-           "compactor_paged_attention")
+    _check(_fastcall.attention(cache._address, cache._device, layer, ctypes.addressof(opt), q, lengths, out, workspace, k_new, v_new,
+                               new_positions, lse_out, status), "compactor_paged_attention")
 
 
 def paged_evict(cache: PagedCache, lengths: torch.Tensor, budgets: torch.Tensor, lengths_out: torch.Tensor, max_length: int,
@@ -488,11 +438,8 @@ def paged_evict(cache: PagedCache, lengths: torch.Tensor, budgets: torch.Tensor,
                 status: Optional[torch.Tensor] = None) -> None:
     """Evicts every unit that holds more than its budget down to it: the `recent` newest tokens and those of the greatest
     accumulated weight stay.  lengths, budgets, lengths_out: int32 [layers, heads, batch]; lengths_out may be lengths."""
-    _check(LIB.compactor_paged_evict(byref(cache.c), first_layer, cache.layers - first_layer if layers is None else layers,
-                                     cache._per_unit(lengths, "lengths"), cache._per_unit(budgets, "budgets"),
-                                     cache._per_sequence(next_position, "next_position"), recent, max_length,
-                                     cache._per_unit(lengths_out, "lengths_out"), cache._per_unit(status, "status"),
-                                     cache._stream()), "compactor_paged_evict")
+    _check(_fastcall.evict(cache._address, cache._device, first_layer, cache.layers - first_layer if layers is None else layers, lengths,
+                           budgets, next_position, recent, max_length, lengths_out, status), "compactor_paged_evict")
 
 
 def wait_selftest() -> int:

@@ -658,8 +658,9 @@ join_kernel(const __grid_constant__ DecodeArgs a, int join_blocks, int chunk, in
 
 cudaError_t launch_paged_attention(const DecodeArgs& a, int sm_count, cudaStream_t stream) {
     const int grid = a.workers / kWarps;
+    static std::atomic<unsigned long long> done[2];
     auto kernel = a.g <= 8 ? decode_kernel<1> : decode_kernel<2>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+    cudaError_t e = allow_smem(kernel, (int)kSmemBytes, done[a.g <= 8 ? 0 : 1]);
     if (e != cudaSuccess) return e;
     if ((e = launch_chained(kPdlOther, kernel, dim3(grid), dim3(kThreads), kSmemBytes, stream, a)) != cudaSuccess) return e;
     // the second kernel: 16 warps a block where its blocks do not fill the GPU anyway

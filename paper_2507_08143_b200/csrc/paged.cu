@@ -469,8 +469,8 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap, int part) {
 template <int kThreads>
 cudaError_t launch_evict(const EvictArgs& a, int ranks, int max_length, int part, cudaStream_t stream) {
     const auto kernel = evict_kernel<kThreads>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (kThreads == kSmallThreads ? kSmallSlice : kLargeSlice) * (int)sizeof(uint32_t));
+    static std::atomic<unsigned long long> done;
+    cudaError_t e = allow_smem(kernel, (kThreads == kSmallThreads ? kSmallSlice : kLargeSlice) * (int)sizeof(uint32_t), done);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];

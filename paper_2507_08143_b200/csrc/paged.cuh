@@ -1,5 +1,7 @@
 // Device-side view of a paged cache (compactor_paged_cache) shared by the kernels that fill, read and evict it.
 #pragma once
+#include <atomic>
+
 #include "common.cuh"
 
 namespace compactor {
@@ -29,6 +31,20 @@ __device__ __forceinline__ long long row_in_pool(const Paged& c, int page, int s
 // Index of a slot in the weight and position pools.
 __device__ __forceinline__ long long slot_in_pool(const Paged& c, int page, int slot) {
     return ((long long)page << c.page_shift) + (slot & ((1 << c.page_shift) - 1));
+}
+
+// Dynamic shared memory limit of a kernel, set on its first launch on each device (`done`: a static of the caller; setting it twice
+// from two threads does no harm).
+template <typename K>
+inline cudaError_t allow_smem(K kernel, int bytes, std::atomic<unsigned long long>& done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+    if (bit != 0 && (done.load(std::memory_order_relaxed) & bit) != 0) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 // Sequences per launch of the fill kernel: their prefix tables travel as kernel arguments.

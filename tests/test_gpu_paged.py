@@ -481,6 +481,24 @@ def test_evict_long_units_shared_by_a_cluster(n, b):
     run_evict([[[n]]], [[[b]]], page=256, recent=100, weights=lambda u, t: w[t], seed=1)
 
 
+@pytest.mark.parametrize("alias", [False, True])
+def test_evict_of_many_units_some_of_them_long(alias):
+    # 48 units, so that long and short ones go their own ways; lengths around the border between them, units at their budget,
+    # empty ones and refused ones among them
+    rng = np.random.default_rng(4)
+    lengths = rng.integers(1, 300, size=(2, 4, 6)).astype(np.int32)
+    lengths[0, 0] = [8256, 8257, 20000, 8300, 16513, 9000]
+    lengths[1, 2] = [8258, 100, -1, 0, 12000, 31]
+    budgets = np.maximum(0, lengths - rng.integers(-2, 200, size=lengths.shape)).astype(np.int32)
+    budgets[0, 0] = [8000, 8256, 50, 8300, 9000, 0]
+    budgets[1, 2, 4] = -1
+    st = run_evict(lengths, budgets, page=32, recent=16, alias=alias, seed=6)
+    assert np.all(st == 0)
+    lengths[0, 0, 2] = 20001                                             # one token more than the call allows
+    st = run_evict(lengths, budgets, page=32, recent=16, alias=alias, seed=7, max_length=20000)
+    assert st[0, 0, 2] == 16 and st.sum() == 16
+
+
 def test_evict_refuses_units_beyond_the_bound_or_with_a_bad_page():
     from paper_2507_08143_b200 import binding as B
     st = run_evict([[[50, 30]]], [[[20, 20]]], max_length=40)

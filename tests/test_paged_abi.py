@@ -114,15 +114,57 @@ def test_binding_refuses_tensors_of_other_shapes():
                 dict(mass=torch.zeros(4, 8)), dict(positions=torch.zeros(4, 16)), dict(v_pages=torch.zeros(4, 128, 16, dtype=torch.bfloat16).transpose(1, 2))):
         with pytest.raises(ValueError):
             B.PagedCache(**{**dict(k_pages=k, v_pages=k, page_table=table), **bad})
-    with pytest.raises(ValueError, match="current CUDA device"):          # a cache that does not live on the current device
-        B.paged_evict(c, torch.zeros(1, 2, 3, dtype=torch.int32), torch.zeros(1, 2, 3, dtype=torch.int32),
-                      torch.zeros(1, 2, 3, dtype=torch.int32), 32)
-    with pytest.raises(ValueError):
-        c._per_unit(torch.zeros(5, dtype=torch.int32), "lengths")
-    with pytest.raises(ValueError):
-        c._per_sequence(torch.zeros(3), "new_positions")
-    with pytest.raises(ValueError):
-        c._rows(torch.zeros(3, 5, 128, dtype=torch.bfloat16), 4, "q")
+
+
+def test_calls_refuse_tensors_of_other_shapes_types_and_devices():
+    # every wrong tensor is named; with all of them right, a cache outside the current CUDA device is what is left to refuse
+    k = torch.zeros(4, 16, 128, dtype=torch.bfloat16)
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    c = B.PagedCache(k, k.clone(), i32(1, 2, 3, 2), mass=torch.zeros(4, 16), positions=i32(4, 16))
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
+    ok = dict(q=bf(3, 4, 128), lengths=i32(1, 2, 3), out=bf(3, 4, 128), workspace=bf(100), k_new=bf(3, 2, 128), v_new=bf(3, 2, 128),
+              new_positions=i32(3), lse_out=torch.zeros(3, 4), status=i32(1, 2, 3))
+    call = lambda **kw: B.paged_attention(c, 0, B.decode_options(2, 20), **{**ok, **kw})
+    with pytest.raises(ValueError, match="current CUDA device"):
+        call()
+    for name, bad in (("q", bf(3, 5, 128)), ("q", bf(2, 4, 128)), ("q", bf(3, 4, 64)), ("q", torch.zeros(3, 4, 128)), ("q", bf(3, 128, 4).transpose(1, 2)),
+                      ("out", bf(3, 2, 128)), ("out", bf(12, 128)), ("k_new", bf(3, 4, 128)), ("v_new", bf(3, 2, 128).half()),
+                      ("lengths", i32(5)), ("lengths", i32(1, 2, 3).long()), ("lengths", i32(1, 2, 6)[..., ::2]), ("new_positions", i32(4)),
+                      ("lse_out", torch.zeros(3, 3)), ("lse_out", bf(3, 4)), ("status", i32(2)), ("workspace", bf(10, 10).t()[::2])):
+        with pytest.raises(ValueError, match=name):
+            call(**{name: bad})
+    for name in ("k_new", "v_new"):
+        with pytest.raises(ValueError, match="come together"):
+            call(**{name: None})
+    for name in ("q", "lengths", "out", "workspace"):
+        with pytest.raises(TypeError):
+            call(**{name: None})
+        with pytest.raises(TypeError):
+            call(**{name: 7})
+    shape = B.Shape(1, 2, 128, 48, [4, 0, 3])
+    ok_f = dict(k_cache=bf(1, 2, 7, 128), v_cache=bf(1, 2, 7, 128), keep_counts=[2, 0, 3], idx=i32(1, 2, 5), head_offsets=i32(1, 3, 3),
+                mass_in=torch.zeros(1, 2, 7), first_position=i32(3), lengths=i32(6), lengths_out=i32(6), status=i32(6))
+    fill = lambda **kw: B.paged_fill(c, shape, **{**ok_f, **kw})
+    with pytest.raises(ValueError, match="current CUDA device"):
+        fill()
+    for name, bad in (("k_cache", bf(1, 2, 8, 128)), ("v_cache", torch.zeros(1, 2, 7, 128)), ("v_cache", bf(1, 2, 128, 7).transpose(2, 3)),
+                      ("keep_counts", [2, 0]), ("idx", i32(9)), ("idx", i32(10).long()), ("head_offsets", i32(8)), ("mass_in", torch.zeros(13)),
+                      ("first_position", i32(2)), ("lengths", i32(5)), ("lengths_out", torch.zeros(6)), ("status", i32(7))):
+        with pytest.raises(ValueError, match=name):
+            fill(**{name: bad})
+    with pytest.raises(TypeError):
+        fill(keep_counts=None)
+    with pytest.raises(TypeError):
+        fill(keep_counts=[2, 0, "3"])
+    ok_e = dict(lengths=i32(6), budgets=i32(6), lengths_out=i32(6), max_length=32, recent=1, next_position=i32(3), status=i32(6))
+    evict = lambda **kw: B.paged_evict(c, **{**ok_e, **kw})
+    with pytest.raises(ValueError, match="current CUDA device"):
+        evict()
+    for name, bad in (("lengths", i32(5)), ("budgets", i32(6).long()), ("lengths_out", i32(7)), ("next_position", i32(6)), ("status", i32(1))):
+        with pytest.raises(ValueError, match=name):
+            evict(**{name: bad})
+    with pytest.raises(OverflowError):
+        evict(max_length=1 << 40)
 
 
 def _small(seed=0, layers=1, heads=1, batch=1, page=8, max_pages=3):
