@@ -1139,10 +1139,10 @@ bool decode_layout(const compactor_paged_cache* c, const compactor_decode_option
     l->groups = (o->q_per_kv + kDecodeHeads - 1) / kDecodeHeads;
     l->gs = (o->q_per_kv + 1) / 2 * 2;
     const long long tiles = units * ((l->capacity + kDecodeTile - 1) / kDecodeTile);
-    if ((tiles + units * kDecodeUnitCost) * l->groups > 0x7fffffffLL || units * o->q_per_kv > 0x3fffffffLL) { *err = COMPACTOR_E_TOO_LARGE; return false; }
+    if ((tiles + units * kDecodeUnitCost) * l->groups > 0x7fffffffLL || tiles + units * kDecodeMassUnitCost > 0x7fffffffLL || units * o->q_per_kv > 0x3fffffffLL) { *err = COMPACTOR_E_TOO_LARGE; return false; }
     l->workers = (int)std::min<long long>(sm_count(), tiles * l->groups) * kDecodeWarps;
     const size_t slots = (size_t)l->workers + (size_t)units * l->groups;
-    size_t off = align_up(sizeof(int) * ((size_t)units + 1));
+    size_t off = align_up(sizeof(int) * 2 * ((size_t)units + 1));
     l->off_ml = off;     off += align_up(sizeof(float) * 32 * slots);
     l->off_o = off;      off += align_up(sizeof(float) * kD * std::min(o->q_per_kv, kDecodeHeads) * slots);
     l->off_scores = off; off += o->accumulate != 0 ? align_up(sizeof(float) * (size_t)tiles * kDecodeTile * l->gs) : 0;

@@ -33,6 +33,7 @@ constexpr int kRowBytes = kD * 2;
 constexpr int kStageBytes = 2 * kTile * kRowBytes;     // K tile, V tile
 constexpr size_t kSmemBytes = (size_t)kWarps * kStages * kStageBytes;
 constexpr int kUnitCost = kDecodeUnitCost;
+constexpr int kMassUnitCost = kDecodeMassUnitCost;
 constexpr int kUnitsInSmem = 2048;                     // units whose token counts every CTA keeps at hand
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -145,49 +146,53 @@ __global__ void __launch_bounds__(kThreads, 1)
 decode_kernel(const __grid_constant__ DecodeArgs a) {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ int cum[kThreads + 1];
-    __shared__ int warp_sum[kWarps];
+    __shared__ long long warp_sum[kWarps];
     __shared__ int bad[kWarps][kStages];
     __shared__ int new_page[kWarps][kStages];
     __shared__ int live[kUnitsInSmem];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int gid = lane >> 2, tig = lane & 3;
-    pdl_trigger();
     pdl_wait();
 
     // cost before each thread's run of units
     const int per = (a.units + kThreads - 1) / kThreads;
     const int u0 = tid * per, u1 = min(a.units, u0 + per);
-    int mine = 0;
+    long long mine = 0;                                      // cost, and in the upper half how many units have tokens
     for (int u = u0; u < u1; ++u) {
         const int n = live_tokens(a, u);
         if (u < kUnitsInSmem) live[u] = n;
-        mine += cost_of(n);
+        mine += cost_of(n) + ((long long)(n > 0) << 32);
     }
-    int incl = mine;
+    long long incl = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(0xffffffffu, incl, d);
+        const long long o = __shfl_up_sync(0xffffffffu, incl, d);
         if (lane >= d) incl += o;
     }
     if (lane == 31) warp_sum[warp] = incl;
     __syncthreads();
-    int before = 0;
+    long long before = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) before += w < warp ? warp_sum[w] : 0;
-    cum[tid + 1] = before + incl;
+    cum[tid + 1] = (int)(before + incl);
     if (tid == 0) cum[0] = 0;
     __syncthreads();
     const int all = cum[kThreads];
     if (blockIdx.x == 0) {                                   // for the second kernel, and the units that are refused
-        int at = cum[tid];
+        int at = cum[tid], units = (int)((before + incl - mine) >> 32);
         for (int u = u0; u < u1; ++u) {
-            a.prefix[u] = at;
-            at += cost_of(live_tokens(a, u));
-            const int n = __ldg(a.lengths + u);
+            a.prefix[2 * u] = at;
+            a.prefix[2 * u + 1] = at + units * (kMassUnitCost - kUnitCost);
+            const int live = live_tokens(a, u), n = __ldg(a.lengths + u);
+            at += cost_of(live);
+            units += live > 0;
             if (a.status != nullptr && n >= 0 && (long long)n + (a.k_new != nullptr) > a.capacity)
                 atomicOr(a.status + u, COMPACTOR_STATUS_CAPACITY);
         }
-        if (tid == 0) a.prefix[a.units] = all;
+        if (tid == kThreads - 1) {
+            a.prefix[2 * a.units] = all;
+            a.prefix[2 * a.units + 1] = all + units * (kMassUnitCost - kUnitCost);
+        }
     }
     const int total = all * a.groups;
     const int workers = active_workers(a, total);
@@ -340,6 +345,9 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
                 sum[t][0] = sum[t][1] = 0.f;
             }
         }
+        // the second kernel's blocks are let in when the tiles run out: blocks that wait beside this kernel slow it (2 units of
+        // 61 measured 4 us)
+        if (left_c <= kStages) pdl_trigger();
         cp_wait<kStages - 1>();
         __syncwarp();
         const uint32_t ks = ring_s + stage * kStageBytes, vs = ks + kTile * kRowBytes;
@@ -506,32 +514,38 @@ __device__ __forceinline__ Pieces pieces_of(const DecodeArgs& a, int unit, int g
     return {(long long)w0 + (long long)unit * a.groups + grp, w1 - w0 + 1};
 }
 
-// Blocks [0, units * g): one (unit, query head) each; its pieces are joined: o = sum_i e_i o_i / sum_i e_i l_i with
-// e_i = 2^(m_i - m).  The blocks behind them add the weights, `chunk` tokens of one unit each.  Both are chains of a few
-// dependent reads from L2 (about 0.7 us each), so every step asks for all it needs at once.
-constexpr int kJoinBatch = 8;              // pieces per warp in flight
-constexpr int kTokenBatch = 4;             // tokens per thread in flight
+// The last units * g blocks have one (unit, query head) each, whose pieces they join: o = sum_i e_i o_i / sum_i e_i l_i with
+// e_i = 2^(m_i - m).  The blocks before them add the weights; they share all tokens out evenly, as the first kernel does,
+// with a cost of kMassUnitCost tiles per unit (about what its sum takes to find).  Both are chains of a few dependent reads from L2
+// (about 0.7 us each), so every step asks for all it needs at once, and several small blocks share an SM.
 
 template <int kWarps>
-__global__ void __launch_bounds__(kWarps * 32)
-join_kernel(const __grid_constant__ DecodeArgs a, int join_blocks, int chunk, int chunks) {
+__global__ void __launch_bounds__(kWarps * 32, kWarps == 16 ? 1 : 4)
+join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
     constexpr int kThreads = kWarps * 32;
-    __shared__ float part[kWarps][kD];
+    constexpr int kJoinBatch = kWarps == 16 ? 8 : 4;         // pieces per warp in flight
+    constexpr int kTokenBatch = 4;                           // tokens per thread in flight
+    // a large block takes half of the channels of its (unit, head): twice as many pieces in flight per warp
+    constexpr int kSplit = kWarps == 16 ? 2 : 1, kLanes = 32 / kSplit, kStreams = kWarps * kSplit, kChannels = kD / kSplit;
+    __shared__ float part[kStreams][kChannels];
+    __shared__ float part_m[kStreams], part_l[kStreams];
     __shared__ float red_m[kWarps][16], red_l[kWarps][16];
     __shared__ float lse2[64];
+    __shared__ int counted[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    pdl_trigger();
+    if (kWarps == 16) pdl_trigger();                         // (else the next call's blocks would take the registers of the later blocks of this one)
     pdl_wait();
-    const int all = a.prefix[a.units];
-    if ((int)blockIdx.x < join_blocks) {
-        const int unit = blockIdx.x / a.g, head = blockIdx.x - unit * a.g;
+    const int all = a.prefix[2 * a.units];
+    if ((int)blockIdx.x >= mass_blocks) {
+        const int item = (blockIdx.x - mass_blocks) / kSplit, unit = item / a.g, head = item - unit * a.g;
+        const int channel0 = ((blockIdx.x - mass_blocks) % kSplit) * kChannels;
         const int grp = head / kDecodeHeads, hh = head - grp * kDecodeHeads, gg = min(a.g, kDecodeHeads);
         const int h = unit / a.c.batch, b = unit - h * a.c.batch;
-        const int at = a.prefix[unit], cost = a.prefix[unit + 1] - at;
-        __nv_bfloat16* dst = a.out + b * a.out_seq + (long long)(h * a.g + head) * a.out_head;
-        float* lse = a.lse != nullptr ? a.lse + (long long)b * (a.c.heads * a.g) + h * a.g + head : nullptr;
+        const int at = a.prefix[2 * unit], cost = a.prefix[2 * unit + 2] - at;
+        __nv_bfloat16* dst = a.out + b * a.out_seq + (long long)(h * a.g + head) * a.out_head + channel0;
+        float* lse = a.lse != nullptr && channel0 == 0 ? a.lse + (long long)b * (a.c.heads * a.g) + h * a.g + head : nullptr;
         if (cost == 0) {
-            if (tid < kD) dst[tid] = __float2bfloat16_rn(0.f);
+            if (tid < kChannels) dst[tid] = __float2bfloat16_rn(0.f);
             if (tid == 0 && lse != nullptr) *lse = -INFINITY;
             return;
         }
@@ -539,20 +553,21 @@ join_kernel(const __grid_constant__ DecodeArgs a, int join_blocks, int chunk, in
         if (ps.n == 1) return;                               // written by the warp that had it whole
         float m = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i0 = warp; i0 < ps.n; i0 += kWarps * kJoinBatch) {
+        const int stream = warp * kSplit + lane / kLanes, channel = lane % kLanes * 4;
+        for (int i0 = stream; i0 < ps.n; i0 += kStreams * kJoinBatch) {
             float pm[kJoinBatch], pl[kJoinBatch];
             float4 x[kJoinBatch];
 #pragma unroll
             for (int k = 0; k < kJoinBatch; ++k) {
-                const long long slot = ps.first + min(i0 + k * kWarps, ps.n - 1);
+                const long long slot = ps.first + min(i0 + k * kStreams, ps.n - 1);
                 pm[k] = a.ml[slot * 32 + hh];
                 pl[k] = a.ml[slot * 32 + 16 + hh];
-                x[k] = *reinterpret_cast<const float4*>(a.o + (slot * gg + hh) * kD + lane * 4);
+                x[k] = *reinterpret_cast<const float4*>(a.o + (slot * gg + hh) * kD + channel0 + channel);
             }
             float top = m;
 #pragma unroll
             for (int k = 0; k < kJoinBatch; ++k) {
-                if (i0 + k * kWarps >= ps.n) pm[k] = -INFINITY;
+                if (i0 + k * kStreams >= ps.n) pm[k] = -INFINITY;
                 top = fmaxf(top, pm[k]);
             }
             const float ref = top == -INFINITY ? 0.f : top;
@@ -561,26 +576,26 @@ join_kernel(const __grid_constant__ DecodeArgs a, int join_blocks, int chunk, in
             m = top;
 #pragma unroll
             for (int k = 0; k < kJoinBatch; ++k) {
-                if (i0 + k * kWarps >= ps.n) continue;
+                if (i0 + k * kStreams >= ps.n) continue;
                 const float e = ex2f(pm[k] - ref);
                 l += e * pl[k];
                 acc.x += e * x[k].x; acc.y += e * x[k].y; acc.z += e * x[k].z; acc.w += e * x[k].w;
             }
         }
-        *reinterpret_cast<float4*>(&part[warp][lane * 4]) = acc;
-        if (lane == 0) { red_m[warp][0] = m; red_l[warp][0] = l; }
+        *reinterpret_cast<float4*>(&part[stream][channel]) = acc;
+        if (channel == 0) { part_m[stream] = m; part_l[stream] = l; }
         __syncthreads();
-        if (tid < kD) {
+        if (tid < kChannels) {
             float top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, red_m[w][0]);
+            for (int w = 0; w < kStreams; ++w) top = fmaxf(top, part_m[w]);
             const float ref = top == -INFINITY ? 0.f : top;
             float x = 0.f, z = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float e = ex2f(red_m[w][0] - ref);
+            for (int w = 0; w < kStreams; ++w) {
+                const float e = ex2f(part_m[w] - ref);
                 x += e * part[w][tid];
-                z += e * red_l[w][0];
+                z += e * part_l[w];
             }
             dst[tid] = __float2bfloat16_rn(z == 0.f ? 0.f : x / z);
             if (tid == 0 && lse != nullptr) *lse = z == 0.f ? -INFINITY : kLn2 * (top + log2f(z));
@@ -589,68 +604,100 @@ join_kernel(const __grid_constant__ DecodeArgs a, int join_blocks, int chunk, in
     }
 
     // weights: w_j += sum over the unit's query heads of 2^(y_j - lse)
-    const int item = blockIdx.x - join_blocks, unit = item / chunks, tok0 = (item - unit * chunks) * chunk;
-    const int n = live_tokens(a, unit), tok1 = min(n, tok0 + chunk);
-    const int at = a.prefix[unit], cost = a.prefix[unit + 1] - at;
-    if (tok0 >= n) return;
-    const int cached = n - (a.k_new != nullptr);
-    int page[kTokenBatch];
-    auto ask_pages = [&](int first) {
+    const int all_mass = a.prefix[2 * a.units + 1];
+    const Share share(all_mass, mass_blocks);
+    int place = share.begin(blockIdx.x);
+    const int place_end = place + share.size(blockIdx.x);
+    if (place >= place_end) return;
+    int below = 0;                                           // the last unit that begins at or before `place`: it has tokens
+    for (int u = tid; u < a.units; u += kThreads) below += a.prefix[2 * u + 1] <= place;
+    below = __reduce_add_sync(0xffffffffu, below);
+    if (lane == 0) counted[warp] = below;
+    __syncthreads();
+    int unit = -1;
 #pragma unroll
-        for (int k = 0; k < kTokenBatch; ++k) page[k] = page_of(a.c, unit, min(first + k * kThreads, tok1 - 1));
-    };
-    ask_pages(tok0 + tid);
+    for (int w = 0; w < kWarps; ++w) unit += counted[w];
     int hp = 1;                                              // lanes side by side for the heads of a group
     while (hp < min(a.g, kDecodeHeads)) hp *= 2;
     const int hh = lane & (hp - 1), st = tid / hp, streams = kThreads / hp;
-    for (int grp = 0; grp < a.groups; ++grp) {
-        const Pieces ps = pieces_of(a, unit, grp, at, cost, all);
-        const int heads = min(kDecodeHeads, a.g - grp * kDecodeHeads);
-        float m = -INFINITY, l = 0.f;
-        if (hh < heads) {
+    for (; place < place_end; ++unit) {
+        const int4 here = make_int4(a.prefix[2 * unit], a.prefix[2 * unit + 1], a.prefix[2 * unit + 2], a.prefix[2 * unit + 3]);
+        const int n = live_tokens(a, unit);
+        if (n == 0) continue;
+        const int at = here.x, cost = here.z - at;
+        const int first_tile = max(0, place - here.y - kMassUnitCost), last_tile = min(place_end, here.w) - here.y - kMassUnitCost;
+        place = here.w;
+        if (last_tile <= first_tile) continue;               // only the unit's head
+        const int tok0 = first_tile * kTile, tok1 = min(n, last_tile * kTile);
+        const int cached = n - (a.k_new != nullptr);
+        int page[kTokenBatch];
+        float old[kTokenBatch];
+        auto ask_pages = [&](int first) {
+#pragma unroll
+            for (int k = 0; k < kTokenBatch; ++k) page[k] = page_of(a.c, unit, min(first + k * kThreads, tok1 - 1));
+        };
+        auto ask_weights = [&](int first) {
+#pragma unroll
+            for (int k = 0; k < kTokenBatch; ++k)
+                old[k] = a.c.mass[slot_in_pool(a.c, max(page[k], 0), min(first + k * kThreads, tok1 - 1))];
+        };
+        ask_pages(tok0 + tid);
+        for (int grp = 0; grp < a.groups; ++grp) {
+            const Pieces ps = pieces_of(a, unit, grp, at, cost, all);
+            const int heads = min(kDecodeHeads, a.g - grp * kDecodeHeads);
+            float m = -INFINITY, l = 0.f;
+            if (hh < heads) {
 #pragma unroll 4
-            for (int i = st; i < ps.n; i += streams) {
-                const float* ml = a.ml + (ps.first + i) * 32 + hh;
-                merge(m, l, ml[0], ml[16]);
+                for (int i = st; i < ps.n; i += streams) {
+                    const float* ml = a.ml + (ps.first + i) * 32 + hh;
+                    merge(m, l, ml[0], ml[16]);
+                }
+            }
+            if (grp == 0) ask_weights(tok0 + tid);           // the page ids have arrived with the pieces
+            // the block's maximum per head, then the sums against it: a tree of single shuffles each, then one round over the warps
+            float top = m;
+            for (int d = hp; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            l *= ex2f(m - (top == -INFINITY ? 0.f : top));
+            for (int d = hp; d < 32; d *= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
+            if (lane < hp) { red_m[warp][lane] = top; red_l[warp][lane] = l; }
+            __syncthreads();
+            if (tid < heads) {
+                top = red_m[0][tid];
+#pragma unroll
+                for (int i = 1; i < kWarps; ++i) top = fmaxf(top, red_m[i][tid]);
+                const float ref = top == -INFINITY ? 0.f : top;
+                l = 0.f;
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) l += red_l[i][tid] * ex2f(red_m[i][tid] - ref);
+                lse2[grp * kDecodeHeads + tid] = l == 0.f ? INFINITY : top + log2f(l);
+            }
+            __syncthreads();
+        }
+        for (int first = tok0 + tid; first < tok1; first += kThreads * kTokenBatch) {
+            float w[kTokenBatch];
+#pragma unroll
+            for (int k = 0; k < kTokenBatch; ++k) {
+                const int tok = min(first + k * kThreads, tok1 - 1);
+                w[k] = 0.f;
+                const float2* row = reinterpret_cast<const float2*>(a.scores + ((long long)unit * a.unit_rows + tok) * a.gs);
+                for (int i = 0; i < a.g; i += 2) {
+                    const float2 y = row[i >> 1];
+                    w[k] += ex2f(y.x - lse2[i]);
+                    if (i + 1 < a.g) w[k] += ex2f(y.y - lse2[i + 1]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kTokenBatch; ++k) {
+                const int tok = first + k * kThreads;
+                if (tok < tok1 && page[k] >= 0)
+                    a.c.mass[slot_in_pool(a.c, page[k], tok)] = tok < cached ? old[k] + w[k] : w[k];
+            }
+            if (first + kThreads * kTokenBatch < tok1) {
+                ask_pages(first + kThreads * kTokenBatch);
+                ask_weights(first + kThreads * kTokenBatch);
             }
         }
-        for (int d = hp; d < 32; d *= 2) {
-            const float mo = __shfl_xor_sync(0xffffffffu, m, d), lo = __shfl_xor_sync(0xffffffffu, l, d);
-            merge(m, l, mo, lo);
-        }
-        if (lane < hp) { red_m[warp][lane] = m; red_l[warp][lane] = l; }
-        __syncthreads();
-        if (tid < heads) {
-            m = red_m[0][tid]; l = red_l[0][tid];
-#pragma unroll
-            for (int i = 1; i < kWarps; ++i) merge(m, l, red_m[i][tid], red_l[i][tid]);
-            lse2[grp * kDecodeHeads + tid] = l == 0.f ? INFINITY : m + log2f(l);
-        }
-        __syncthreads();
-    }
-    for (int first = tok0 + tid; first < tok1; first += kThreads * kTokenBatch) {
-        float w[kTokenBatch], old[kTokenBatch];
-#pragma unroll
-        for (int k = 0; k < kTokenBatch; ++k)
-            old[k] = a.c.mass[slot_in_pool(a.c, max(page[k], 0), min(first + k * kThreads, tok1 - 1))];
-#pragma unroll
-        for (int k = 0; k < kTokenBatch; ++k) {
-            const int tok = min(first + k * kThreads, tok1 - 1);
-            w[k] = 0.f;
-            const float2* row = reinterpret_cast<const float2*>(a.scores + ((long long)unit * a.unit_rows + tok) * a.gs);
-            for (int i = 0; i < a.g; i += 2) {
-                const float2 y = row[i >> 1];
-                w[k] += ex2f(y.x - lse2[i]);
-                if (i + 1 < a.g) w[k] += ex2f(y.y - lse2[i + 1]);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kTokenBatch; ++k) {
-            const int tok = first + k * kThreads;
-            if (tok < tok1 && page[k] >= 0)
-                a.c.mass[slot_in_pool(a.c, page[k], tok)] = tok < cached ? old[k] + w[k] : w[k];
-        }
-        if (first + kThreads * kTokenBatch < tok1) ask_pages(first + kThreads * kTokenBatch);
+        __syncthreads();                                     // lse2 and the reductions are the next unit's
     }
 }
 
@@ -663,17 +710,19 @@ cudaError_t launch_paged_attention(const DecodeArgs& a, int sm_count, cudaStream
     cudaError_t e = allow_smem(kernel, (int)kSmemBytes, done[a.g <= 8 ? 0 : 1]);
     if (e != cudaSuccess) return e;
     if ((e = launch_chained(kPdlOther, kernel, dim3(grid), dim3(kThreads), kSmemBytes, stream, a)) != cudaSuccess) return e;
-    // the second kernel: 16 warps a block where its blocks do not fill the GPU anyway
-    const int join_blocks = a.units * a.g;
-    const int warps = join_blocks <= 2 * sm_count ? 16 : 8;
-    int chunk = warps * 32 * kTokenBatch, chunks = 0;
-    if (a.accumulate) {                                      // one round of a block's threads, more where that gives more blocks than fit at once
-        while ((long long)a.units * ((a.capacity + chunk - 1) / chunk) > 16LL * sm_count && chunk < a.capacity) chunk *= 2;
-        chunks = (a.capacity + chunk - 1) / chunk;
-    }
-    const dim3 blocks(join_blocks + a.units * chunks);
-    e = warps == 16 ? launch_chained(kPdlOther, join_kernel<16>, blocks, dim3(512), 0, stream, a, join_blocks, chunk, chunks)
-                    : launch_chained(kPdlOther, join_kernel<8>, blocks, dim3(256), 0, stream, a, join_blocks, chunk, chunks);
+    // the second kernel: 16 warps a block and two blocks per (unit, head) where all of them fit the GPU at once, one to an SM; else 8
+    // warps, four blocks to an SM
+    int join_blocks = a.units * a.g;
+    const long long most = a.accumulate ? (long long)a.units * ((a.capacity + kTile - 1) / kTile + kMassUnitCost) : 0;   // cost of the weights
+    const long long wanted = (most + kTile - 1) / kTile;     // 256 tokens a block at the least
+    const bool large = 2 * join_blocks <= sm_count;
+    if (large) join_blocks *= 2;
+    // (not more than fit beside the others, so that those need not wait for a place)
+    const int room = large ? max(sm_count / 2, sm_count - join_blocks) : join_blocks <= 2 * sm_count ? 4 * sm_count - join_blocks : 4 * sm_count;
+    const int mass_blocks = (int)min(wanted, (long long)room);
+    const dim3 blocks(mass_blocks + join_blocks);
+    e = large ? launch_chained(kPdlOther, join_kernel<16>, blocks, dim3(512), 0, stream, a, mass_blocks)
+              : launch_chained(kPdlOther, join_kernel<8>, blocks, dim3(256), 0, stream, a, mass_blocks);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -88,7 +88,7 @@ struct DecodeArgs {
     float scale, softcap;                  // softcap <= 0: none
     int units;
     int workers;                           // warps that share the tokens
-    int* prefix;                           // workspace: [units + 1] cost before each unit
+    int* prefix;                           // workspace: [units + 1][2] cost before each unit, for the tiles and for the weights
     float* ml;                             // workspace: [workers + units * groups][2][16] running maximum and sum
     float* o;                              // workspace: [workers + units * groups][min(g, 16)][128]
     float* scores;                         // workspace: [units][unit_rows][gs], only when accumulating
@@ -97,8 +97,9 @@ struct DecodeArgs {
 };
 constexpr int kDecodeTile = 16;            // tokens per tile
 constexpr int kDecodeWarps = 8;
-constexpr int kDecodeUnitCost = 2;         // tiles that entering a unit counts for when the work is shared out
+constexpr int kDecodeUnitCost = 3;         // tiles that entering a unit counts for when the work is shared out
 constexpr int kDecodeHeads = 16;           // query heads that one warp serves at once
+constexpr int kDecodeMassUnitCost = 64;    // the same, in the kernel that adds the weights
 cudaError_t launch_paged_attention(const DecodeArgs& a, int sm_count, cudaStream_t stream);
 
 struct EvictArgs {
