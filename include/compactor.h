@@ -480,7 +480,7 @@ int compactor_paged_attention(const compactor_paged_cache* cache, int32_t layer,
  * of equal weights the lower slots stay.  Not-a-number ranks above +inf.  (If more tokens than B are that recent, which takes repeated
  * positions, the lower slots of them stay.)  The others leave, and the holes they leave in slots [0, B) are filled from
  * behind: the j-th evicted slot below B receives row, weight and position of the j-th kept slot at or above B.  Slots
- * from B on keep what they hold.  lengths_out[u] (may be `lengths`; the entries of other layers are left alone) becomes B.
+ * from B on keep what they hold.  lengths_out[u] (may be `lengths`, not `budgets`; the entries of other layers are left alone) becomes B.
  * A unit with n <= B, a negative length or a negative budget stays as it is, lengths_out[u] = lengths[u]; so does one with
  * n > max_length or beyond its pages (COMPACTOR_STATUS_CAPACITY) and one with a page that is none (COMPACTOR_STATUS_PAGE).
  *   next_position  device int32 [batch]; may be NULL when recent = 0.

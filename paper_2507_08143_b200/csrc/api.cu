@@ -1159,7 +1159,8 @@ extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t 
                                     int32_t* status, void* stream) {
     int err = 0;
     if (!cache_ok(cache, &err) || !shape_ok(shape, &err)) return err;
-    if (!mat_ok(k_cache) || !mat_ok(v_cache) || keep_counts == nullptr || (head_offsets != nullptr && idx == nullptr) ||
+    const bool some = shape->cu_seqlens[shape->batch] > 0;               // without tokens there is nothing to point to
+    if ((some && (!mat_ok(k_cache) || !mat_ok(v_cache))) || keep_counts == nullptr || (head_offsets != nullptr && idx == nullptr) ||
         shape->heads != cache->heads || shape->batch != cache->batch || first_layer < 0 ||
         first_layer > cache->layers - shape->layers)
         return COMPACTOR_E_INVALID_ARGUMENT;

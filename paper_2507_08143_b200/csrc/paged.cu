@@ -17,7 +17,7 @@ namespace {
 constexpr int kFillThreads = 256;
 constexpr int kFillRows = 128;
 constexpr int kFillRowsPerIter = kFillThreads / 16;
-constexpr int kFillBatch = 2;                   // rows per thread in flight
+constexpr int kFillBatch = 4;                   // rows per thread in flight (2: 116 us instead of 113 for 32 x 8 heads x 2458 rows)
 
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
     uint4 v;
@@ -516,7 +516,7 @@ int evict_max_tokens() { return 8 * kLargeSlice; }
 cudaError_t launch_paged_evict(const EvictArgs& a, int sm_count, cudaStream_t stream) {
     // Many units: CTAs of 256 threads, four to an SM; where some units may need several CTAs, those go in a launch of clusters, the others
     // in one of single CTAs beside it (one launch of clusters for all left most of their CTAs without work: 128 of 512 ragged
-    // units of up to 32768 tokens 57 us against WHAT).  Few units or very long ones: CTAs of 512 threads, more of them per unit while
+    // units of up to 32768 tokens 57 us against 45).  Few units or very long ones: CTAs of 512 threads, more of them per unit while
     // the GPU is not full and a slice still has 2048 slots.
     const int n = a.max_length;
     cudaError_t e;

@@ -402,6 +402,17 @@ def test_fill_skips_bad_rows_and_refuses_units_without_room():
     assert st[0, 0, 1] == 8                                              # fits the table, but only its first page is one
 
 
+def test_fill_without_any_tokens():
+    from paper_2507_08143_b200 import binding as B
+    _, cache, len_d = make_cache([[[4, -1]]], 8, 2, 8)
+    before = pools_of(cache)
+    empty = torch.empty(1, 1, 0, 128, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(len_d, 9)
+    B.paged_fill(cache, B.Shape(1, 1, 128, 48, [0, 0]), empty, empty, [0, 0], lengths=len_d, lengths_out=out)
+    assert out.cpu().tolist() == [[[4, -1]]]
+    same_bits(pools_of(cache), before, "nothing")
+
+
 def test_fill_of_more_sequences_than_one_launch_takes():
     rng = np.random.default_rng(9)
     n = rng.integers(0, 20, 600).tolist()
