@@ -28,7 +28,7 @@ namespace {
 constexpr int kTile = kDecodeTile;
 constexpr int kWarps = kDecodeWarps;
 constexpr int kThreads = kWarps * 32;
-constexpr int kStages = 3;
+constexpr int kStages = 2;
 constexpr int kRowBytes = kD * 2;
 constexpr int kStageBytes = 2 * kTile * kRowBytes;     // K tile, V tile
 constexpr size_t kSmemBytes = (size_t)kWarps * kStages * kStageBytes;
@@ -46,6 +46,9 @@ __device__ __forceinline__ float ex2f(float x) {
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
     asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -97,7 +100,12 @@ struct Share {
         return at < longer ? at / (q + 1) : r + (at - longer) / q;
     }
 };
-__device__ __forceinline__ int active_workers(const DecodeArgs& a, int total) { return min(a.workers, total); }
+// Warps that share the work.  Where each gets many tiles one warp of a CTA stays out: with seven warps of two stages 112 KB are on
+// their way to an SM, enough for its share of HBM; more of them disturb each other (131072 tokens: 90.0 us with seven warps, 93.4 with
+// eight, 96 with eight of three stages, 90.7 with six).  With few tiles all eight are wanted (padded batch: 34.9 against 36.7 us).
+__device__ __forceinline__ int active_workers(const DecodeArgs& a, int total) {
+    return total / 16 >= a.workers ? a.workers / kWarps * (kWarps - 1) : min(a.workers, total);
+}
 
 // A place in the order of all tiles: unit by unit, within a unit group by group.
 struct Cursor {
@@ -144,7 +152,7 @@ __device__ __forceinline__ void load_queries(const DecodeArgs& a, const Cursor& 
 template <int NG>
 __global__ void __launch_bounds__(kThreads, 1)
 decode_kernel(const __grid_constant__ DecodeArgs a) {
-    extern __shared__ __align__(128) unsigned char ring[];
+    extern __shared__ __align__(1024) unsigned char ring[];
     __shared__ int cum[kThreads + 1];
     __shared__ long long warp_sum[kWarps];
     __shared__ int bad[kWarps][kStages];
@@ -243,6 +251,21 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
     bool q_waiting = true;
     load_queries<NG>(a, pc, qn, lane);
     if (nc.next_unit(a, live)) ids_next_unit = page_ids(a, nc, 0, lane);
+    // Eight rows to `dst` (and the same of V a tile further) from `src`, this lane's piece of the run's first or second row on.  Row r's pieces stand in
+    // the stage with their number xor r & 7, so that the eight rows of a matrix fragment meet different banks.
+    const long long two_rows = 2 * a.c.stride_token * (long long)sizeof(__nv_bfloat16);
+    const long long v_from_k = reinterpret_cast<const char*>(a.c.v) - reinterpret_cast<const char*>(a.c.k);
+    uint32_t place[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) place[i] = (2 * i + row_hi) * kRowBytes + ((piece ^ (2 * i + row_hi)) << 4);
+    auto copy_rows = [&](uint32_t dst, const char* src) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            cp_async16(dst + place[i], src);
+            cp_async16(dst + place[i] + kTile * kRowBytes, src + v_from_k);
+            src += two_rows;
+        }
+    };
     int in_stage = 0;
     auto issue = [&]() {
         if (left_p > 0) {
@@ -266,24 +289,27 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
             int p0 = __shfl_sync(0xffffffffu, ids, e - e0), p1 = __shfl_sync(0xffffffffu, ids, ((base + 8) >> a.c.page_shift) - e0);
             if ((unsigned)p0 >= (unsigned)a.c.n_pages) p0 = -1;
             if ((unsigned)p1 >= (unsigned)a.c.n_pages || base + 8 >= n) p1 = -1;
-            const uint32_t ks = ring_s + stage * kStageBytes, vs = ks + kTile * kRowBytes;
-            const __nv_bfloat16* kn = a.c.k;
-            const __nv_bfloat16* vn = a.c.v;
+            const uint32_t ks = ring_s + stage * kStageBytes;
             const int fresh_row = cached < n ? cached - base : -1;           // the new token's row of this tile, if it has it
-            if (fresh_row >= 0 && fresh_row < kTile) {
+            if (base + kTile <= cached && p0 >= 0 && p1 >= 0) {              // all rows come from pages: two runs of eight
+                const char* src = reinterpret_cast<const char*>(a.c.k + row_in_pool(a.c, p0, base + row_hi)) + piece * 16;
+                copy_rows(ks, src);
+                src = reinterpret_cast<const char*>(a.c.k + row_in_pool(a.c, p1, base + 8 + row_hi)) + piece * 16;
+                copy_rows(ks + 8 * kRowBytes, src);
+            } else {
                 const int h = unit / a.c.batch, b = unit - h * a.c.batch;
-                kn = a.k_new + b * a.kn_seq + h * a.kn_head + piece * 8;
-                vn = a.v_new + b * a.vn_seq + h * a.vn_head + piece * 8;
-            }
-#pragma unroll
-            for (int i = 0; i < kTile / 2; ++i) {
-                const int row = 2 * i + row_hi, tok = base + row;
-                const int page = i < kTile / 4 ? p0 : p1;
-                const bool is_new = row == fresh_row, on = is_new || (tok < cached && page >= 0);
-                const long long off = on && !is_new ? row_in_pool(a.c, page, tok) + piece * 8 : 0;
-                const uint32_t dst = row * kRowBytes + ((piece ^ (row & 7)) << 4);
-                cp_async16(ks + dst, is_new ? kn : a.c.k + off, on ? 16 : 0);
-                cp_async16(vs + dst, is_new ? vn : a.c.v + off, on ? 16 : 0);
+#pragma unroll 1
+                for (int i = 0; i < kTile / 2; ++i) {
+                    const int row = 2 * i + row_hi, tok = base + row;
+                    const int page = i < kTile / 4 ? p0 : p1;
+                    const bool is_new = row == fresh_row, on = is_new || (tok < cached && page >= 0);
+                    const long long off = on && !is_new ? row_in_pool(a.c, page, tok) + piece * 8 : 0;
+                    const __nv_bfloat16* kr = is_new ? a.k_new + b * a.kn_seq + h * a.kn_head + piece * 8 : a.c.k + off;
+                    const __nv_bfloat16* vr = is_new ? a.v_new + b * a.vn_seq + h * a.vn_head + piece * 8 : a.c.v + off;
+                    const uint32_t dst = ks + row * kRowBytes + ((piece ^ (row & 7)) << 4);
+                    cp_async16(dst, kr, on ? 16 : 0);
+                    cp_async16(dst + kTile * kRowBytes, vr, on ? 16 : 0);
+                }
             }
             if (lane == 0) {
                 const int bits = (p0 < 0 && base < cached ? 1 : 0) | (p1 < 0 && base + 8 < cached ? 2 : 0);
@@ -313,6 +339,9 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
     for (int s = 0; s < kStages; ++s) issue();
 
     // ---- consumer
+    // fragment s of a row: pieces 2 s and 2 s + 1, i.e. (piece ^ r & 7) << 4 = place of piece 0 or 1, xor s << 5 (a stage starts at a multiple of 256)
+    const uint32_t k_frag = ((lane & 7) + ((lane >> 3) & 1) * 8) * kRowBytes + (((lane >> 4) ^ (lane & 7)) << 4);
+    const uint32_t v_frag = ((lane & 7) + (lane >> 4) * 8) * kRowBytes + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
     Cursor cc = start;
     const float scale2 = a.scale * kLog2e;
     const float cap_in = a.softcap > 0.f ? a.scale / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
@@ -358,11 +387,10 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
 #pragma unroll
         for (int t = 0; t < NG; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
         {
-            const int row = (lane & 7) + ((lane >> 3) & 1) * 8, half = lane >> 4;
 #pragma unroll
             for (int st = 0; st < 8; ++st) {
                 uint32_t kf[4];
-                ldsm4(kf, ks + row * kRowBytes + (((2 * st + half) ^ (row & 7)) << 4));
+                ldsm4(kf, (ks + k_frag) ^ (st << 5));
 #pragma unroll
                 for (int t = 0; t < NG; ++t) mma(s[t], kf, qf[t][st][0], qf[t][st][1]);
             }
@@ -422,11 +450,10 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
         }
         // O^T += V^T P^T: 128 channels x 8 NG heads
         {
-            const int row = (lane & 7) + (lane >> 4) * 8, half = (lane >> 3) & 1;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 uint32_t vf[4];
-                ldsm4t(vf, vs + row * kRowBytes + (((2 * j + half) ^ (row & 7)) << 4));
+                ldsm4t(vf, (vs + v_frag) ^ (j << 5));
 #pragma unroll
                 for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pf[t][0], pf[t][1]);
             }
