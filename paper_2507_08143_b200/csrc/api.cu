@@ -1123,7 +1123,7 @@ bool rows_ok(const compactor_rows& r) {
 }
 
 struct DecodeLayout {
-    int workers, groups, gs, capacity;
+    int workers, groups, capacity;
     size_t off_ml, off_o, off_scores, total;
 };
 // Workspace of the attention: tile prefix, partial (max, sum) pairs, partial outputs, scores.
@@ -1137,7 +1137,6 @@ bool decode_layout(const compactor_paged_cache* c, const compactor_decode_option
     const long long units = (long long)c->heads * c->batch;
     l->capacity = (int)std::min<long long>(o->max_length, (long long)c->max_pages * c->page_tokens);
     l->groups = (o->q_per_kv + kDecodeHeads - 1) / kDecodeHeads;
-    l->gs = (o->q_per_kv + 1) / 2 * 2;
     const long long tiles = units * ((l->capacity + kDecodeTile - 1) / kDecodeTile);
     if ((tiles + units * kDecodeUnitCost) * l->groups > 0x7fffffffLL || tiles + units * kDecodeMassUnitCost > 0x7fffffffLL || units * o->q_per_kv > 0x3fffffffLL) { *err = COMPACTOR_E_TOO_LARGE; return false; }
     l->workers = (int)std::min<long long>(sm_count(), tiles * l->groups) * kDecodeWarps;
@@ -1145,7 +1144,7 @@ bool decode_layout(const compactor_paged_cache* c, const compactor_decode_option
     size_t off = align_up(sizeof(int) * 2 * ((size_t)units + 1));
     l->off_ml = off;     off += align_up(sizeof(float) * 32 * slots);
     l->off_o = off;      off += align_up(sizeof(float) * kD * std::min(o->q_per_kv, kDecodeHeads) * slots);
-    l->off_scores = off; off += o->accumulate != 0 ? align_up(sizeof(float) * (size_t)tiles * kDecodeTile * l->gs) : 0;
+    l->off_scores = off; off += o->accumulate != 0 ? align_up(sizeof(float) * (size_t)tiles * kDecodeTile * o->q_per_kv) : 0;
     l->total = off;
     return true;
 }
@@ -1228,7 +1227,7 @@ extern "C" int compactor_paged_attention(const compactor_paged_cache* cache, int
     a.new_positions = new_positions;
     a.out = static_cast<__nv_bfloat16*>(out.ptr); a.out_seq = out.stride_seq; a.out_head = out.stride_head;
     a.lse = lse_out;
-    a.g = options->q_per_kv; a.groups = l.groups; a.gs = l.gs; a.capacity = l.capacity; a.workers = l.workers;
+    a.g = options->q_per_kv; a.groups = l.groups; a.capacity = l.capacity; a.workers = l.workers;
     a.accumulate = options->accumulate != 0; a.scale = options->scale; a.softcap = options->softcap;
     a.prefix = reinterpret_cast<int*>(ws);
     a.ml = reinterpret_cast<float*>(ws + l.off_ml);

@@ -431,13 +431,16 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
             }
         }
         if (a.accumulate) {                                  // kept until the sum over the whole unit is known
-            float* row = a.scores + ((long long)cc.unit * a.unit_rows + base + gid) * a.gs + cc.grp * kDecodeHeads + 2 * tig;
+            float* col = a.scores + ((long long)cc.unit * a.g + cc.grp * kDecodeHeads + 2 * tig) * a.unit_rows + base + gid;
 #pragma unroll
             for (int t = 0; t < NG; ++t)
-                if (t * 8 + 2 * tig < heads) {
-                    *reinterpret_cast<float2*>(row + t * 8) = make_float2(s[t][0], s[t][1]);
-                    *reinterpret_cast<float2*>(row + t * 8 + 8 * (long long)a.gs) = make_float2(s[t][2], s[t][3]);
-                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (t * 8 + 2 * tig + c < heads) {       // 32 bytes of a head's scores per group of eight lanes
+                        float* at = col + (long long)(t * 8 + c) * a.unit_rows;
+                        at[0] = s[t][c];
+                        at[8] = s[t][c + 2];
+                    }
         }
         if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
@@ -551,7 +554,6 @@ __global__ void __launch_bounds__(kWarps * 32, kWarps == 16 ? 1 : 4)
 join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
     constexpr int kThreads = kWarps * 32;
     constexpr int kJoinBatch = kWarps == 16 ? 8 : 4;         // pieces per warp in flight
-    constexpr int kTokenBatch = 4;                           // tokens per thread in flight
     // a large block takes half of the channels of its (unit, head): twice as many pieces in flight per warp
     constexpr int kSplit = kWarps == 16 ? 2 : 1, kLanes = 32 / kSplit, kStreams = kWarps * kSplit, kChannels = kD / kSplit;
     __shared__ float part[kStreams][kChannels];
@@ -657,18 +659,14 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
         if (last_tile <= first_tile) continue;               // only the unit's head
         const int tok0 = first_tile * kTile, tok1 = min(n, last_tile * kTile);
         const int cached = n - (a.k_new != nullptr);
-        int page[kTokenBatch];
-        float old[kTokenBatch];
-        auto ask_pages = [&](int first) {
-#pragma unroll
-            for (int k = 0; k < kTokenBatch; ++k) page[k] = page_of(a.c, unit, min(first + k * kThreads, tok1 - 1));
-        };
+        // four tokens a thread: they share a page and a 16-byte piece of its weights
+        int page;
+        float4 old;
+        auto ask_page = [&](int first) { page = page_of(a.c, unit, min(first, (tok1 - 1) & ~3)); };
         auto ask_weights = [&](int first) {
-#pragma unroll
-            for (int k = 0; k < kTokenBatch; ++k)
-                old[k] = a.c.mass[slot_in_pool(a.c, max(page[k], 0), min(first + k * kThreads, tok1 - 1))];
+            old = *reinterpret_cast<const float4*>(a.c.mass + slot_in_pool(a.c, max(page, 0), min(first, (tok1 - 1) & ~3)));
         };
-        ask_pages(tok0 + tid);
+        ask_page(tok0 + 4 * tid);
         for (int grp = 0; grp < a.groups; ++grp) {
             const Pieces ps = pieces_of(a, unit, grp, at, cost, all);
             const int heads = min(kDecodeHeads, a.g - grp * kDecodeHeads);
@@ -680,7 +678,7 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
                     merge(m, l, ml[0], ml[16]);
                 }
             }
-            if (grp == 0) ask_weights(tok0 + tid);           // the page ids have arrived with the pieces
+            if (grp == 0) ask_weights(tok0 + 4 * tid);       // the page ids have arrived with the pieces
             // the block's maximum per head, then the sums against it: a tree of single shuffles each, then one round over the warps
             float top = m;
             for (int d = hp; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -700,28 +698,29 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
             }
             __syncthreads();
         }
-        for (int first = tok0 + tid; first < tok1; first += kThreads * kTokenBatch) {
-            float w[kTokenBatch];
+        for (int first = tok0 + 4 * tid; first < tok1; first += 4 * kThreads) {
+            float w[4] = {};
+            const float* col = a.scores + (long long)unit * a.g * a.unit_rows + first;
+#pragma unroll 4
+            for (int i = 0; i < a.g; ++i, col += a.unit_rows) {
+                const float4 y = *reinterpret_cast<const float4*>(col);
+                const float z = lse2[i];
+                w[0] += ex2f(y.x - z); w[1] += ex2f(y.y - z); w[2] += ex2f(y.z - z); w[3] += ex2f(y.w - z);
+            }
+            if (page >= 0) {
+                float* at_mass = a.c.mass + slot_in_pool(a.c, page, first);
+                if (first + 4 <= min(tok1, cached)) {
+                    *reinterpret_cast<float4*>(at_mass) = make_float4(old.x + w[0], old.y + w[1], old.z + w[2], old.w + w[3]);
+                } else {
+                    const float o[4] = {old.x, old.y, old.z, old.w};
 #pragma unroll
-            for (int k = 0; k < kTokenBatch; ++k) {
-                const int tok = min(first + k * kThreads, tok1 - 1);
-                w[k] = 0.f;
-                const float2* row = reinterpret_cast<const float2*>(a.scores + ((long long)unit * a.unit_rows + tok) * a.gs);
-                for (int i = 0; i < a.g; i += 2) {
-                    const float2 y = row[i >> 1];
-                    w[k] += ex2f(y.x - lse2[i]);
-                    if (i + 1 < a.g) w[k] += ex2f(y.y - lse2[i + 1]);
+                    for (int k = 0; k < 4; ++k)
+                        if (first + k < tok1) at_mass[k] = first + k < cached ? o[k] + w[k] : w[k];
                 }
             }
-#pragma unroll
-            for (int k = 0; k < kTokenBatch; ++k) {
-                const int tok = first + k * kThreads;
-                if (tok < tok1 && page[k] >= 0)
-                    a.c.mass[slot_in_pool(a.c, page[k], tok)] = tok < cached ? old[k] + w[k] : w[k];
-            }
-            if (first + kThreads * kTokenBatch < tok1) {
-                ask_pages(first + kThreads * kTokenBatch);
-                ask_weights(first + kThreads * kTokenBatch);
+            if (first + 4 * kThreads < tok1) {
+                ask_page(first + 4 * kThreads);
+                ask_weights(first + 4 * kThreads);
             }
         }
         __syncthreads();                                     // lse2 and the reductions are the next unit's

@@ -91,9 +91,8 @@ struct DecodeArgs {
     int* prefix;                           // workspace: [units + 1][2] cost before each unit, for the tiles and for the weights
     float* ml;                             // workspace: [workers + units * groups][2][16] running maximum and sum
     float* o;                              // workspace: [workers + units * groups][min(g, 16)][128]
-    float* scores;                         // workspace: [units][unit_rows][gs], only when accumulating
-    int gs;                                // g rounded up to an even number
-    int unit_rows;                         // score rows of a unit
+    float* scores;                         // workspace: [units][g][unit_rows] in base 2, only when accumulating
+    int unit_rows;                         // the capacity in whole tiles
 };
 constexpr int kDecodeTile = 16;            // tokens per tile
 constexpr int kDecodeWarps = 8;
