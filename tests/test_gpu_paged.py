@@ -644,3 +644,128 @@ def test_attention_captured_behind_copies_and_memsets():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and st.unique().tolist() == [5 if status is None else 0]
+
+
+@pytest.mark.parametrize("page,heads,lens", [(8, 4, [90001, 120007]), (16, 2, [400003]), (1024, 4, [70000, 131071, 1])])
+def test_attention_of_long_contexts_against_torch_in_64_bits(page, heads, lens):
+    # every warp walks over many page ids and, where it changes units, over their ends; reference unit by unit on the GPU
+    from paper_2507_08143_b200 import binding as B
+    batch, g = len(lens), 3
+    gen = torch.Generator(device="cuda").manual_seed(page)
+    pages = [(n + 1 + page - 1) // page for n in lens]
+    n_pages = heads * sum(pages)
+    ids = torch.randperm(n_pages, device="cuda", generator=gen).int()
+    table = torch.full((1, heads, batch, max(pages)), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for h in range(heads):
+        for b in range(batch):
+            table[0, h, b, :pages[b]] = ids[at:at + pages[b]]
+            at += pages[b]
+    k = torch.randn(n_pages, page, 128, device="cuda", generator=gen, dtype=torch.bfloat16)
+    v = torch.randn(n_pages, page, 128, device="cuda", generator=gen, dtype=torch.bfloat16)
+    mass = torch.rand(n_pages, page, device="cuda", generator=gen)
+    mass0 = mass.double()
+    cache = B.PagedCache(k, v, table, mass=mass)
+    q = torch.randn(batch, heads * g, 128, device="cuda", generator=gen).bfloat16()
+    kn, vn = torch.randn(batch, heads, 128, device="cuda", generator=gen).bfloat16(), torch.randn(batch, heads, 128, device="cuda", generator=gen).bfloat16()
+    lengths = torch.tensor(lens, dtype=torch.int32, device="cuda").expand(1, heads, batch).contiguous()
+    opt = B.decode_options(g, max(lens) + 1, accumulate=True)
+    out, lse = torch.empty_like(q), torch.empty(batch, heads * g, device="cuda")
+    B.paged_attention(cache, 0, opt, q, lengths, out, B.alloc_paged_attention_workspace(cache, opt), k_new=kn, v_new=vn, lse_out=lse)
+    for h in range(heads):
+        for b, n in enumerate(lens):
+            used = table[0, h, b, :pages[b]].long()
+            kk, vv = k[used].reshape(-1, 128)[:n + 1].double(), v[used].reshape(-1, 128)[:n + 1].double()
+            assert torch.equal(kk[n], kn[b, h].double()) and torch.equal(vv[n], vn[b, h].double())       # appended
+            qq = q[b, h * g:(h + 1) * g].double()
+            y = qq @ kk.T * 128 ** -0.5
+            p = torch.softmax(y, 1)
+            ref = p @ vv
+            mag = float((qq.abs() @ kk.abs().T).max()) * 128 ** -0.5
+            dy, rel, tol = attention_bounds(g, None, (p @ vv.abs()).cpu().numpy(), ref.cpu().numpy(), mag, 128 ** -0.5, 0.0, n + 1)
+            assert np.all(np.abs((out[b, h * g:(h + 1) * g].double() - ref).cpu().numpy()) <= tol)
+            ref_lse = torch.logsumexp(y, 1)
+            assert torch.all((lse[b, h * g:(h + 1) * g].double() - ref_lse).abs() <= dy + rel + 2.0 ** -22 * ref_lse.abs())
+            got, want = mass[used].reshape(-1)[:n + 1].double(), mass0[used].reshape(-1)[:n + 1].clone()
+            want[n] = 0
+            want += p.sum(0)
+            # an element of the sum: its own bound, and the rounding of the addition to what was there
+            assert torch.all((got - want).abs() <= (1.01 * rel + (g + 2) * 2.0 ** -24) * p.sum(0) + 2.0 ** -24 * want)
+
+
+def test_attention_of_more_units_than_a_block_keeps_at_hand():
+    rng = np.random.default_rng(15)
+    lengths = rng.integers(-1, 40, size=(1, 8, 300)).astype(np.int32)    # 2400 units
+    lengths[0, 7, 299] = 700
+    run_attention(lengths, 1, 8, accumulate=True, seed=15)
+
+
+@pytest.mark.parametrize("b", [393000, 1000])
+def test_evict_of_the_longest_unit(b):
+    w = np.random.default_rng(b).exponential(size=393216).astype(np.float32)
+    run_evict([[[393216]]], [[[b]]], page=1024, recent=500, weights=lambda u, t: w[t], seed=2)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_batches(seed):
+    # shapes, page sizes, masks and options drawn together
+    rng = np.random.default_rng(1000 + seed)
+    layers, heads, batch = int(rng.integers(1, 3)), int(rng.integers(1, 6)), int(rng.integers(1, 9))
+    page = int(2 ** rng.integers(3, 8))
+    top = int(2 ** rng.uniform(0, 11))
+    lengths = rng.integers(-1, top + 1, size=(layers, heads, batch)).astype(np.int32)
+    run_attention(lengths, int(rng.integers(1, 25)), page, accumulate=bool(rng.integers(2)), softcap=float(rng.choice([0.0, 0.0, 20.0])),
+                  append=bool(rng.integers(2)), strided=bool(rng.integers(2)), layer=int(rng.integers(layers)), seed=seed)
+    budgets = (lengths * rng.random(lengths.shape) * 1.2).astype(np.int32) - int(rng.integers(0, 2))
+    ties = bool(rng.integers(2))
+    w = rng.exponential(size=(top + 1,)).astype(np.float32)
+    run_evict(lengths, budgets, page=page, recent=int(rng.integers(0, 40)), seed=seed, strided=bool(rng.integers(2)),
+              weights=(lambda u, t: float(np.floor(4 * w[t]))) if ties else None, alias=bool(rng.integers(2)))
+    seqlens = rng.integers(0, top + 1, size=batch).tolist()
+    keep = [int(rng.integers(0, n + 1)) for n in seqlens]
+    across = bool(rng.integers(2))
+    held = None if across else rng.integers(-1, 30, size=(layers, heads, batch))
+    run_fill(seqlens, keep, page, layers=layers, cache_layers=layers, heads=heads, across=across, held=held, use_idx=across or bool(rng.integers(2)),
+             mass=bool(rng.integers(2)), strided=bool(rng.integers(2)), alias=bool(rng.integers(2)), seed=seed)
+
+
+def test_the_steps_of_a_decoding_loop_in_one_graph():
+    # attention of every layer, lengths and positions advanced, eviction: captured once, replayed; as the same calls made directly
+    from paper_2507_08143_b200 import binding as B
+    L, heads, batch, g, page = 2, 3, 4, 2, 16
+    lens = np.random.default_rng(3).integers(40, 90, size=(L, heads, batch)).astype(np.int32)
+    lens[:, :, 2] = -1
+
+    def start():
+        _, cache, len_d = make_cache(lens, page, 20, 77)
+        gen = torch.Generator(device="cuda").manual_seed(5)
+        rnd = lambda *s: torch.randn(*s, device="cuda", generator=gen).bfloat16()
+        st = dict(cache=cache, len=len_d, pos=torch.full((batch,), 200, dtype=torch.int32, device="cuda"), q=rnd(L, batch, heads * g, 128),
+                  k=rnd(L, batch, heads, 128), v=rnd(L, batch, heads, 128), out=torch.zeros(L, batch, heads * g, 128, dtype=torch.bfloat16, device="cuda"),
+                  budgets=torch.full((L, heads, batch), 60, dtype=torch.int32, device="cuda"), opt=B.decode_options(g, 110, accumulate=True))
+        st["ws"] = B.alloc_paged_attention_workspace(cache, st["opt"])
+        return st
+
+    def step(s):
+        for l in range(L):
+            B.paged_attention(s["cache"], l, s["opt"], s["q"][l], s["len"], s["out"][l], s["ws"], k_new=s["k"][l], v_new=s["v"][l], new_positions=s["pos"])
+        s["len"].add_((s["len"] >= 0).int())
+        s["pos"].add_(1)
+        B.paged_evict(s["cache"], s["len"], s["budgets"], s["len"], 110, recent=8, next_position=s["pos"])
+
+    a, b = start(), start()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):                                        # set-up before capture, on a cache of its own
+        step(start())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a)
+    for i in range(5):
+        graph.replay()
+        step(b)
+    torch.cuda.synchronize()
+    assert torch.equal(a["len"], b["len"]) and torch.equal(a["out"], b["out"])
+    for x, y in zip(a["cache"].tensors, b["cache"].tensors):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    assert int(a["len"].max()) <= 60 and torch.all(a["len"][:, :, 2] == -1)
