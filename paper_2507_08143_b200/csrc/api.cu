@@ -1141,7 +1141,7 @@ bool decode_layout(const compactor_paged_cache* c, const compactor_decode_option
     if ((tiles + units * kDecodeUnitCost) * l->groups > 0x7fffffffLL || tiles + units * kDecodeMassUnitCost > 0x7fffffffLL || units * o->q_per_kv > 0x3fffffffLL) { *err = COMPACTOR_E_TOO_LARGE; return false; }
     l->workers = (int)std::min<long long>(sm_count(), tiles * l->groups) * kDecodeWarps;
     const size_t slots = (size_t)l->workers + (size_t)units * l->groups;
-    size_t off = align_up(sizeof(int) * 2 * ((size_t)units + 1));
+    size_t off = align_up(sizeof(int) * ((size_t)units + 1));
     l->off_ml = off;     off += align_up(sizeof(float) * 32 * slots);
     l->off_o = off;      off += align_up(sizeof(float) * kD * std::min(o->q_per_kv, kDecodeHeads) * slots);
     l->off_scores = off; off += o->accumulate != 0 ? align_up(sizeof(float) * (size_t)tiles * kDecodeTile * o->q_per_kv) : 0;
@@ -1188,7 +1188,6 @@ extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t 
         for (int b = 0; b <= a.nb; ++b) t.cu_seqlens[b] = shape->cu_seqlens[a.b0 + b];
         for (int b = 0; b < a.nb; ++b) t.cu_keep[b + 1] = done += keep_counts[a.b0 + b];
         CK(launch_paged_fill(a, t, st));
-        if (lengths_out != nullptr || status != nullptr) CK(launch_paged_fill_lengths(a, t, st));
     }
     return COMPACTOR_OK;
 }

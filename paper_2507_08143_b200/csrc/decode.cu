@@ -34,6 +34,7 @@ constexpr int kStageBytes = 2 * kTile * kRowBytes;     // K tile, V tile
 constexpr size_t kSmemBytes = (size_t)kWarps * kStages * kStageBytes;
 constexpr int kUnitCost = kDecodeUnitCost;
 constexpr int kMassUnitCost = kDecodeMassUnitCost;
+constexpr int kUnitsPerBlock = 1024;                   // most units that every block of the second kernel scans
 constexpr int kUnitsInSmem = 2048;                     // units whose token counts every CTA keeps at hand
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -78,7 +79,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // Tokens that a unit attends to, the new one included; 0 for a row without a sequence (negative length) and for a unit
 // that would not fit (reported by the caller).
 __device__ __forceinline__ int live_tokens(const DecodeArgs& a, int unit) {
-    const int n = __ldg(a.lengths + unit);
+    const int n = __ldcg(a.lengths + unit);
     if (n < 0) return 0;
     const long long t = (long long)n + (a.k_new != nullptr);
     return t > a.capacity ? 0 : (int)t;
@@ -127,7 +128,7 @@ struct Cursor {
 // Page ids of a unit, entry `e0 + lane` of its row of the table (-1 behind its last token's).
 __device__ __forceinline__ int page_ids(const DecodeArgs& a, const Cursor& c, int e0, int lane) {
     const int e = e0 + lane;
-    return e <= (c.tokens - 1) >> a.c.page_shift ? __ldg(a.c.table + (long long)c.unit * a.c.max_pages + e) : -1;
+    return e <= (c.tokens - 1) >> a.c.page_shift ? __ldcg(a.c.table + (long long)c.unit * a.c.max_pages + e) : -1;
 }
 
 // Query fragments (B operand) of a unit's group: head t * 8 + gid, channels 16 s + 2 tig, + 1 and + 8, + 9.
@@ -142,7 +143,7 @@ __device__ __forceinline__ void load_queries(const DecodeArgs& a, const Cursor& 
         const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + b * a.q_seq + (long long)(head0 + (on ? t * 8 + gid : 0)) * a.q_head);
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-            const uint32_t x0 = __ldg(q + s * 8 + tig), x1 = __ldg(q + s * 8 + tig + 4);
+            const uint32_t x0 = q[s * 8 + tig], x1 = q[s * 8 + tig + 4];
             qf[t][s][0] = on ? x0 : 0u;
             qf[t][s][1] = on ? x1 : 0u;
         }
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 decode_kernel(const __grid_constant__ DecodeArgs a) {
     extern __shared__ __align__(1024) unsigned char ring[];
     __shared__ int cum[kThreads + 1];
-    __shared__ long long warp_sum[kWarps];
+    __shared__ int warp_sum[kWarps];
     __shared__ int bad[kWarps][kStages];
     __shared__ int new_page[kWarps][kStages];
     __shared__ int live[kUnitsInSmem];
@@ -165,42 +166,37 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
     // cost before each thread's run of units
     const int per = (a.units + kThreads - 1) / kThreads;
     const int u0 = tid * per, u1 = min(a.units, u0 + per);
-    long long mine = 0;                                      // cost, and in the upper half how many units have tokens
+    int mine = 0;
     for (int u = u0; u < u1; ++u) {
         const int n = live_tokens(a, u);
         if (u < kUnitsInSmem) live[u] = n;
-        mine += cost_of(n) + ((long long)(n > 0) << 32);
+        mine += cost_of(n);
     }
-    long long incl = mine;
+    int incl = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+        const int o = __shfl_up_sync(0xffffffffu, incl, d);
         if (lane >= d) incl += o;
     }
     if (lane == 31) warp_sum[warp] = incl;
     __syncthreads();
-    long long before = 0;
+    int before = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) before += w < warp ? warp_sum[w] : 0;
-    cum[tid + 1] = (int)(before + incl);
+    cum[tid + 1] = before + incl;
     if (tid == 0) cum[0] = 0;
     __syncthreads();
     const int all = cum[kThreads];
     if (blockIdx.x == 0) {                                   // for the second kernel, and the units that are refused
-        int at = cum[tid], units = (int)((before + incl - mine) >> 32);
+        int at = cum[tid];
         for (int u = u0; u < u1; ++u) {
-            a.prefix[2 * u] = at;
-            a.prefix[2 * u + 1] = at + units * (kMassUnitCost - kUnitCost);
-            const int live = live_tokens(a, u), n = __ldg(a.lengths + u);
-            at += cost_of(live);
-            units += live > 0;
+            a.prefix[u] = at;
+            at += cost_of(live_tokens(a, u));
+            const int n = __ldcg(a.lengths + u);
             if (a.status != nullptr && n >= 0 && (long long)n + (a.k_new != nullptr) > a.capacity)
                 atomicOr(a.status + u, COMPACTOR_STATUS_CAPACITY);
         }
-        if (tid == kThreads - 1) {
-            a.prefix[2 * a.units] = all;
-            a.prefix[2 * a.units + 1] = all + units * (kMassUnitCost - kUnitCost);
-        }
+        if (tid == 0) a.prefix[a.units] = all;
     }
     const int total = all * a.groups;
     const int workers = active_workers(a, total);
@@ -471,7 +467,7 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
                 *reinterpret_cast<uint4*>((row_hi == 0 ? a.c.k : a.c.v) + row_in_pool(a.c, page, cached) + piece * 8) = x;
                 const long long at = slot_in_pool(a.c, page, cached);
                 if (lane == 0 && a.c.positions != nullptr)
-                    a.c.positions[at] = a.new_positions != nullptr ? __ldg(a.new_positions + cc.unit % a.c.batch) : cached;
+                    a.c.positions[at] = a.new_positions != nullptr ? a.new_positions[cc.unit % a.c.batch] : cached;
                 if (lane == 0 && a.c.mass != nullptr && !a.accumulate) a.c.mass[at] = 0.f;
             }
         }
@@ -560,17 +556,37 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
     __shared__ float part_m[kStreams], part_l[kStreams];
     __shared__ float red_m[kWarps][16], red_l[kWarps][16];
     __shared__ float lse2[64];
-    __shared__ int counted[kWarps];
+    __shared__ long long sums[kWarps];
+    __shared__ int found[3];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // Until pdl_wait() nothing of the first kernel's is read: what depends on lengths, pages and old weights alone (they were there
+    // before it began, and are read from L2) is worked out while its last warps finish.  No block ends before pdl_wait(): the next launch counts on both kernels being done.
     if (kWarps == 16) pdl_trigger();                         // (else the next call's blocks would take the registers of the later blocks of this one)
-    pdl_wait();
-    const int all = a.prefix[2 * a.units];
     if ((int)blockIdx.x >= mass_blocks) {
         const int item = (blockIdx.x - mass_blocks) / kSplit, unit = item / a.g, head = item - unit * a.g;
         const int channel0 = ((blockIdx.x - mass_blocks) % kSplit) * kChannels;
         const int grp = head / kDecodeHeads, hh = head - grp * kDecodeHeads, gg = min(a.g, kDecodeHeads);
         const int h = unit / a.c.batch, b = unit - h * a.c.batch;
-        const int at = a.prefix[2 * unit], cost = a.prefix[2 * unit + 2] - at;
+        int at, cost, all;                                   // the unit's place and cost, the cost of all units
+        if (a.units <= kUnitsPerBlock) {
+            long long x = 0;                                 // cost before the unit, and in the upper half of all
+            for (int u = tid; u < a.units; u += kThreads) {
+                const int c = cost_of(live_tokens(a, u));
+                x += ((long long)c << 32) + (u < unit ? c : 0);
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+            if (lane == 0) sums[warp] = x;
+            __syncthreads();
+            x = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) x += sums[w];
+            at = (int)x; all = (int)(x >> 32); cost = cost_of(live_tokens(a, unit));
+            pdl_wait();
+        } else {                                             // the first kernel's prefix, so that the many blocks need not scan the many units
+            pdl_wait();
+            at = a.prefix[unit]; cost = a.prefix[unit + 1] - at; all = a.prefix[a.units];
+        }
         __nv_bfloat16* dst = a.out + b * a.out_seq + (long long)(h * a.g + head) * a.out_head + channel0;
         float* lse = a.lse != nullptr && channel0 == 0 ? a.lse + (long long)b * (a.c.heads * a.g) + h * a.g + head : nullptr;
         if (cost == 0) {
@@ -579,7 +595,7 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
             return;
         }
         const Pieces ps = pieces_of(a, unit, grp, at, cost, all);
-        if (ps.n == 1) return;                               // written by the warp that had it whole
+        if (ps.n == 1) return;                               // written by the warp that had it whole (pdl_wait() is behind us)
         float m = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         const int stream = warp * kSplit + lane / kLanes, channel = lane % kLanes * 4;
@@ -633,42 +649,71 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
     }
 
     // weights: w_j += sum over the unit's query heads of 2^(y_j - lse)
-    const int all_mass = a.prefix[2 * a.units + 1];
-    const Share share(all_mass, mass_blocks);
-    int place = share.begin(blockIdx.x);
-    const int place_end = place + share.size(blockIdx.x);
-    if (place >= place_end) return;
-    int below = 0;                                           // the last unit that begins at or before `place`: it has tokens
-    for (int u = tid; u < a.units; u += kThreads) below += a.prefix[2 * u + 1] <= place;
-    below = __reduce_add_sync(0xffffffffu, below);
-    if (lane == 0) counted[warp] = below;
-    __syncthreads();
-    int unit = -1;
+    int unit, at, place_of_unit, all;                        // the unit that holds this block's first place, its place for the tiles and for the weights
+    int place, place_end;
+    {
+        const int per = (a.units + kThreads - 1) / kThreads, u0 = tid * per, u1 = min(a.units, u0 + per);
+        long long mine = 0;                                  // cost, and in the upper half how many units have tokens
+        for (int u = u0; u < u1; ++u) {
+            const int n = live_tokens(a, u);
+            mine += cost_of(n) + ((long long)(n > 0) << 32);
+        }
+        long long incl = mine;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) unit += counted[w];
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += o;
+        }
+        if (lane == 31) sums[warp] = incl;
+        __syncthreads();
+        long long before = incl - mine, total = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) before += sums[w];
+            total += sums[w];
+        }
+        constexpr int kMore = kMassUnitCost - kUnitCost;
+        all = (int)total;
+        const Share share(all + (int)(total >> 32) * kMore, mass_blocks);
+        place = share.begin(blockIdx.x);
+        place_end = place + share.size(blockIdx.x);
+        int my_at = (int)before, my_place = my_at + (int)(before >> 32) * kMore;
+        for (int u = u0; u < u1; ++u) {
+            const int c = cost_of(live_tokens(a, u));
+            if (c == 0) continue;
+            if (my_place <= place && place < my_place + c + kMore) { found[0] = u; found[1] = my_at; found[2] = my_place; }
+            my_at += c; my_place += c + kMore;
+        }
+        __syncthreads();
+        if (place >= place_end) { pdl_wait(); return; }
+        unit = found[0]; at = found[1]; place_of_unit = found[2];
+    }
     int hp = 1;                                              // lanes side by side for the heads of a group
     while (hp < min(a.g, kDecodeHeads)) hp *= 2;
     const int hh = lane & (hp - 1), st = tid / hp, streams = kThreads / hp;
     for (; place < place_end; ++unit) {
-        const int4 here = make_int4(a.prefix[2 * unit], a.prefix[2 * unit + 1], a.prefix[2 * unit + 2], a.prefix[2 * unit + 3]);
-        const int n = live_tokens(a, unit);
+        const int n = live_tokens(a, unit), cost = cost_of(n);
         if (n == 0) continue;
-        const int at = here.x, cost = here.z - at;
-        const int first_tile = max(0, place - here.y - kMassUnitCost), last_tile = min(place_end, here.w) - here.y - kMassUnitCost;
-        place = here.w;
+        const int here = at, first_place = place_of_unit + kMassUnitCost;
+        at += cost;
+        place_of_unit += tiles_of(n) + kMassUnitCost;
+        const int first_tile = max(0, place - first_place), last_tile = min(place_end, place_of_unit) - first_place;
+        place = place_of_unit;
         if (last_tile <= first_tile) continue;               // only the unit's head
         const int tok0 = first_tile * kTile, tok1 = min(n, last_tile * kTile);
         const int cached = n - (a.k_new != nullptr);
         // four tokens a thread: they share a page and a 16-byte piece of its weights
         int page;
         float4 old;
-        auto ask_page = [&](int first) { page = page_of(a.c, unit, min(first, (tok1 - 1) & ~3)); };
+        auto ask_page = [&](int first) { page = page_of<true>(a.c, unit, min(first, (tok1 - 1) & ~3)); };
         auto ask_weights = [&](int first) {
-            old = *reinterpret_cast<const float4*>(a.c.mass + slot_in_pool(a.c, max(page, 0), min(first, (tok1 - 1) & ~3)));
+            old = __ldcg(reinterpret_cast<const float4*>(a.c.mass + slot_in_pool(a.c, max(page, 0), min(first, (tok1 - 1) & ~3))));
         };
         ask_page(tok0 + 4 * tid);
+        ask_weights(tok0 + 4 * tid);
+        pdl_wait();
         for (int grp = 0; grp < a.groups; ++grp) {
-            const Pieces ps = pieces_of(a, unit, grp, at, cost, all);
+            const Pieces ps = pieces_of(a, unit, grp, here, cost, all);
             const int heads = min(kDecodeHeads, a.g - grp * kDecodeHeads);
             float m = -INFINITY, l = 0.f;
             if (hh < heads) {
@@ -678,7 +723,6 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
                     merge(m, l, ml[0], ml[16]);
                 }
             }
-            if (grp == 0) ask_weights(tok0 + 4 * tid);       // the page ids have arrived with the pieces
             // the block's maximum per head, then the sums against it: a tree of single shuffles each, then one round over the warps
             float top = m;
             for (int d = hp; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -725,6 +769,7 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
         }
         __syncthreads();                                     // lse2 and the reductions are the next unit's
     }
+    pdl_wait();                                              // (a block that met only heads of units has not waited yet)
 }
 
 }  // namespace

@@ -21,7 +21,7 @@ constexpr int kFillBatch = 4;                   // rows per thread in flight (2:
 
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n"
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
@@ -34,18 +34,40 @@ __device__ __forceinline__ int kept_rows(const FillArgs& a, const FillTables& t,
 }
 // Slot of a unit's first new row; -1 if the unit takes none (no sequence in the row, or no room).
 __device__ __forceinline__ int first_slot(const FillArgs& a, int unit, int rows) {
-    const int n = a.lengths != nullptr ? __ldg(a.lengths + unit) : 0;
+    const int n = a.lengths != nullptr ? a.lengths[unit] : 0;
     if (n < 0) return -1;
     return (long long)n + rows > ((long long)a.c.max_pages << a.c.page_shift) ? -1 : n;
 }
 
+// New lengths, and the units that had no room.
+__device__ __forceinline__ void write_lengths(const FillArgs& a, const FillTables& t, long long i) {
+    if (i >= (long long)a.layers * a.c.heads * a.nb) return;
+    const int b = (int)(i % a.nb), lh = (int)(i / a.nb), layer = lh / a.c.heads, head = lh - layer * a.c.heads;
+    const int unit = ((a.first_layer + layer) * a.c.heads + head) * a.c.batch + a.b0 + b;
+    const int rows = kept_rows(a, t, layer, head, b), first = first_slot(a, unit, rows);
+    const int n = a.lengths != nullptr ? a.lengths[unit] : 0;
+    if (first < 0 && n >= 0 && a.status != nullptr) atomicOr(a.status + unit, COMPACTOR_STATUS_CAPACITY);
+    if (a.lengths_out != nullptr) a.lengths_out[unit] = first < 0 ? n : n + rows;
+}
+// Where lengths_out is lengths, which every block of the fill reads, they are written by a launch of their own.
+__global__ void fill_lengths_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTables t) {
+    pdl_trigger();
+    pdl_wait();
+    write_lengths(a, t, (long long)blockIdx.x * blockDim.x + threadIdx.x);
+}
+
 template <bool ACROSS>
 __global__ void __launch_bounds__(kFillThreads)
-fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTables t) {
+fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTables t, int row_blocks) {
     __shared__ long long src_k[kFillRows], src_v[kFillRows], dst[kFillRows];       // elements; dst < 0: the row is skipped
     const int tid = threadIdx.x;
     pdl_trigger();
     pdl_wait();
+    if ((int)blockIdx.x >= row_blocks) {                     // blocks behind those with rows: the lengths, a row of the grid's share each
+        const long long per = ((long long)a.layers * a.c.heads * a.nb + gridDim.y - 1) / gridDim.y;
+        for (long long i = tid; i < per; i += kFillThreads) write_lengths(a, t, blockIdx.y * per + i);
+        return;
+    }
     const int layer = ACROSS ? blockIdx.y : blockIdx.y / a.c.heads;
     const long long per_outer = ACROSS ? (long long)a.c.heads * a.total_keep : a.total_keep;     // rows per layer or (layer, head)
     const int scale = ACROSS ? a.c.heads : 1;
@@ -55,7 +77,7 @@ fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTabl
         const long long row = row0 + tid;
         long long to = -1;
         if (row < end) {
-            const int local0 = a.idx != nullptr ? __ldg(a.idx + (long long)blockIdx.y * per_outer + row) : 0;
+            const int local0 = a.idx != nullptr ? a.idx[(long long)blockIdx.y * per_outer + row] : 0;
             const int b = find_segment(t.cu_keep, a.nb, (int)(row / scale));
             int head, j;
             if (ACROSS) {
@@ -72,7 +94,7 @@ fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTabl
             const int unit = ((a.first_layer + layer) * a.c.heads + head) * a.c.batch + a.b0 + b;
             const int rows = kept_rows(a, t, layer, head, b), first = first_slot(a, unit, rows);
             if (first >= 0 && j >= 0 && j < rows && (unsigned)local < (unsigned)n) {
-                const int slot = first + j, page = page_of(a.c, unit, slot);
+                const int slot = first + j, page = page_of<false>(a.c, unit, slot);
                 if (page >= 0) {
                     const long long tok = (long long)t.cu_seqlens[b] + local;
                     to = row_in_pool(a.c, page, slot);
@@ -111,21 +133,6 @@ fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTabl
             *(reinterpret_cast<uint4*>(a.c.v + dst[r]) + piece) = vv[u];
         }
     }
-}
-
-// New lengths, and the units that had no room.  A launch of its own: lengths_out may be lengths, which every block of the
-// fill reads.
-__global__ void fill_lengths_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTables t) {
-    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    pdl_trigger();
-    pdl_wait();
-    if (i >= (long long)a.layers * a.c.heads * a.nb) return;
-    const int b = (int)(i % a.nb), lh = (int)(i / a.nb), layer = lh / a.c.heads, head = lh - layer * a.c.heads;
-    const int unit = ((a.first_layer + layer) * a.c.heads + head) * a.c.batch + a.b0 + b;
-    const int rows = kept_rows(a, t, layer, head, b), first = first_slot(a, unit, rows);
-    const int n = a.lengths != nullptr ? a.lengths[unit] : 0;
-    if (first < 0 && n >= 0 && a.status != nullptr) atomicOr(a.status + unit, COMPACTOR_STATUS_CAPACITY);
-    if (a.lengths_out != nullptr) a.lengths_out[unit] = first < 0 ? n : n + rows;
 }
 
 // ------------------------------------------------------------------------------------------ evict
@@ -193,7 +200,7 @@ __device__ __forceinline__ void block_prefix2(EvictShared<kThreads>& s, int& x, 
 
 // One unit.  `part`: which units the launch is for.
 enum { kEvictAll, kEvictLong, kEvictShort };
-template <int kThreads>
+template <int kThreads, bool L2>
 __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, int part) {
     constexpr int kWarps = kThreads / 32;
     constexpr int kRowBatch = kThreads == kSmallThreads ? 4 : 8;     // rows per warp in flight
@@ -204,7 +211,7 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
     const int cluster_size = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int unit = a.first_unit + (int)(blockIdx.x / cluster_size);
-    const int n = a.lengths[unit], budget = a.budgets[unit];
+    const int n = load<L2>(a.lengths + unit), budget = load<L2>(a.budgets + unit);
     const long long capacity = min((long long)a.max_length, (long long)a.c.max_pages << a.c.page_shift);
     if (part == kEvictLong ? n <= kSmallSlice : part == kEvictShort && n > kSmallSlice) return;
     // nothing to do: the same decision in every CTA of the cluster, before any barrier between them
@@ -225,7 +232,7 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
     };
     const int slice = ((n + ranks - 1) / ranks + 31) / 32 * 32;              // at most slice_cap
     const int lo = min(n, rank * slice), count = min(n, lo + slice) - lo;
-    const int recent_from = a.recent > 0 ? a.next_position[unit % a.c.batch] - min(a.recent, budget) : 0;
+    const int recent_from = a.recent > 0 ? load<L2>(a.next_position + unit % a.c.batch) - min(a.recent, budget) : 0;
 
     if (tid == 0) s.bad = 0;
     for (int i = tid; i < 2 * kBins / 4; i += kThreads) reinterpret_cast<int4*>(s.hist)[i] = make_int4(0, 0, 0, 0);
@@ -236,14 +243,14 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
         int page[kLoadBatch];
         int4 pos[kLoadBatch];
 #pragma unroll
-        for (int k = 0; k < kLoadBatch; ++k) page[k] = page_of(a.c, unit, lo + 4 * min(q0 + k * kThreads, quads - 1));
+        for (int k = 0; k < kLoadBatch; ++k) page[k] = page_of<L2>(a.c, unit, lo + 4 * min(q0 + k * kThreads, quads - 1));
 #pragma unroll
         for (int k = 0; k < kLoadBatch; ++k) {               // weights into the keys' place, positions into registers: all in flight at once
             const int q = min(q0 + k * kThreads, quads - 1);
             const long long at = slot_in_pool(a.c, max(page[k], 0), lo + 4 * q);
             if (q0 + k * kThreads < quads)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(key_s + 16 * q), "l"(a.c.mass + at) : "memory");
-            pos[k] = a.recent > 0 ? *reinterpret_cast<const int4*>(a.c.positions + at) : make_int4(0, 0, 0, 0);
+            pos[k] = a.recent > 0 ? load<L2>(reinterpret_cast<const int4*>(a.c.positions + at)) : make_int4(0, 0, 0, 0);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");     // each thread reads only what it copied itself
 #pragma unroll
@@ -424,11 +431,11 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
             while (jm >= s.rank_movers[rm]) jm -= s.rank_movers[rm++];
             const int to = (int)cluster.map_shared_rank(key, rh)[jh];
             const int from = (int)cluster.map_shared_rank(key, rm)[s.rank_holes[rm] + jm];
-            const int from_page = page_of(a.c, unit, from), to_page = page_of(a.c, unit, to);
+            const int from_page = page_of<L2>(a.c, unit, from), to_page = page_of<L2>(a.c, unit, to);
             move[tid] = make_int4(from_page, from, to_page, to);
             const long long f = slot_in_pool(a.c, from_page, from), t = slot_in_pool(a.c, to_page, to);
-            const float w = a.c.mass[f];
-            const int pos = a.c.positions != nullptr ? a.c.positions[f] : 0;
+            const float w = load<L2>(a.c.mass + f);
+            const int pos = a.c.positions != nullptr ? load<L2>(a.c.positions + f) : 0;
             a.c.mass[t] = w;
             if (a.c.positions != nullptr) a.c.positions[t] = pos;
         }
@@ -439,7 +446,7 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
 #pragma unroll
             for (int k = 0; k < kRowBatch; ++k) {
                 const int4 mv = move[min(i + k, batch - 1)];       // loads without a condition stay in flight together
-                x[k] = *(reinterpret_cast<const uint4*>(pool + row_in_pool(a.c, mv.x, mv.y)) + piece);
+                x[k] = load<L2>(reinterpret_cast<const uint4*>(pool + row_in_pool(a.c, mv.x, mv.y)) + piece);
                 to[k] = row_in_pool(a.c, mv.z, mv.w);
             }
 #pragma unroll
@@ -455,20 +462,20 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
 }
 
 // kEvictShort runs beside a launch for the long units, which holds it back only from ending: what came before that launch is
-// complete when it lets this one start, and the two touch different units.  (A length that the other launch has already replaced,
+// complete when it lets this one start (which reads from L2, where all of that is), and the two touch different units.  (A length that the other launch has already replaced,
 // where lengths_out is lengths, reads as a unit at its budget, which stays as it is.)
-template <int kThreads>
+template <int kThreads, int PART>
 __global__ void __launch_bounds__(kThreads, kThreads == kSmallThreads ? 4 : 1)
-evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap, int part) {
-    if (part != kEvictShort) pdl_wait();
+evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
+    if (PART != kEvictShort) pdl_wait();
     pdl_trigger();
-    evict_unit<kThreads>(a, slice_cap, part);
-    if (part == kEvictShort) pdl_wait();
+    evict_unit<kThreads, PART == kEvictShort>(a, slice_cap, PART);
+    if (PART == kEvictShort) pdl_wait();
 }
 
-template <int kThreads>
-cudaError_t launch_evict(const EvictArgs& a, int ranks, int max_length, int part, cudaStream_t stream) {
-    const auto kernel = evict_kernel<kThreads>;
+template <int kThreads, int PART>
+cudaError_t launch_evict(const EvictArgs& a, int ranks, int max_length, cudaStream_t stream) {
+    const auto kernel = evict_kernel<kThreads, PART>;
     static std::atomic<unsigned long long> done;
     cudaError_t e = allow_smem(kernel, (kThreads == kSmallThreads ? kSmallSlice : kLargeSlice) * (int)sizeof(uint32_t), done);
     if (e != cudaSuccess) return e;
@@ -492,7 +499,7 @@ cudaError_t launch_evict(const EvictArgs& a, int ranks, int max_length, int part
             cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg) == cudaSuccess && fit >= a.units) break;
         (void)cudaGetLastError();
     }
-    e = cudaLaunchKernelEx(&cfg, kernel, a, slice_cap, part);
+    e = cudaLaunchKernelEx(&cfg, kernel, a, slice_cap);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -501,12 +508,15 @@ cudaError_t launch_evict(const EvictArgs& a, int ranks, int max_length, int part
 cudaError_t launch_paged_fill(const FillArgs& a, const FillTables& t, cudaStream_t stream) {
     const bool across = a.head_offsets != nullptr;
     const long long rows = (long long)(t.cu_keep[a.nb] - t.cu_keep[0]) * (across ? a.c.heads : 1);
-    if (rows == 0) return cudaSuccess;
-    const dim3 grid((unsigned)((rows + kFillRows - 1) / kFillRows), across ? a.layers : a.layers * a.c.heads);
-    return launch_chained(kPdlOther, across ? fill_kernel<true> : fill_kernel<false>, grid, dim3(kFillThreads), 0, stream, a, t);
-}
-
-cudaError_t launch_paged_fill_lengths(const FillArgs& a, const FillTables& t, cudaStream_t stream) {
+    const bool lengths = a.lengths_out != nullptr || a.status != nullptr, apart = lengths && (rows == 0 || a.lengths_out == a.lengths);
+    if (rows > 0) {
+        const int row_blocks = (int)((rows + kFillRows - 1) / kFillRows);
+        const dim3 grid((unsigned)(row_blocks + (lengths && !apart ? 1 : 0)), across ? a.layers : a.layers * a.c.heads);
+        const cudaError_t e = launch_chained(kPdlOther, across ? fill_kernel<true> : fill_kernel<false>, grid, dim3(kFillThreads), 0, stream,
+                                             a, t, row_blocks);
+        if (e != cudaSuccess) return e;
+    }
+    if (!apart) return cudaSuccess;
     const long long units = (long long)a.layers * a.c.heads * a.nb;
     return launch_chained(kPdlOther, fill_lengths_kernel, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, stream, a, t);
 }
@@ -521,17 +531,17 @@ cudaError_t launch_paged_evict(const EvictArgs& a, int sm_count, cudaStream_t st
     const int n = a.max_length;
     cudaError_t e;
     if (n <= 8 * kSmallSlice && (long long)a.units * 8 > 2 * sm_count) {
-        if (n <= kSmallSlice) return launch_evict<kSmallThreads>(a, 1, n, kEvictAll, stream);
+        if (n <= kSmallSlice) return launch_evict<kSmallThreads, kEvictAll>(a, 1, n, stream);
         int ranks = 2;
         while (n > ranks * kSmallSlice) ranks *= 2;
-        e = launch_evict<kSmallThreads>(a, ranks, n, kEvictLong, stream);
-        return e != cudaSuccess ? e : launch_evict<kSmallThreads>(a, 1, kSmallSlice, kEvictShort, stream);
+        e = launch_evict<kSmallThreads, kEvictLong>(a, ranks, n, stream);
+        return e != cudaSuccess ? e : launch_evict<kSmallThreads, kEvictShort>(a, 1, kSmallSlice, stream);
     }
     int ranks = 1;
     while ((ranks < 8 && n > (long long)ranks * 12288) ||
            (ranks < kMaxCluster && (long long)a.units * ranks * 2 <= sm_count && n > 4096LL * ranks))
         ranks *= 2;
-    return launch_evict<kLargeThreads>(a, ranks, n, kEvictAll, stream);
+    return launch_evict<kLargeThreads, kEvictAll>(a, ranks, n, stream);
 }
 
 }  // namespace compactor

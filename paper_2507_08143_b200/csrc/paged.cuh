@@ -18,10 +18,16 @@ struct Paged {
     int layers, heads, batch;
 };
 
+// Chained kernels are already running while their predecessor still writes.  What they read after pdl_wait() they read plainly; never
+// through the read-only path (ld.global.nc), whose lines may be old.  What a kernel reads before pdl_wait() (because a
+// kernel further back in the chain has waited for its writer) it reads from L2 (`L2`).
+template <bool L2, typename T> __device__ __forceinline__ T load(const T* p) { return L2 ? __ldcg(p) : *p; }
+
 // Page of slot `slot` of unit `unit`, or -1 where the table holds no page of the pool.  The caller has checked that
 // the slot lies within the unit's row of the table.
+template <bool L2>
 __device__ __forceinline__ int page_of(const Paged& c, int unit, int slot) {
-    const int id = __ldg(c.table + (long long)unit * c.max_pages + (slot >> c.page_shift));
+    const int id = load<L2>(c.table + (long long)unit * c.max_pages + (slot >> c.page_shift));
     return (unsigned)id < (unsigned)c.n_pages ? id : -1;
 }
 // Element offset of a slot's row in the pools, given its page (64 bits: a pool may hold more than 2^32 elements).
@@ -65,7 +71,6 @@ struct FillArgs {
     int* status;
 };
 cudaError_t launch_paged_fill(const FillArgs& a, const FillTables& t, cudaStream_t stream);
-cudaError_t launch_paged_fill_lengths(const FillArgs& a, const FillTables& t, cudaStream_t stream);
 
 // One new token per sequence against one layer of the cache.
 struct DecodeArgs {
@@ -88,7 +93,7 @@ struct DecodeArgs {
     float scale, softcap;                  // softcap <= 0: none
     int units;
     int workers;                           // warps that share the tokens
-    int* prefix;                           // workspace: [units + 1][2] cost before each unit, for the tiles and for the weights
+    int* prefix;                           // workspace: [units + 1] cost before each unit
     float* ml;                             // workspace: [workers + units * groups][2][16] running maximum and sum
     float* o;                              // workspace: [workers + units * groups][min(g, 16)][128]
     float* scores;                         // workspace: [units][g][unit_rows] in base 2, only when accumulating
