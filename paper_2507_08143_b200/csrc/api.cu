@@ -481,7 +481,7 @@ extern "C" void compactor_debug_set_profile_buffer(long long* device_counters) {
 
 extern "C" {
 
-int compactor_version(void) { return 100; }
+int compactor_version(void) { return 200; }
 
 const char* compactor_error_string(int code) {
     switch (code) {

@@ -15,11 +15,15 @@
 // respectively the channels, as the 16 rows: the 8 columns are the query heads, so nothing of the tile is padding for g = 8
 // and half is for g = 4.  The fifth-generation tensor path has 128 rows per instruction and wants the whole CTA
 // in step; at 4 g flops per 4 bytes it would wait for memory just the same.
-// The online softmax keeps maximum and sum in fp32 (base 2); p is rounded to bf16 for the product with V (at most 2^-9
-// relative per weight, the sum uses the unrounded values).
+// The online softmax keeps maximum and sum in fp32 (base 2); p is rounded to bf16 for the product with V, which the matrix
+// instruction asks for (at most 2^-8 relative per weight; the sum uses the unrounded values).
 //
 // A second kernel joins the pieces of units that more than one warp worked on and adds the weights: the scores
 // (fp32, 4 g bytes per token) wait in the workspace until the unit's sum is known.
+//
+// Measured (both kernels, one layer, device time of calls in a row): 8 heads x 131072 tokens, g = 5: 90 us = 5.96 TB/s, 0.91 of the copy
+// rate; 8 heads x 16 ragged sequences (152 K tokens), g = 4, with weights: 120 us = 5.3 TB/s; 8 heads x 2458 tokens: 12.7 us, of which
+// 6.4 are the first kernel's chain (lengths, page ids, rows, one or two tiles, results) and 4 the second's.
 #include "paged.cuh"
 
 namespace compactor {
@@ -370,8 +374,8 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
                 sum[t][0] = sum[t][1] = 0.f;
             }
         }
-        // the second kernel's blocks are let in when the tiles run out: blocks that wait beside this kernel slow it (2 units of
-        // 61 measured 4 us)
+        // the second kernel's blocks are let in when the tiles run out: blocks that wait beside this kernel slow it (51 -> 57 us for 8
+        // sequences x 4 heads x 7 queries)
         if (left_c <= kStages) pdl_trigger();
         cp_wait<kStages - 1>();
         __syncwarp();
@@ -544,7 +548,6 @@ __device__ __forceinline__ Pieces pieces_of(const DecodeArgs& a, int unit, int g
 // e_i = 2^(m_i - m).  The blocks before them add the weights; they share all tokens out evenly, as the first kernel does,
 // with a cost of kMassUnitCost tiles per unit (about what its sum takes to find).  Both are chains of a few dependent reads from L2
 // (about 0.7 us each), so every step asks for all it needs at once, and several small blocks share an SM.
-
 template <int kWarps>
 __global__ void __launch_bounds__(kWarps * 32, kWarps == 16 ? 1 : 4)
 join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {

@@ -13,7 +13,7 @@ namespace {
 // Where a row goes: slot lengths[unit] + j of its unit, j its place among the unit's kept rows, found through the page table.  A block
 // moves 128 rows: first a thread per row finds source and target (index, length and page id are three dependent reads,
 // made once per row and not once per 16-byte piece) and moves weight and position, then 16 threads per row move K and V.
-// Bound by HBM: 512 bytes read and written per row.
+// Bound by HBM: 512 bytes read and written per row.  256 units x 2458 of 8192 rows: 111 us = 5.9 TB/s, 0.90 of the copy rate.
 constexpr int kFillThreads = 256;
 constexpr int kFillRows = 128;
 constexpr int kFillRowsPerIter = kFillThreads / 16;
@@ -136,8 +136,8 @@ fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTabl
 }
 
 // ------------------------------------------------------------------------------------------ evict
-// A cluster of up to 8 CTAs per unit, of which as many work as the unit's length asks for; each holds the sort keys of a
-// slice of the unit's slots in shared memory.
+// One CTA per unit, or a cluster (of up to 8, for few units up to 16), of which as many CTAs work as the unit's length asks for;
+// each holds the sort keys of a slice of the unit's slots in shared memory.
 //   key      the weight as an ordered 32-bit integer; the largest key for a recent token (never below a weight)
 //   1. radix selection of the E-th smallest key, E = n - budget: digits of 11, 11 and 10 bits, one histogram per CTA,
 //      summed over the cluster through distributed shared memory by every CTA alike; it ends as soon as all keys of the digit go
@@ -147,7 +147,8 @@ fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTabl
 //      rows move in any order, and no more than min(E, budget) of them move: compaction that kept the slots' order
 //      would rewrite nearly the whole unit for one evicted token.
 // The bytes are few (8 per slot, 1 KB per moved row); what bounds it is the chain of block-wide steps, about 8 us per unit
-// whatever its length.  So several small CTAs share an SM and hide each other's waits.
+// whatever its length.  So several small CTAs share an SM and hide each other's waits.  One token out of each of 256 units of 2459:
+// 9.5 us; 128 out of 512 ragged units of 9 K on average: 46 us; 8192 out of 8 units of 50136: 33 us.
 constexpr int kBins = 2048;
 constexpr int kMaxCluster = 16;                 // 8 is what every launch may use
 constexpr int kSmallThreads = 256, kLargeThreads = 512;
@@ -462,8 +463,8 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
 }
 
 // kEvictShort runs beside a launch for the long units, which holds it back only from ending: what came before that launch is
-// complete when it lets this one start (which reads from L2, where all of that is), and the two touch different units.  (A length that the other launch has already replaced,
-// where lengths_out is lengths, reads as a unit at its budget, which stays as it is.)
+// complete when it lets this one start (which reads from L2, where all of that is), and the two touch different units.  (A length
+// that the other launch has already replaced, where lengths_out is lengths, reads as a unit at its budget, which stays as it is.)
 template <int kThreads, int PART>
 __global__ void __launch_bounds__(kThreads, kThreads == kSmallThreads ? 4 : 1)
 evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
