@@ -544,19 +544,22 @@ __device__ __forceinline__ Pieces pieces_of(const DecodeArgs& a, int unit, int g
     return {(long long)w0 + (long long)unit * a.groups + grp, w1 - w0 + 1};
 }
 
-// The last units * g blocks have one (unit, query head) each, whose pieces they join: o = sum_i e_i o_i / sum_i e_i l_i with
+// The last blocks have kItems (unit, query head) pairs each, whose pieces they join: o = sum_i e_i o_i / sum_i e_i l_i with
 // e_i = 2^(m_i - m).  The blocks before them add the weights; they share all tokens out evenly, as the first kernel does,
 // with a cost of kMassUnitCost tiles per unit (about what its sum takes to find).  Both are chains of a few dependent reads from L2
 // (about 0.7 us each), so every step asks for all it needs at once, and several small blocks share an SM.
-template <int kWarps>
+template <int kWarps, int kItems>
 __global__ void __launch_bounds__(kWarps * 32, kWarps == 16 ? 1 : 4)
 join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
     constexpr int kThreads = kWarps * 32;
     constexpr int kJoinBatch = kWarps == 16 ? 8 : 4;         // pieces per warp in flight
     // a large block takes half of the channels of its (unit, head): twice as many pieces in flight per warp
-    constexpr int kSplit = kWarps == 16 ? 2 : 1, kLanes = 32 / kSplit, kStreams = kWarps * kSplit, kChannels = kD / kSplit;
-    __shared__ float part[kStreams][kChannels];
-    __shared__ float part_m[kStreams], part_l[kStreams];
+    constexpr int kSplit = kWarps == 16 ? 2 : 1, kLanes = 32 / kSplit, kChannels = kD / kSplit;
+    constexpr int kItemWarps = kWarps / kItems, kStreams = kItemWarps * kSplit;
+    static_assert(kItems == 1 || kSplit == 1, "a block has several pairs or half of one");
+    __shared__ float part[kItems * kStreams][kChannels];
+    __shared__ float part_m[kItems * kStreams], part_l[kItems * kStreams];
+    __shared__ bool to_write[kItems];
     __shared__ float red_m[kWarps][16], red_l[kWarps][16];
     __shared__ float lse2[64];
     __shared__ long long sums[kWarps];
@@ -566,14 +569,14 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
     // before it began, and are read from L2) is worked out while its last warps finish.  No block ends before pdl_wait(): the next launch counts on both kernels being done.
     if (kWarps == 16) pdl_trigger();                         // (else the next call's blocks would take the registers of the later blocks of this one)
     if ((int)blockIdx.x >= mass_blocks) {
-        const int item = (blockIdx.x - mass_blocks) / kSplit, unit = item / a.g, head = item - unit * a.g;
+        const int nth = warp / kItemWarps, warp_of_item = warp - nth * kItemWarps;
+        const int item = (blockIdx.x - mass_blocks) / kSplit * kItems + nth, unit = min(item / a.g, a.units - 1);
         const int channel0 = ((blockIdx.x - mass_blocks) % kSplit) * kChannels;
-        const int grp = head / kDecodeHeads, hh = head - grp * kDecodeHeads, gg = min(a.g, kDecodeHeads);
-        const int h = unit / a.c.batch, b = unit - h * a.c.batch;
+        const int head = item - unit * a.g, grp = head / kDecodeHeads, hh = head - grp * kDecodeHeads, gg = min(a.g, kDecodeHeads);
         int at, cost, all;                                   // the unit's place and cost, the cost of all units
         if (a.units <= kUnitsPerBlock) {
             long long x = 0;                                 // cost before the unit, and in the upper half of all
-            for (int u = tid; u < a.units; u += kThreads) {
+            for (int u = warp_of_item * 32 + lane; u < a.units; u += kItemWarps * 32) {
                 const int c = cost_of(live_tokens(a, u));
                 x += ((long long)c << 32) + (u < unit ? c : 0);
             }
@@ -583,26 +586,22 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
             __syncthreads();
             x = 0;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) x += sums[w];
+            for (int w = 0; w < kItemWarps; ++w) x += sums[nth * kItemWarps + w];
             at = (int)x; all = (int)(x >> 32); cost = cost_of(live_tokens(a, unit));
             pdl_wait();
         } else {                                             // the first kernel's prefix, so that the many blocks need not scan the many units
             pdl_wait();
             at = a.prefix[unit]; cost = a.prefix[unit + 1] - at; all = a.prefix[a.units];
         }
-        __nv_bfloat16* dst = a.out + b * a.out_seq + (long long)(h * a.g + head) * a.out_head + channel0;
-        float* lse = a.lse != nullptr && channel0 == 0 ? a.lse + (long long)b * (a.c.heads * a.g) + h * a.g + head : nullptr;
-        if (cost == 0) {
-            if (tid < kChannels) dst[tid] = __float2bfloat16_rn(0.f);
-            if (tid == 0 && lse != nullptr) *lse = -INFINITY;
-            return;
-        }
-        const Pieces ps = pieces_of(a, unit, grp, at, cost, all);
-        if (ps.n == 1) return;                               // written by the warp that had it whole (pdl_wait() is behind us)
+        // an empty unit: nothing to add up, which gives a zero row and lse = -inf; a unit of one piece was written by the warp that had it
+        Pieces ps = {0, 0};
+        if (cost > 0) ps = pieces_of(a, unit, grp, at, cost, all);
+        const bool write = item < a.units * a.g && ps.n != 1;
+        if (kItems == 1 && !write) return;
         float m = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int stream = warp * kSplit + lane / kLanes, channel = lane % kLanes * 4;
-        for (int i0 = stream; i0 < ps.n; i0 += kStreams * kJoinBatch) {
+        const int stream = warp_of_item * kSplit + lane / kLanes, channel = lane % kLanes * 4;
+        for (int i0 = stream; write && i0 < ps.n; i0 += kStreams * kJoinBatch) {
             float pm[kJoinBatch], pl[kJoinBatch];
             float4 x[kJoinBatch];
 #pragma unroll
@@ -630,23 +629,29 @@ join_kernel(const __grid_constant__ DecodeArgs a, int mass_blocks) {
                 acc.x += e * x[k].x; acc.y += e * x[k].y; acc.z += e * x[k].z; acc.w += e * x[k].w;
             }
         }
-        *reinterpret_cast<float4*>(&part[stream][channel]) = acc;
-        if (channel == 0) { part_m[stream] = m; part_l[stream] = l; }
+        *reinterpret_cast<float4*>(&part[nth * kStreams + stream][channel]) = acc;
+        if (channel == 0) { part_m[nth * kStreams + stream] = m; part_l[nth * kStreams + stream] = l; }
+        if (lane == 0) to_write[nth] = write;
         __syncthreads();
-        if (tid < kChannels) {
+        for (int i = tid; i < kItems * kChannels; i += kThreads) {
+            const int which = i / kChannels, ch = i % kChannels, first = which * kStreams;
+            if (!to_write[which]) continue;
+            const int pair = (blockIdx.x - mass_blocks) / kSplit * kItems + which, u = pair / a.g;
+            const int h = u / a.c.batch, b = u - h * a.c.batch, q_head = h * a.g + pair - u * a.g;
             float top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kStreams; ++w) top = fmaxf(top, part_m[w]);
+            for (int w = 0; w < kStreams; ++w) top = fmaxf(top, part_m[first + w]);
             const float ref = top == -INFINITY ? 0.f : top;
             float x = 0.f, z = 0.f;
 #pragma unroll
             for (int w = 0; w < kStreams; ++w) {
-                const float e = ex2f(part_m[w] - ref);
-                x += e * part[w][tid];
-                z += e * part_l[w];
+                const float e = ex2f(part_m[first + w] - ref);
+                x += e * part[first + w][ch];
+                z += e * part_l[first + w];
             }
-            dst[tid] = __float2bfloat16_rn(z == 0.f ? 0.f : x / z);
-            if (tid == 0 && lse != nullptr) *lse = z == 0.f ? -INFINITY : kLn2 * (top + log2f(z));
+            a.out[b * a.out_seq + (long long)q_head * a.out_head + channel0 + ch] = __float2bfloat16_rn(z == 0.f ? 0.f : x / z);
+            if (channel0 + ch == 0 && a.lse != nullptr)
+                a.lse[(long long)b * (a.c.heads * a.g) + q_head] = z == 0.f ? -INFINITY : kLn2 * (top + log2f(z));
         }
         return;
     }
@@ -784,19 +789,20 @@ cudaError_t launch_paged_attention(const DecodeArgs& a, int sm_count, cudaStream
     cudaError_t e = allow_smem(kernel, (int)kSmemBytes, done[a.g <= 8 ? 0 : 1]);
     if (e != cudaSuccess) return e;
     if ((e = launch_chained(kPdlOther, kernel, dim3(grid), dim3(kThreads), kSmemBytes, stream, a)) != cudaSuccess) return e;
-    // the second kernel: 16 warps a block and two blocks per (unit, head) where all of them fit the GPU at once, one to an SM; else 8
-    // warps, four blocks to an SM
-    int join_blocks = a.units * a.g;
+    // the second kernel.  Few (unit, head) pairs: 16 warps a block and two blocks per pair, where all of them fit the GPU at once, one to
+    // an SM.  More: 8 warps a block, four blocks to an SM; with few pieces a pair, four pairs a block.
+    const int pairs = a.units * a.g;
     const long long most = a.accumulate ? (long long)a.units * ((a.capacity + kTile - 1) / kTile + kMassUnitCost) : 0;   // cost of the weights
     const long long wanted = (most + kTile - 1) / kTile;     // 256 tokens a block at the least
-    const bool large = 2 * join_blocks <= sm_count;
-    if (large) join_blocks *= 2;
+    const bool large = 2 * pairs <= sm_count, few_pieces = a.workers < 6 * a.units * a.groups;
+    const int join_blocks = large ? 2 * pairs : few_pieces ? (pairs + 3) / 4 : pairs;
     // (not more than fit beside the others, so that those need not wait for a place)
     const int room = large ? max(sm_count / 2, sm_count - join_blocks) : join_blocks <= 2 * sm_count ? 4 * sm_count - join_blocks : 4 * sm_count;
     const int mass_blocks = (int)min(wanted, (long long)room);
     const dim3 blocks(mass_blocks + join_blocks);
-    e = large ? launch_chained(kPdlOther, join_kernel<16>, blocks, dim3(512), 0, stream, a, mass_blocks)
-              : launch_chained(kPdlOther, join_kernel<8>, blocks, dim3(256), 0, stream, a, mass_blocks);
+    e = large        ? launch_chained(kPdlOther, join_kernel<16, 1>, blocks, dim3(512), 0, stream, a, mass_blocks)
+        : few_pieces ? launch_chained(kPdlOther, join_kernel<8, 4>, blocks, dim3(256), 0, stream, a, mass_blocks)
+                     : launch_chained(kPdlOther, join_kernel<8, 1>, blocks, dim3(256), 0, stream, a, mass_blocks);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -769,3 +769,36 @@ def test_the_steps_of_a_decoding_loop_in_one_graph():
     for x, y in zip(a["cache"].tensors, b["cache"].tensors):
         assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
     assert int(a["len"].max()) <= 60 and torch.all(a["len"][:, :, 2] == -1)
+
+
+def test_evict_of_long_and_short_units_and_fill_in_one_graph():
+    # the two launches of an eviction of many ragged units, behind a fill that appends in place: captured, replayed, compared
+    from paper_2507_08143_b200 import binding as B
+    rng = np.random.default_rng(31)
+    lens = rng.integers(100, 400, size=(1, 8, 6)).astype(np.int32)
+    lens[0, :, 0] = 8300
+    lens[0, 3, 1] = 16600
+    host, cache, len_d = make_cache(lens, 32, 5, 31)
+    k, v, _ = _prefill(1, 8, [5] * 6, 3)
+    shape, kd, vd = B.Shape(1, 8, 128, 48, [5] * 6), k.cuda(), v.cuda()
+    budgets = np.maximum(lens - 40, 1)
+    bud, lens0, start = torch.from_numpy(budgets).cuda(), len_d.clone(), [t.clone() for t in cache.tensors]
+
+    def calls():
+        B.paged_fill(cache, shape, kd, vd, [5] * 6, lengths=len_d, lengths_out=len_d)
+        B.paged_evict(cache, len_d, bud, len_d, 16605)
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    want, want_len = po.fill(host, 0, H.bits(k), H.bits(v), [5 * b for b in range(7)], lambda l, h, b: np.arange(5), lengths=lens)
+    want, want_len = po.evict(want, list(np.ndindex(lens.shape)), want_len, budgets)
+    for _ in range(3):
+        for t, s in zip(cache.tensors, start):
+            t.copy_(s)
+        len_d.copy_(lens0)
+        graph.replay()
+        torch.cuda.synchronize()
+        same_bits(pools_of(cache), want, "replay")
+        np.testing.assert_array_equal(len_d.cpu().numpy(), want_len)
