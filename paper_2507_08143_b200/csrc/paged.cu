@@ -474,8 +474,27 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
     if (PART == kEvictShort) pdl_wait();
 }
 
+// How many clusters of `ranks` CTAs run at once on the current device.  Asked once per size and device: CTAs of the large kernel take an SM
+// each, whatever their slice.
+template <typename K>
+int clusters_that_fit(K kernel, cudaLaunchConfig_t cfg, int ranks) {
+    static std::atomic<int> known[64][kMaxCluster + 1];      // 1 more than the number; 0: not asked yet
+    int dev = 0, fit = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return 0;
+    if (const int k = known[dev][ranks].load(std::memory_order_relaxed)) return k - 1;
+    cfg.gridDim = dim3((unsigned)ranks);
+    cfg.dynamicSmemBytes = kLargeSlice * sizeof(uint32_t);
+    if ((ranks > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
+        cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        fit = 0;
+    }
+    known[dev][ranks].store(fit + 1, std::memory_order_relaxed);
+    return fit;
+}
+
 template <int kThreads, int PART>
-cudaError_t launch_evict(const EvictArgs& a, int ranks, int max_length, cudaStream_t stream) {
+cudaError_t launch_evict(const EvictArgs& a, int ranks, int least, int max_length, cudaStream_t stream) {
     const auto kernel = evict_kernel<kThreads, PART>;
     static std::atomic<unsigned long long> done;
     cudaError_t e = allow_smem(kernel, (kThreads == kSmallThreads ? kSmallSlice : kLargeSlice) * (int)sizeof(uint32_t), done);
@@ -489,16 +508,15 @@ cudaError_t launch_evict(const EvictArgs& a, int ranks, int max_length, cudaStre
     cfg.attrs = attr;
     cfg.numAttrs = pdl_enabled(kPdlOther) ? 2 : 1;
     int slice_cap = 0;
-    for (;; ranks -= 2) {
+    for (;; ranks = max(least, ranks - 2)) {
         slice_cap = ((max_length + ranks - 1) / ranks + 31) / 32 * 32;
         cfg.gridDim = dim3((unsigned)(a.units * ranks));
         cfg.dynamicSmemBytes = sizeof(uint32_t) * (size_t)slice_cap;
         attr[0].val.clusterDim.x = ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        if (ranks <= 8) break;
-        int fit = 0;                                         // more than 8 CTAs pay if all units get theirs at once
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-            cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg) == cudaSuccess && fit >= a.units) break;
-        (void)cudaGetLastError();
+        if (ranks <= least) break;
+        // larger clusters than the slices ask for pay only if all units get theirs at once, which the GPU's parts of 16 to 20 SMs may
+        // not allow (16 units of 30000 tokens: 25 us with clusters of 8, of which 14 fit, 17 with clusters of 6)
+        if (clusters_that_fit(kernel, cfg, ranks) >= a.units) break;
     }
     e = cudaLaunchKernelEx(&cfg, kernel, a, slice_cap);
     return e != cudaSuccess ? e : cudaGetLastError();
@@ -532,17 +550,17 @@ cudaError_t launch_paged_evict(const EvictArgs& a, int sm_count, cudaStream_t st
     const int n = a.max_length;
     cudaError_t e;
     if (n <= 8 * kSmallSlice && (long long)a.units * 8 > 2 * sm_count) {
-        if (n <= kSmallSlice) return launch_evict<kSmallThreads, kEvictAll>(a, 1, n, stream);
+        if (n <= kSmallSlice) return launch_evict<kSmallThreads, kEvictAll>(a, 1, 1, n, stream);
         int ranks = 2;
         while (n > ranks * kSmallSlice) ranks *= 2;
-        e = launch_evict<kSmallThreads, kEvictLong>(a, ranks, n, stream);
-        return e != cudaSuccess ? e : launch_evict<kSmallThreads, kEvictShort>(a, 1, kSmallSlice, stream);
+        e = launch_evict<kSmallThreads, kEvictLong>(a, ranks, ranks, n, stream);
+        return e != cudaSuccess ? e : launch_evict<kSmallThreads, kEvictShort>(a, 1, 1, kSmallSlice, stream);
     }
-    int ranks = 1;
-    while ((ranks < 8 && n > (long long)ranks * 12288) ||
-           (ranks < kMaxCluster && (long long)a.units * ranks * 2 <= sm_count && n > 4096LL * ranks))
-        ranks *= 2;
-    return launch_evict<kLargeThreads, kEvictAll>(a, ranks, n, stream);
+    int least = 1;
+    while (least < 8 && n > (long long)least * 12288) least *= 2;
+    int ranks = least;
+    while (ranks < kMaxCluster && (long long)a.units * ranks * 2 <= sm_count && n > 4096LL * ranks) ranks *= 2;
+    return launch_evict<kLargeThreads, kEvictAll>(a, ranks, least, n, stream);
 }
 
 }  // namespace compactor
