@@ -456,8 +456,8 @@ int compactor_paged_fill(const compactor_paged_cache* cache, int32_t first_layer
  *                token (cache->mass) and sets the new token's; otherwise the new token's is set to 0.
  * A unit without tokens (or with a negative length, or beyond its capacity: COMPACTOR_STATUS_CAPACITY) gives zero rows and
  * lse = -inf.  Tokens on a page that is none are left out (COMPACTOR_STATUS_PAGE).
- * Scores and sums are fp32; weights are rounded to bf16 for the product with V only.  Results do not depend on
- * timing: a unit's partial sums are joined in a fixed order.
+ * Scores and sums are fp32; for the product with V a weight is the sum of two bf16 terms (within 2^-16 of it).  Results
+ * do not depend on timing: a unit's partial sums are joined in a fixed order.
  * Workspace: compactor_paged_attention_workspace_bytes(), 256-byte aligned, contents not preserved; 0 = bad arguments.  When
  * accumulating it holds 4 bytes per query head for every token up to max_length (or the table's pages) of every sequence of
  * the layer: keep max_length close to what the units hold.

@@ -15,8 +15,9 @@
 // respectively the channels, as the 16 rows: the 8 columns are the query heads, so nothing of the tile is padding for g = 8
 // and half is for g = 4.  The fifth-generation tensor path has 128 rows per instruction and wants the whole CTA
 // in step; at 4 g flops per 4 bytes it would wait for memory just the same.
-// The online softmax keeps maximum and sum in fp32 (base 2); p is rounded to bf16 for the product with V, which the matrix
-// instruction asks for (at most 2^-8 relative per weight; the sum uses the unrounded values).
+// The online softmax keeps maximum and sum in fp32 (base 2).  For the product with V, whose matrix instruction takes bf16, p enters as two
+// bf16 terms: its upper half and what that leaves out, together within 2^-16 of p (one term, 2^-8, showed where the values
+// cancel: 13 times the error bound of the other roundings).  The second product is eight instructions per tile on a pipe that waits for memory.
 //
 // A second kernel joins the pieces of units that more than one warp worked on and adds the weights: the scores
 // (fp32, 4 g bytes per token) wait in the workspace until the unit's sum is known.
@@ -78,6 +79,16 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t*>(&h);
+}
+// Two weights (0, or 2^-126 .. 1) as two pairs of bf16 terms, hi + lo.  hi is cut off, so lo is not negative, below 2^-7 of its weight's power of
+// two, and rounded by at most 2^-16 of that.  lo is never 0 where the weight is not, so that a weight of an infinite value gives infinity and not
+// 0 * inf in the second product; the least that it is raised to, 2^-126, is where weights end as well.
+__device__ __forceinline__ void split_bf16(float x, float y, uint32_t& hi, uint32_t& lo) {
+    const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
+    const float xl = fmaxf(x - __uint_as_float(xb & 0xffff0000u), fminf(x, 0x1p-126f));
+    const float yl = fmaxf(y - __uint_as_float(yb & 0xffff0000u), fminf(y, 0x1p-126f));
+    hi = __byte_perm(xb, yb, 0x7632);
+    lo = pack_bf16(xl, yl);
 }
 
 // Tokens that a unit attends to, the new one included; 0 for a row without a sequence (negative length) and for a unit
@@ -400,7 +411,7 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
         const int cached = cc.tokens - (a.k_new != nullptr);
         const int ta = base + gid, tb = ta + 8;
         const bool la = ta < cc.tokens && !((bits & 1) && ta < cached), lb = tb < cc.tokens && !((bits & 2) && tb < cached);
-        uint32_t pf[NG][2];
+        uint32_t pf[NG][2], pl[NG][2];                       // weights: first and second term
         bool grew = false;
         float scale_by[NG][2];
 #pragma unroll
@@ -425,10 +436,12 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
                 sum[t][c] = sum[t][c] * scale_by[t][c] + (pa + pb);
                 if (c == 0) { pf[t][0] = __float_as_uint(pa); pf[t][1] = __float_as_uint(pb); }
                 else {
-                    pf[t][0] = transpose8x8(pack_bf16(__uint_as_float(pf[t][0]), pa));
-                    pf[t][1] = transpose8x8(pack_bf16(__uint_as_float(pf[t][1]), pb));
+                    split_bf16(__uint_as_float(pf[t][0]), pa, pf[t][0], pl[t][0]);
+                    split_bf16(__uint_as_float(pf[t][1]), pb, pf[t][1], pl[t][1]);
                 }
             }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { pf[t][i] = transpose8x8(pf[t][i]); pl[t][i] = transpose8x8(pl[t][i]); }
         }
         if (a.accumulate) {                                  // kept until the sum over the whole unit is known
             float* col = a.scores + ((long long)cc.unit * a.g + cc.grp * kDecodeHeads + 2 * tig) * a.unit_rows + base + gid;
@@ -458,7 +471,10 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
                 uint32_t vf[4];
                 ldsm4t(vf, (vs + v_frag) ^ (j << 5));
 #pragma unroll
-                for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pf[t][0], pf[t][1]);
+                for (int t = 0; t < NG; ++t) {
+                    mma(o[t][j], vf, pf[t][0], pf[t][1]);
+                    mma(o[t][j], vf, pl[t][0], pl[t][1]);
+                }
             }
         }
         // the new token's row goes from the ring to its page
