@@ -399,6 +399,12 @@ class PagedCache:
         self._device = self.device.index if self.device.type == "cuda" else -1
 
 
+def _expect(x, kind: type, name: str) -> None:
+    """The compiled calls take structs by address: whose they are is settled here."""
+    if not isinstance(x, kind):
+        raise TypeError(f"{name}: a {kind.__name__} is expected")
+
+
 def paged_fill(cache: PagedCache, shape: Shape, k_cache: torch.Tensor, v_cache: torch.Tensor, keep_counts: Sequence[int],
                idx: Optional[torch.Tensor] = None, head_offsets: Optional[torch.Tensor] = None,
                mass_in: Optional[torch.Tensor] = None, first_position: Optional[torch.Tensor] = None,
@@ -406,6 +412,8 @@ def paged_fill(cache: PagedCache, shape: Shape, k_cache: torch.Tensor, v_cache: 
                status: Optional[torch.Tensor] = None) -> None:
     """Compaction into pages: the kept rows (`idx`, and `head_offsets` after a selection across heads; without `idx` the first
     keep_counts[b] rows of every sequence) of k_cache / v_cache [layers, heads, tokens, d] go behind `lengths`."""
+    _expect(cache, PagedCache, "cache")
+    _expect(shape, Shape, "shape")
     _check(_fastcall.fill(cache._address, cache._device, first_layer, ctypes.addressof(shape.c), k_cache, v_cache, keep_counts, idx,
                           head_offsets, mass_in, first_position, lengths, lengths_out, status), "compactor_paged_fill")
 
@@ -416,6 +424,8 @@ def decode_options(q_per_kv: int, max_length: int, scale: float = 128 ** -0.5, s
 
 
 def paged_attention_workspace_bytes(cache: PagedCache, opt: CompactorDecodeOptions) -> int:
+    _expect(cache, PagedCache, "cache")
+    _expect(opt, CompactorDecodeOptions, "opt")
     return int(LIB.compactor_paged_attention_workspace_bytes(byref(cache.c), byref(opt)))
 
 
@@ -429,6 +439,8 @@ def paged_attention(cache: PagedCache, layer: int, opt: CompactorDecodeOptions, 
                     lse_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
     """Attention of one new token per sequence: q, out [batch, heads * q_per_kv, d], k_new, v_new [batch, heads, d],
     lse_out fp32 [batch, heads * q_per_kv]; `lengths` [layers, heads, batch] without the new token, left as it is."""
+    _expect(cache, PagedCache, "cache")
+    _expect(opt, CompactorDecodeOptions, "opt")
     _check(_fastcall.attention(cache._address, cache._device, layer, ctypes.addressof(opt), q, lengths, out, workspace, k_new, v_new,
                                new_positions, lse_out, status), "compactor_paged_attention")
 
@@ -438,6 +450,7 @@ def paged_evict(cache: PagedCache, lengths: torch.Tensor, budgets: torch.Tensor,
                 status: Optional[torch.Tensor] = None) -> None:
     """Evicts every unit that holds more than its budget down to it: the `recent` newest tokens and those of the greatest
     accumulated weight stay.  lengths, budgets, lengths_out: int32 [layers, heads, batch]; lengths_out may be lengths."""
+    _expect(cache, PagedCache, "cache")
     _check(_fastcall.evict(cache._address, cache._device, first_layer, cache.layers - first_layer if layers is None else layers, lengths,
                            budgets, next_position, recent, max_length, lengths_out, status), "compactor_paged_evict")
 
