@@ -4,10 +4,12 @@
 Function names mirror the C entry points of `include/compactor.h`.  Device buffers are torch
 CUDA tensors (torch is used for device memory and streams, nothing else); every step of the
 path runs in the library's kernels.  Importing this module fails loudly if the library cannot
-be built or loaded - there is no fallback."""
+be built or loaded, the paged calls do if `_fastcall` cannot - there is no fallback."""
 from __future__ import annotations
 
 import ctypes
+import importlib.util
+import subprocess
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 from typing import Optional, Sequence
 
@@ -115,10 +117,32 @@ def _load() -> ctypes.CDLL:
 LIB = _load()
 LIB_PATH = _build.LIB
 
-from . import _fastcall  # noqa: E402  (built with the library)
 
-_fastcall.bind(*[ctypes.cast(f, c_void_p).value for f in (LIB.compactor_paged_fill, LIB.compactor_paged_attention,
-                                                         LIB.compactor_paged_evict)])
+def _load_fastcall():
+    path = _build.build_fastcall()
+    spec = importlib.util.spec_from_file_location(f"{__package__}._fastcall", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    module.bind(*[ctypes.cast(f, c_void_p).value for f in (LIB.compactor_paged_fill, LIB.compactor_paged_attention,
+                                                          LIB.compactor_paged_evict)])
+    return module
+
+
+class _NoFastcall:
+    """In the place of the compiled checks where they can be neither built nor loaded: the paged calls say so, everything
+    else needs only ctypes."""
+
+    def __init__(self, cause: Exception):
+        self._cause = cause
+
+    def __getattr__(self, name):
+        raise RuntimeError("the paged calls need their compiled argument checks, which could not be built or loaded") from self._cause
+
+
+try:
+    _fastcall = _load_fastcall()
+except (OSError, ImportError, subprocess.CalledProcessError) as e:
+    _fastcall = _NoFastcall(e)
 
 EXPORTS = ["compactor_version", "compactor_error_string", "compactor_make_sketch", "compactor_make_sketch_srht", "compactor_keep_count",
            "compactor_calibrated_ratio", "compactor_fit_calibration", "compactor_workspace_bytes", "compactor_score", "compactor_select",
