@@ -418,8 +418,8 @@ typedef struct compactor_rows {
  *   shape         the prefill (heads and batch those of the cache); its layers go to the cache's layers
  *                 first_layer .. first_layer + shape->layers - 1.  m is not used (any valid value).
  *   idx           device int32 in the layout of compactor_select, or of compactor_select_across_heads when
- *                 head_offsets is given; NULL (without head_offsets): rows 0 .. keep_counts[b] - 1 of every
- *                 sequence, i.e. the tokens are appended as they are.
+ *                 head_offsets is given; NULL (without head_offsets, or where nothing is kept): rows 0 .. keep_counts[b] - 1
+ *                 of every sequence, i.e. the tokens are appended as they are.
  *   head_offsets  device int32 [shape->layers][batch][heads + 1] from compactor_select_across_heads, or NULL.
  *   keep_counts   HOST int32 [batch], as in compactor_compact.
  *   mass_in       device fp32 [shape->layers][heads][total_tokens] (the attention term of Eq. 5 without

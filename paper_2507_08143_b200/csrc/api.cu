@@ -1159,7 +1159,7 @@ extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t 
     int err = 0;
     if (!cache_ok(cache, &err) || !shape_ok(shape, &err)) return err;
     const bool some = shape->cu_seqlens[shape->batch] > 0;               // without tokens there is nothing to point to
-    if ((some && (!mat_ok(k_cache) || !mat_ok(v_cache))) || keep_counts == nullptr || (head_offsets != nullptr && idx == nullptr) ||
+    if ((some && (!mat_ok(k_cache) || !mat_ok(v_cache))) || keep_counts == nullptr ||
         shape->heads != cache->heads || shape->batch != cache->batch || first_layer < 0 ||
         first_layer > cache->layers - shape->layers)
         return COMPACTOR_E_INVALID_ARGUMENT;
@@ -1169,6 +1169,7 @@ extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t 
         kept += keep_counts[b];
     }
     if (kept * shape->heads > 0x7fffffffLL) return COMPACTOR_E_INVALID_ARGUMENT;
+    if (head_offsets != nullptr && idx == nullptr && kept > 0) return COMPACTOR_E_INVALID_ARGUMENT;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     FillArgs a;
     memset(&a, 0, sizeof(a));

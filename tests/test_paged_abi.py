@@ -216,3 +216,9 @@ def test_oracle_evict_pins():
     assert [int(after["positions"][at[t]]) for t in range(6)] == [12, 14, 17, 18, 19, 5]
     after, out = po.evict(c, [unit], n, np.array([[[20]]], np.int32))
     assert out[unit] == 20 and all(np.array_equal(after[k], c[k]) for k in c)
+
+
+def test_fill_of_nothing_across_heads():
+    """Where no sequence keeps a row, a selection across heads has no indices: an empty tensor, whose address is null."""
+    assert _fill(idx=None, offs=1 << 14, keep=(0, 0, 0)) == 0
+    assert _fill(idx=None, offs=1 << 14, keep=(0, 0, 1)) == -1
