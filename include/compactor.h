@@ -450,7 +450,8 @@ int compactor_paged_fill(const compactor_paged_cache* cache, int32_t first_layer
  *                changed: all layers of a step see the same lengths, the caller adds 1 after the last.
  *   lengths      device int32 [units of the cache]: cached tokens, without the new one.
  *   lse_out      device fp32 [batch][heads * q_per_kv] or NULL.
- *   options (HOST): q_per_kv, scale (> 0), softcap (0: none), accumulate, and max_length, the most tokens a unit may have
+ *   options (HOST): q_per_kv, scale (> 0), softcap (0: none; scale log2(e), scale / softcap and softcap log2(e) have to be normal fp32
+ *                numbers), accumulate, and max_length, the most tokens a unit may have
  *                in this call, the new one included (what lies beyond the table's pages does not count).
  *                accumulate != 0 adds sum over the KV head's query heads of p_j to the weight of every cached
  *                token (cache->mass) and sets the new token's; otherwise the new token's is set to 0.

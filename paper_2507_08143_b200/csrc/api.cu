@@ -1132,6 +1132,9 @@ bool decode_layout(const compactor_paged_cache* c, const compactor_decode_option
     *err = COMPACTOR_E_INVALID_ARGUMENT;
     if (o == nullptr || o->q_per_kv < 1 || o->max_length < 1 || !(o->scale > 0.f) || !isfinite(o->scale) ||
         !(o->softcap >= 0.f) || !isfinite(o->softcap)) return false;
+    // what the kernel makes of the two (in fp32) has to be a normal number
+    constexpr float kLog2e = 1.4426950408889634f;
+    if (!isnormal(o->scale * kLog2e) || (o->softcap > 0.f && (!isnormal(o->scale / o->softcap) || !isnormal(o->softcap * kLog2e)))) return false;
     if (o->q_per_kv > kMaxQPerKv) { *err = COMPACTOR_E_UNSUPPORTED; return false; }
     if (o->accumulate != 0 && c->mass == nullptr) return false;
     const long long units = (long long)c->heads * c->batch;

@@ -222,3 +222,13 @@ def test_fill_of_nothing_across_heads():
     """Where no sequence keeps a row, a selection across heads has no indices: an empty tensor, whose address is null."""
     assert _fill(idx=None, offs=1 << 14, keep=(0, 0, 0)) == 0
     assert _fill(idx=None, offs=1 << 14, keep=(0, 0, 1)) == -1
+
+
+def test_attention_refuses_scales_that_leave_fp32():
+    """The kernel works with scale log2(e), scale / softcap and softcap log2(e): one of them infinite gives inf * 0, one of them
+    below the normal numbers loses the scores' bits."""
+    fine = _attention(opt=B.decode_options(2, 100, scale=1e30, softcap=1e30), ws_bytes=256)
+    assert fine == -3 and _attention(opt=B.decode_options(2, 100, scale=1e-30, softcap=1e-30), ws_bytes=256) == -3
+    for scale, softcap in ((3e38, 0.0), (1e-39, 0.0), (1.0, 1e-39), (1.0, 3e38), (1e-20, 1e20), (1e20, 1e-20)):
+        assert _attention(opt=B.decode_options(2, 100, scale=scale, softcap=softcap), ws_bytes=256) == -1, (scale, softcap)
+        assert B.LIB.compactor_paged_attention_workspace_bytes(ctypes.byref(_cache()), ctypes.byref(B.decode_options(2, 100, scale=scale, softcap=softcap))) == 0
