@@ -233,7 +233,7 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
     };
     const int slice = ((n + ranks - 1) / ranks + 31) / 32 * 32;              // at most slice_cap
     const int lo = min(n, rank * slice), count = min(n, lo + slice) - lo;
-    const int recent_from = a.recent > 0 ? load<L2>(a.next_position + unit % a.c.batch) - min(a.recent, budget) : 0;
+    const int recent_from = a.recent > 0 ? (int)max((long long)load<L2>(a.next_position + unit % a.c.batch) - min(a.recent, budget), -0x80000000LL) : 0;
 
     if (tid == 0) s.bad = 0;
     for (int i = tid; i < 2 * kBins / 4; i += kThreads) reinterpret_cast<int4*>(s.hist)[i] = make_int4(0, 0, 0, 0);

@@ -19,3 +19,15 @@ def test_fill_of_nothing_across_heads():
                  head_offsets=torch.zeros(1, 2, 3, dtype=torch.int32, device="cuda"), lengths=len_d, lengths_out=out, status=st)
     assert torch.equal(out, len_d) and not st.any()
     same_bits(pools_of(cache), before, "nothing")
+
+
+def test_evict_window_that_begins_below_the_least_position():
+    """next_position - recent below -2^31: every token is recent, so the lowest slots stay and nothing moves."""
+    from paper_2507_08143_b200 import binding as B
+    _, cache, len_d = make_cache([[[50]]], 16, 0, 3)
+    before = pools_of(cache)
+    out, budgets = torch.zeros_like(len_d), torch.full_like(len_d, 20)
+    nxt = torch.tensor([-2 ** 31 + 5], dtype=torch.int32, device="cuda")
+    B.paged_evict(cache, len_d, budgets, out, 50, recent=10, next_position=nxt)
+    assert int(out) == 20
+    same_bits(pools_of(cache), before, "nothing moves")
