@@ -474,10 +474,11 @@ evict_kernel(const __grid_constant__ EvictArgs a, int slice_cap) {
     if (PART == kEvictShort) pdl_wait();
 }
 
-// How many clusters of `ranks` CTAs run at once on the current device.  Asked once per size and device: CTAs of the large kernel take an SM
-// each, whatever their slice.
-template <typename K>
-int clusters_that_fit(K kernel, cudaLaunchConfig_t cfg, int ranks) {
+// How many clusters of `ranks` CTAs of the kernel run at once on the current device.  Asked once per kernel, size and device: CTAs of the
+// large kernel take an SM each, whatever their slice.
+template <int kThreads, int PART>
+int clusters_that_fit(cudaLaunchConfig_t cfg, int ranks) {
+    const auto kernel = evict_kernel<kThreads, PART>;
     static std::atomic<int> known[64][kMaxCluster + 1];      // 1 more than the number; 0: not asked yet
     int dev = 0, fit = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return 0;
@@ -516,7 +517,7 @@ cudaError_t launch_evict(const EvictArgs& a, int ranks, int least, int max_lengt
         if (ranks <= least) break;
         // larger clusters than the slices ask for pay only if all units get theirs at once, which the GPU's parts of 16 to 20 SMs may
         // not allow (16 units of 30000 tokens: 25 us with clusters of 8, of which 14 fit, 17 with clusters of 6)
-        if (clusters_that_fit(kernel, cfg, ranks) >= a.units) break;
+        if (clusters_that_fit<kThreads, PART>(cfg, ranks) >= a.units) break;
     }
     e = cudaLaunchKernelEx(&cfg, kernel, a, slice_cap);
     return e != cudaSuccess ? e : cudaGetLastError();
