@@ -471,10 +471,9 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
                 uint32_t vf[4];
                 ldsm4t(vf, (vs + v_frag) ^ (j << 5));
 #pragma unroll
-                for (int t = 0; t < NG; ++t) {
-                    mma(o[t][j], vf, pf[t][0], pf[t][1]);
-                    mma(o[t][j], vf, pl[t][0], pl[t][1]);
-                }
+                for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pf[t][0], pf[t][1]);
+#pragma unroll
+                for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pl[t][0], pl[t][1]);
             }
         }
         // the new token's row goes from the ring to its page
