@@ -51,7 +51,7 @@ extern "C" {
 
 #define COMPACTOR_OK                  0
 #define COMPACTOR_E_INVALID_ARGUMENT -1   /* null pointer, bad size, bad stride or alignment      */
-#define COMPACTOR_E_UNSUPPORTED      -2   /* d != 128 or m outside [1, 128]                      */
+#define COMPACTOR_E_UNSUPPORTED      -2   /* d != 128, m outside [1, 128], more than 64 query heads per KV head */
 #define COMPACTOR_E_WORKSPACE        -3   /* workspace smaller than compactor_workspace_bytes()  */
 #define COMPACTOR_E_CUDA             -4   /* a CUDA runtime call failed (see cudaGetLastError)   */
 #define COMPACTOR_E_TOO_LARGE        -5   /* problem exceeds the library's built-in scratch      */
@@ -456,7 +456,8 @@ int compactor_paged_fill(const compactor_paged_cache* cache, int32_t first_layer
  *                accumulate != 0 adds sum over the KV head's query heads of p_j to the weight of every cached
  *                token (cache->mass) and sets the new token's; otherwise the new token's is set to 0.
  * A unit without tokens (or with a negative length, or beyond its capacity: COMPACTOR_STATUS_CAPACITY) gives zero rows and
- * lse = -inf.  Tokens on a page that is none are left out (COMPACTOR_STATUS_PAGE).
+ * lse = -inf.  Cached tokens on a page that is none are left out (COMPACTOR_STATUS_PAGE); the new token is attended to
+ * whatever its page, and not written where that is none (COMPACTOR_STATUS_PAGE).
  * Scores and sums are fp32; for the product with V a weight is the sum of two bf16 terms (within 2^-16 of it).  Results
  * do not depend on timing: a unit's partial sums are joined in a fixed order.
  * Workspace: compactor_paged_attention_workspace_bytes(), 256-byte aligned, contents not preserved; 0 = bad arguments.  When
@@ -485,9 +486,12 @@ int compactor_paged_attention(const compactor_paged_cache* cache, int32_t layer,
  * behind: the j-th evicted slot below B receives row, weight and position of the j-th kept slot at or above B.  Slots
  * from B on keep what they hold.  lengths_out[u] (may be `lengths`, not `budgets`; the entries of other layers are left alone) becomes B.
  * A unit with n <= B, a negative length or a negative budget stays as it is, lengths_out[u] = lengths[u]; so does one with
- * n > max_length or beyond its pages (COMPACTOR_STATUS_CAPACITY) and one with a page that is none (COMPACTOR_STATUS_PAGE).
+ * n > max_length or beyond its pages (COMPACTOR_STATUS_CAPACITY) and one with a page that is none (COMPACTOR_STATUS_PAGE;
+ * with B = 0 no page is looked at and the length becomes 0).
  *   next_position  device int32 [batch]; may be NULL when recent = 0.
- *   max_length     the most tokens a unit may have, at most 393216 (COMPACTOR_E_TOO_LARGE beyond).
+ *   max_length     the most tokens a unit may have, at most 393216 (COMPACTOR_E_TOO_LARGE beyond).  It decides how the work is laid
+ *                  out (what lies beyond the table's pages does not count): keep it close to what the units hold, and below 66048 where
+ *                  none needs more.  256 units of 2459 tokens take 9 us, 14 with a bound of 66048 and 50 with one of 131072.
  * cache->mass is required, cache->positions when recent > 0.  No workspace.
  */
 int compactor_paged_evict(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* lengths,

@@ -22,9 +22,11 @@
 // A second kernel joins the pieces of units that more than one warp worked on and adds the weights: the scores
 // (fp32, 4 g bytes per token) wait in the workspace until the unit's sum is known.
 //
-// Measured (both kernels, one layer, device time of calls in a row): 8 heads x 131072 tokens, g = 5: 90 us = 5.96 TB/s, 0.91 of the copy
-// rate; 8 heads x 16 ragged sequences (152 K tokens), g = 4, with weights: 120 us = 5.3 TB/s; 8 heads x 2458 tokens: 12.7 us, of which
-// 6.4 are the first kernel's chain (lengths, page ids, rows, one or two tiles, results) and 4 the second's.
+// Measured (both kernels, one layer, device time of calls in a row): 8 heads x 131072 tokens, g = 5: 89.3 us = 6.0 TB/s, 0.92 of the copy
+// rate; 8 heads x 16 ragged sequences (152 K tokens), g = 4, with weights: 118 us = 5.4 TB/s; 8 heads x 2458 tokens, g = 4, with
+// weights: 10.9 us, the chains of two kernels (lengths, page ids, rows, one or two tiles, results; results, scores, weights).
+// More than 16 query heads per KV head are served 16 at a time, and every 16 read the unit's rows again: 8 heads x 131072 tokens
+// 98 us for g = 16, 172 for 32, 326 for 64.
 #include "paged.cuh"
 
 namespace compactor {
@@ -39,7 +41,7 @@ constexpr int kStageBytes = 2 * kTile * kRowBytes;     // K tile, V tile
 constexpr size_t kSmemBytes = (size_t)kWarps * kStages * kStageBytes;
 constexpr int kUnitCost = kDecodeUnitCost;
 constexpr int kMassUnitCost = kDecodeMassUnitCost;
-constexpr int kUnitsPerBlock = 1024;                   // most units that every block of the second kernel scans
+constexpr int kUnitsPerBlock = 1024;                   // most units that every joining block scans (a block of the weights scans them all, however many)
 constexpr int kUnitsInSmem = 2048;                     // units whose token counts every CTA keeps at hand
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -102,7 +104,7 @@ __device__ __forceinline__ int live_tokens(const DecodeArgs& a, int unit) {
 __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + kTile - 1) / kTile; }
 // What a (unit, group) counts for when the work is shared out: its tiles and kUnitCost more, since a warp that enters
 // a unit waits for its queries, page ids and row of results (with 0 the warps that got many short units of a padded batch ended
-// last: 32 against 20 us).
+// last: the first kernel took 36 us instead of 22).
 __device__ __forceinline__ int cost_of(int tokens) { return tokens == 0 ? 0 : tiles_of(tokens) + kUnitCost; }
 
 // `total` cost shared by `workers`: the first total % workers get one more than the others.
@@ -117,8 +119,8 @@ struct Share {
     }
 };
 // Warps that share the work.  Where each gets many tiles one warp of a CTA stays out: with seven warps of two stages 112 KB are on
-// their way to an SM, enough for its share of HBM; more of them disturb each other (131072 tokens: 90.0 us with seven warps, 93.4 with
-// eight, 96 with eight of three stages, 90.7 with six).  With few tiles all eight are wanted (padded batch: 34.9 against 36.7 us).
+// their way to an SM, enough for its share of HBM; more of them disturb each other (131072 tokens: 88.9 us with seven warps, 89.1
+// with eight, 96.4 with eight of three stages, 90.1 with six).  With few tiles all eight are wanted (padded batch: 31.8 against 33.1 us).
 __device__ __forceinline__ int active_workers(const DecodeArgs& a, int total) {
     return total / 16 >= a.workers ? a.workers / kWarps * (kWarps - 1) : min(a.workers, total);
 }
@@ -385,8 +387,8 @@ decode_kernel(const __grid_constant__ DecodeArgs a) {
                 sum[t][0] = sum[t][1] = 0.f;
             }
         }
-        // the second kernel's blocks are let in when the tiles run out: blocks that wait beside this kernel slow it (51 -> 57 us for 8
-        // sequences x 4 heads x 7 queries)
+        // the second kernel's blocks are let in when the tiles run out: let in at the start they gain nothing (47.7 us either way for 8
+        // sequences x 4 heads x 7 queries) and hold registers of every SM all the while
         if (left_c <= kStages) pdl_trigger();
         cp_wait<kStages - 1>();
         __syncwarp();

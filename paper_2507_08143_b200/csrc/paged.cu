@@ -13,11 +13,11 @@ namespace {
 // Where a row goes: slot lengths[unit] + j of its unit, j its place among the unit's kept rows, found through the page table.  A block
 // moves 128 rows: first a thread per row finds source and target (index, length and page id are three dependent reads,
 // made once per row and not once per 16-byte piece) and moves weight and position, then 16 threads per row move K and V.
-// Bound by HBM: 512 bytes read and written per row.  256 units x 2458 of 8192 rows: 111 us = 5.9 TB/s, 0.90 of the copy rate.
+// Bound by HBM: 512 bytes read and written per row.  256 units x 2458 of 8192 rows: 109 us = 6.0 TB/s, 0.92 of the copy rate.
 constexpr int kFillThreads = 256;
 constexpr int kFillRows = 128;
 constexpr int kFillRowsPerIter = kFillThreads / 16;
-constexpr int kFillBatch = 4;                   // rows per thread in flight (2: 116 us instead of 113 for 32 x 8 heads x 2458 rows)
+constexpr int kFillBatch = 4;                   // rows per thread in flight (2: 112.6 us instead of 111.0 for 32 x 8 heads x 2458 rows)
 
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
     uint4 v;
@@ -148,11 +148,14 @@ fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTabl
 //      would rewrite nearly the whole unit for one evicted token.
 // The bytes are few (8 per slot, 1 KB per moved row); what bounds it is the chain of block-wide steps, about 8 us per unit
 // whatever its length.  So several small CTAs share an SM and hide each other's waits.  One token out of each of 256 units of 2459:
-// 9.5 us; 128 out of 512 ragged units of 9 K on average: 46 us; 8192 out of 8 units of 50136: 33 us.
+// 8.6 us; 128 out of 512 ragged units of 9 K on average: 49 us; 8192 out of 8 units of 50136: 35 us.
 constexpr int kBins = 2048;
 constexpr int kMaxCluster = 16;                 // 8 is what every launch may use
 constexpr int kSmallThreads = 256, kLargeThreads = 512;
-constexpr int kSmallSlice = 8256, kLargeSlice = 49152;   // most slots per CTA: 33 KB of keys, four CTAs to an SM; 192 KB, one
+// Most slots per CTA: 33 KB of keys, four CTAs to an SM; 192 KB, one.  The smaller is 8192 and a little more, so that a budget that is a power of
+// two and a block of a few hundred tokens behind it need clusters of the budget's size (512 ragged units of up to 32896 tokens, 128 of them
+// new: 49 us, with slices of 8192 53, of 9216 49).
+constexpr int kSmallSlice = 8256, kLargeSlice = 49152;
 constexpr int kLoadBatch = 8;                   // groups of four slots per thread whose weights are in flight together
 constexpr uint32_t kKeyRecent = 0xffffffffu, kKeyNan = 0xfffffffeu;
 
@@ -516,7 +519,7 @@ cudaError_t launch_evict(const EvictArgs& a, int ranks, int least, int max_lengt
         attr[0].val.clusterDim.x = ranks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         if (ranks <= least) break;
         // larger clusters than the slices ask for pay only if all units get theirs at once, which the GPU's parts of 16 to 20 SMs may
-        // not allow (16 units of 30000 tokens: 25 us with clusters of 8, of which 14 fit, 17 with clusters of 6)
+        // not allow (16 units of 40400 tokens: 27.7 us with clusters of 8, of which not all fit, 18.5 with the largest that do)
         if (clusters_that_fit<kThreads, PART>(cfg, ranks) >= a.units) break;
     }
     e = cudaLaunchKernelEx(&cfg, kernel, a, slice_cap);
@@ -546,9 +549,11 @@ int evict_max_tokens() { return 8 * kLargeSlice; }
 cudaError_t launch_paged_evict(const EvictArgs& a, int sm_count, cudaStream_t stream) {
     // Many units: CTAs of 256 threads, four to an SM; where some units may need several CTAs, those go in a launch of clusters, the others
     // in one of single CTAs beside it (one launch of clusters for all left most of their CTAs without work: 128 of 512 ragged
-    // units of up to 32768 tokens 57 us against 45).  Few units or very long ones: CTAs of 512 threads, more of them per unit while
-    // the GPU is not full and a slice still has 4096 slots (with 2048: 8 units of 5000 tokens 15.7 us against 13.4, 2 of 49169 19.5 against
-    // 17.5; with 8192: 8 units of 50136 52 us against 35).
+    // units of up to 32768 tokens 56 us against 49).  Few units or very long ones: CTAs of 512 threads, more of them per unit while
+    // the GPU is not full and a slice still has 4096 slots (with 2048: 8 units of 5000 tokens 14.1 us against 12.1, 2 of 49169 17.8 against
+    // 15.9; with 8192: 8 units of 20000 16.0 us against 14.0, 32 of 20000 17.4 against 16.0, though 32 of 12000 15 against 16).  `least` is
+    // where the search for a cluster that fits ends: slices of at most 12288 slots up to clusters of eight (of 6144: 16 units of 30000 tokens
+    // 25.6 us against 16.3, since clusters of eight do not all fit; of 24576: no difference in any case tried).
     const int n = a.max_length;
     cudaError_t e;
     if (n <= 8 * kSmallSlice && (long long)a.units * 8 > 2 * sm_count) {
