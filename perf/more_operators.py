@@ -10,8 +10,8 @@ They stand before, in and beside the paged cache that a compressed prefill is de
   sparse   pages chosen for the step's queries by those bounds, and the attention over the chosen ones alone
 
 A row of 128 channels in 4 bits is 80 bytes: for each group of 32 channels the least value `lo` (bf16) and a step s = (greatest -
-least) / 15, rounded up to four significant bits; a channel is the whole number c nearest to (x - lo) / s and stands for
-lo + s c.  All of these operators are bound by memory; `work` counts every byte that has to be touched once."""
+least) / 15, rounded up to four significant bits; a channel is the whole number c nearest to (x - lo) / s (the lower of two)
+and stands for lo + s c.  All of these operators are bound by memory; `work` counts every byte that has to be touched once."""
 import math
 import random
 
@@ -132,8 +132,9 @@ def _quantise(x):
     lo, hi = xg.amin(-1, keepdim=True), xg.amax(-1, keepdim=True)
     s = (hi - lo) / torch.full_like(hi, 15)                                     # (by a number it would be a product with 1 / 15)
     s = ((s.view(torch.int32) + 0xFFFFF) & ~0xFFFFF).view(torch.float32)          # up to four significant bits
+    s = s.masked_fill(s < 2.0 ** -120, 0.0)
     bad = ~(torch.isfinite(xg).all(-1, keepdim=True) & (s <= 2.0 ** 120))
-    c = torch.where(s > 0, torch.round((xg - lo) / s), 0.0)
+    c = torch.where(s > 0, torch.ceil((xg - lo) / s - 0.5), 0.0)
     c = torch.where(bad, 0.0, c).clamp(0, 15).to(torch.uint8).flatten(-2)
     params = torch.cat([s, lo], -1).masked_fill(bad, math.nan).bfloat16().flatten(-2)
     return torch.cat([c[..., 0::2] | (c[..., 1::2] << 4), params.view(torch.uint8)], -1)
@@ -442,7 +443,7 @@ def _held64(x):
     step = torch.div(x.max(-1, keepdim=True).values - lo, torch.full_like(lo, 15))
     m, e = torch.frexp(step)                                                    # step = m 2^e, 1/2 <= m < 1
     step = torch.ldexp(torch.ceil(m * 16) / 16, e)
-    c = torch.where(step > 0, torch.round((x - lo) / step), torch.zeros_like(x))
+    c = torch.where(step > 0, torch.ceil((x - lo) / step - 0.5), torch.zeros_like(x))
     return (lo + c * step).view(-1, D)
 
 
