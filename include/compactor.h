@@ -499,6 +499,125 @@ int compactor_paged_evict(const compactor_paged_cache* cache, int32_t first_laye
                           int32_t* lengths_out, int32_t* status, void* stream);
 
 /*
+ * The same cache with rows held in 4 bits.  A row of 128 channels takes 80 bytes instead of 256: 64 bytes of codes (channel 2 j in the low
+ * half of byte j, 2 j + 1 in the high half), then for each group of 32 channels, in order, two bf16: a step s and the least value lo.  A
+ * channel of code c stands for lo + s c.  With `least` and `greatest` of the group's 32 values
+ *   s = (greatest - least) / 15 rounded up to four significant bits (0 if that is below 2^-120),  lo = least,
+ *   c = ceil((x - lo) / s - 1/2), 0 where s is 0: the nearest code, the lower of two as near, at most s / 2 off (the differences are fp32's);
+ * a group with a value that is not finite, or whose step exceeds 2^120, is held as not a number throughout.
+ * The compactor_paged4_ calls take a compactor_paged_cache whose pools are such rows: k_pages and v_pages 16-byte aligned,
+ * stride_token = 80 (the rows of a page lie back to back) and stride_page, both in BYTES, stride_page a multiple of 16 and at least 80 page_tokens.
+ * A cache of one kind is refused by the calls for the other.  Everything else is as in the calls without the 4:
+ *   paged4_fill       holds the rows as above instead of copying them;
+ *   paged4_attention  attends to the values that the rows stand for.  The new token's row is held in 4 bits first and attended to as it is
+ *                     held, so that later steps see the same.  Its products are exact before they are summed in fp32; weights enter
+ *                     the product with V as two bf16 terms (within 2^-16 of the weight).  Its workspace has a size of its own;
+ *   paged4_evict      moves rows as they are.
+ */
+int compactor_paged4_fill(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape,
+                          compactor_mat k_cache, compactor_mat v_cache, const int32_t* idx,
+                          const int32_t* head_offsets, const int32_t* keep_counts, const float* mass_in,
+                          const int32_t* first_position, const int32_t* lengths, int32_t* lengths_out,
+                          int32_t* status, void* stream);
+size_t compactor_paged4_attention_workspace_bytes(const compactor_paged_cache* cache, const compactor_decode_options* options);
+int compactor_paged4_attention(const compactor_paged_cache* cache, int32_t layer, const compactor_decode_options* options,
+                               compactor_rows q, compactor_rows k_new, compactor_rows v_new, const int32_t* new_positions,
+                               const int32_t* lengths, compactor_rows out, float* lse_out, int32_t* status,
+                               void* workspace, size_t workspace_bytes, void* stream);
+int compactor_paged4_evict(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* lengths,
+                           const int32_t* budgets, const int32_t* next_position, int32_t recent, int32_t max_length,
+                           int32_t* lengths_out, int32_t* status, void* stream);
+
+/*
+ * Rows out of the pages into dense tensors, the counterpart of the fill: row cu_seqlens[b] + j of (layer, head) becomes token
+ * first[u] + j of its unit, for 0 <= j < length of sequence b in `shape` and first[u] + j < lengths[u].  Other rows keep what they hold.
+ *   shape          the dense tensors' (heads and batch those of the cache); its layers are the cache's from first_layer on.  m is not used.
+ *   first          device int32 [units of the cache] or NULL (0); a unit with a negative entry is left out.
+ *   lengths        device int32 [units of the cache]; a unit with a negative length, or one beyond its pages (COMPACTOR_STATUS_CAPACITY), is left out.
+ *   k_out, v_out   bf16 [layers][heads][total tokens][d], strides as for inputs, rows that do not overlap.  From a cache in 4 bits come the
+ *                  nearest bf16 to the values that the rows stand for.
+ * Rows on a page that is none are left alone (COMPACTOR_STATUS_PAGE).  No workspace.
+ */
+int compactor_paged_read(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape, const int32_t* first,
+                         const int32_t* lengths, compactor_mat k_out, compactor_mat v_out, int32_t* status, void* stream);
+int compactor_paged4_read(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape, const int32_t* first,
+                          const int32_t* lengths, compactor_mat k_out, compactor_mat v_out, int32_t* status, void* stream);
+
+/*
+ * Attention to a few pages of every unit, chosen for each step's queries: compactor_paged_bounds keeps the least and the greatest key of every
+ * page, channel by channel; compactor_paged_select scores the pages by them and writes the best as a page table of one layer, which the
+ * attention calls take in the place of the cache's own (layers = 1, max_pages = pages, layer 0, the lengths written here).
+ *   bounds         device bf16 [n_pages][2][d], 16-byte aligned: least values, then greatest, of the keys of the page's tokens (of a cache in 4 bits:
+ *                  of what they stand for, rounded to bf16).  Not-a-number in a channel gives not-a-number.
+ *
+ * compactor_paged_bounds brings the entries of the units' pages up to date, for `layers` layers from first_layer on: after a fill, and
+ * after an eviction, which moves rows between pages.
+ *   first          device int32 [units of the cache] or NULL (0): pages before the one that holds this token stay as they are (after a fill
+ *                  behind `lengths`: the lengths before it).
+ *   max_length     the most tokens a unit may have (what lies beyond the table's pages does not count).
+ * A unit with a negative length or more than max_length tokens (COMPACTOR_STATUS_CAPACITY) is left out, a page that is none (COMPACTOR_STATUS_PAGE) too.
+ *
+ * compactor_paged_select, of a cache of either kind (it reads no rows): a unit with t tokens, the one that the step is going to append
+ * included, has P = ceil(t / page_tokens) pages.  If P <= pages all are taken.  Otherwise the first `first_pages`, the last `last_pages`
+ * and of the others those of the greatest
+ *   score = max over the KV head's query heads of sum_c q_c (q_c > 0 ? greatest_c : least_c)
+ * (summed in 64 bits, rounded to fp32; of equal scores the lower page; not-a-number ranks above +inf, a page that is none below all), `pages` in all.
+ *   q              rows [batch][heads * q_per_kv] of the layer's queries, as the attention gets them.
+ *   k_new          rows [batch][heads] of the token that the attention is going to append, or ptr NULL (nothing will be appended).  It enters the bounds
+ *                  of its page (as given, in a cache of either kind), so that they need no other call while a sequence grows.
+ *   lengths        device int32 [units of the cache], without the new token.
+ *   table_out      device int32 [heads * batch][pages]: the pages taken, in the unit's order, and -1 behind them.
+ *   lengths_out    device int32 [heads * batch], not `lengths`: the unit's length over that table, again without the new token; a
+ *                  negative length stays, a unit beyond max_length or its pages (COMPACTOR_STATUS_CAPACITY) gets -1.
+ *   options (HOST): 1 <= q_per_kv <= 64; max_length, the most tokens a unit may have, the new one included; first_pages >= 0, last_pages
+ *                  >= 1 (a unit's last page is filled only in part, and takes the new token), first_pages + last_pages <= pages.
+ * Pages that are taken and are none are reported (COMPACTOR_STATUS_PAGE) and left to the attention.
+ * At most 49152 pages per unit (COMPACTOR_E_TOO_LARGE).  Workspace: compactor_paged_select_workspace_bytes(), 256-byte aligned, contents
+ * not preserved; 0 = bad arguments.  `bounds` is written (one page per unit): calls that share it are ordered by the caller.
+ */
+typedef struct compactor_select_options {
+    int32_t q_per_kv;
+    int32_t max_length;
+    int32_t pages;
+    int32_t first_pages;
+    int32_t last_pages;
+} compactor_select_options;
+int compactor_paged_bounds(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* first,
+                           const int32_t* lengths, int32_t max_length, void* bounds, int32_t* status, void* stream);
+int compactor_paged4_bounds(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* first,
+                            const int32_t* lengths, int32_t max_length, void* bounds, int32_t* status, void* stream);
+size_t compactor_paged_select_workspace_bytes(const compactor_paged_cache* cache, int32_t max_length);
+int compactor_paged_select(const compactor_paged_cache* cache, int32_t layer, const compactor_select_options* options,
+                           compactor_rows q, compactor_rows k_new, const int32_t* lengths, void* bounds, int32_t* table_out,
+                           int32_t* lengths_out, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Norms of queries and keys for each head and the rotation by position, in one pass: what makes the keys that a prefill is scored by
+ * (k_plain_out), the keys it is held and attended to as (k_out) and the queries (q_out), and the rows of a decoding step.
+ *   y = x * weight / sqrt(mean(x^2) + eps) in fp32, or y = x where the weight is NULL;
+ *   angle_i = position * inv_freq[i] (taken in 64 bits), i < rotary / 2; with (j, k) = (i, i + rotary / 2), or (2 i, 2 i + 1) when interleaved,
+ *   (y_j, y_k) becomes (y_j cos - y_k sin, y_k cos + y_j sin); channels from `rotary` on stay.  Each output is rounded once.
+ *   q, k           rows [tokens][q_heads] and [tokens][k_heads] (stride_seq: between tokens); either number of heads may be 0.
+ *   q_weight, k_weight  device bf16 [d], 16-byte aligned, or NULL: no norm.
+ *   positions      device int32 [tokens];  inv_freq  device fp32 [rotary / 2]; not used (may be NULL) when rotary = 0.
+ *   q_out, k_out   rows as above.  They may be the rows of q and k themselves; other than that outputs overlap neither inputs nor each other.
+ *   k_plain_out    rows of y of the keys, or ptr NULL.
+ *   options (HOST): d = 128, rotary a multiple of 16 up to d, eps >= 0, interleaved 0 or 1.
+ * No workspace.
+ */
+typedef struct compactor_norm_rope_options {
+    int32_t q_heads;
+    int32_t k_heads;
+    int32_t d;
+    int32_t rotary;
+    int32_t interleaved;
+    float   eps;
+} compactor_norm_rope_options;
+int compactor_norm_rope(const compactor_norm_rope_options* options, int64_t tokens, compactor_rows q, compactor_rows k,
+                        const void* q_weight, const void* k_weight, const int32_t* positions, const float* inv_freq,
+                        compactor_rows q_out, compactor_rows k_out, compactor_rows k_plain_out, void* stream);
+
+/*
  * compactor_score for callers that cannot allocate device memory (the paper has no counterpart;
  * this is a deployment convenience).  Same inputs, outputs and results as compactor_score, but
  * no workspace argument: the scratch is a fixed array of compactor_builtin_scratch_bytes()

@@ -47,6 +47,14 @@ class CompactorDecodeOptions(Structure):
     _fields_ = [("q_per_kv", c_int32), ("max_length", c_int32), ("scale", c_float), ("softcap", c_float), ("accumulate", c_int32)]
 
 
+class CompactorSelectOptions(Structure):
+    _fields_ = [("q_per_kv", c_int32), ("max_length", c_int32), ("pages", c_int32), ("first_pages", c_int32), ("last_pages", c_int32)]
+
+
+class CompactorNormRopeOptions(Structure):
+    _fields_ = [("q_heads", c_int32), ("k_heads", c_int32), ("d", c_int32), ("rotary", c_int32), ("interleaved", c_int32), ("eps", c_float)]
+
+
 class CompactorError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -107,6 +115,20 @@ def _load() -> ctypes.CDLL:
                                               c_void_p, c_size_t, c_void_p]
     lib.compactor_paged_evict.argtypes = [POINTER(CompactorPagedCache), c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32,
                                           c_int32, c_void_p, c_void_p, c_void_p]
+    for name in ("fill", "attention_workspace_bytes", "attention", "evict"):
+        four, plain = getattr(lib, f"compactor_paged4_{name}"), getattr(lib, f"compactor_paged_{name}")
+        four.restype, four.argtypes = plain.restype, plain.argtypes
+    for name in ("compactor_paged_read", "compactor_paged4_read"):
+        getattr(lib, name).argtypes = [POINTER(CompactorPagedCache), c_int32, POINTER(CompactorShape), c_void_p, c_void_p, CompactorMat,
+                                       CompactorMat, c_void_p, c_void_p]
+    for name in ("compactor_paged_bounds", "compactor_paged4_bounds"):
+        getattr(lib, name).argtypes = [POINTER(CompactorPagedCache), c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p]
+    lib.compactor_paged_select_workspace_bytes.restype = c_size_t
+    lib.compactor_paged_select_workspace_bytes.argtypes = [POINTER(CompactorPagedCache), c_int32]
+    lib.compactor_paged_select.argtypes = [POINTER(CompactorPagedCache), c_int32, POINTER(CompactorSelectOptions), CompactorRows,
+                                           CompactorRows, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.compactor_norm_rope.argtypes = [POINTER(CompactorNormRopeOptions), c_int64, CompactorRows, CompactorRows, c_void_p, c_void_p,
+                                        c_void_p, c_void_p, CompactorRows, CompactorRows, CompactorRows, c_void_p]
     lib.compactor_wait_selftest.argtypes = [c_void_p, c_void_p]
     lib.compactor_builtin_scratch_bytes.restype = c_size_t
     lib.compactor_score_builtin_scratch.argtypes = [POINTER(CompactorShape), CompactorMat, c_void_p, c_void_p, c_float,
@@ -123,8 +145,10 @@ def _load_fastcall():
     spec = importlib.util.spec_from_file_location(f"{__package__}._fastcall", path)
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)
-    module.bind(*[ctypes.cast(f, c_void_p).value for f in (LIB.compactor_paged_fill, LIB.compactor_paged_attention,
-                                                          LIB.compactor_paged_evict)])
+    module.bind(*[ctypes.cast(f, c_void_p).value for f in (
+        LIB.compactor_paged_fill, LIB.compactor_paged_attention, LIB.compactor_paged_evict, LIB.compactor_paged_read,
+        LIB.compactor_paged_bounds, LIB.compactor_paged4_fill, LIB.compactor_paged4_attention, LIB.compactor_paged4_evict,
+        LIB.compactor_paged4_read, LIB.compactor_paged4_bounds, LIB.compactor_paged_select, LIB.compactor_norm_rope)])
     return module
 
 
@@ -150,7 +174,10 @@ EXPORTS = ["compactor_version", "compactor_error_string", "compactor_make_sketch
            "compactor_builtin_scratch_bytes", "compactor_score_builtin_scratch", "compactor_attention_scores", "compactor_attention_scores_status", "compactor_wait_selftest",
            "compactor_across_heads_workspace_bytes", "compactor_select_across_heads", "compactor_compact_across_heads",
            "compactor_score_variant", "compactor_nll", "compactor_compress_full_workspace_bytes", "compactor_compress_full",
-           "compactor_paged_fill", "compactor_paged_attention_workspace_bytes", "compactor_paged_attention", "compactor_paged_evict"]
+           "compactor_paged_fill", "compactor_paged_attention_workspace_bytes", "compactor_paged_attention", "compactor_paged_evict",
+           "compactor_paged4_fill", "compactor_paged4_attention_workspace_bytes", "compactor_paged4_attention", "compactor_paged4_evict",
+           "compactor_paged_read", "compactor_paged4_read", "compactor_paged_bounds", "compactor_paged4_bounds",
+           "compactor_paged_select_workspace_bytes", "compactor_paged_select", "compactor_norm_rope"]
 
 FACTOR_CHOLESKY = 0
 FACTOR_EIG = 1
@@ -391,18 +418,10 @@ def compress_full(shape: Shape, opt: CompactorOptions, q: Optional[torch.Tensor]
                                        _stream()), "compactor_compress_full")
 
 
-class PagedCache:
-    """A paged cache (compactor_paged_cache) over the caller's tensors, which it keeps alive.
+class _Pages:
+    """What the two kinds of paged cache share: the checks of the page table and of the pools beside the rows."""
 
-    k_pages, v_pages  bf16 [n_pages, page_tokens, d], same strides, contiguous along d; views of larger tensors are fine.
-    page_table        int32 [layers, heads, batch, max_pages], contiguous.
-    mass, positions   fp32 / int32 [n_pages, page_tokens], contiguous, or None."""
-
-    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
-                 mass: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
-        if k_pages.dim() != 3 or k_pages.dtype != torch.bfloat16 or v_pages.dtype != torch.bfloat16 or \
-                k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride() or k_pages.stride(2) != 1:
-            raise ValueError("k_pages and v_pages: bf16 [n_pages, page_tokens, d] with the same strides, contiguous along d")
+    def __init__(self, k_pages, v_pages, page_table, mass, positions, stride_page: int, stride_token: int, d: int):
         if page_table.dim() != 4 or page_table.dtype != torch.int32 or not page_table.is_contiguous():
             raise ValueError("page_table: contiguous int32 [layers, heads, batch, max_pages]")
         for t, dtype, name in ((mass, torch.float32, "mass"), (positions, torch.int32, "positions")):
@@ -413,9 +432,10 @@ class PagedCache:
         if any(t is not None and t.device != self.device for t in self.tensors):
             raise ValueError("the tensors of a cache live on one device")
         self.layers, self.heads, self.batch, self.max_pages = page_table.shape
-        self.n_pages, self.page_tokens, self.d = k_pages.shape
+        self.n_pages, self.page_tokens = k_pages.shape[:2]
+        self.d = d
         self.units = self.layers * self.heads * self.batch
-        self.c = CompactorPagedCache(k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride(0), k_pages.stride(1),
+        self.c = CompactorPagedCache(k_pages.data_ptr(), v_pages.data_ptr(), stride_page, stride_token,
                                      None if mass is None else mass.data_ptr(), None if positions is None else positions.data_ptr(),
                                      page_table.data_ptr(), self.n_pages, self.page_tokens, self.max_pages,
                                      self.layers, self.heads, self.batch, self.d)
@@ -423,23 +443,74 @@ class PagedCache:
         self._device = self.device.index if self.device.type == "cuda" else -1
 
 
-def _expect(x, kind: type, name: str) -> None:
+class PagedCache(_Pages):
+    """A paged cache (compactor_paged_cache) over the caller's tensors, which it keeps alive.
+
+    k_pages, v_pages  bf16 [n_pages, page_tokens, d], same strides, contiguous along d; views of larger tensors are fine.
+    page_table        int32 [layers, heads, batch, max_pages], contiguous.
+    mass, positions   fp32 / int32 [n_pages, page_tokens], contiguous, or None."""
+    _four = 0
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                 mass: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
+        if k_pages.dim() != 3 or k_pages.dtype != torch.bfloat16 or v_pages.dtype != torch.bfloat16 or \
+                k_pages.shape != v_pages.shape or k_pages.stride() != v_pages.stride() or k_pages.stride(2) != 1:
+            raise ValueError("k_pages and v_pages: bf16 [n_pages, page_tokens, d] with the same strides, contiguous along d")
+        super().__init__(k_pages, v_pages, page_table, mass, positions, k_pages.stride(0), k_pages.stride(1), k_pages.shape[2])
+
+
+ROW4_BYTES = 80                              # of a row of 128 channels in 4 bits
+
+
+class PagedCache4(_Pages):
+    """A paged cache whose rows are held in 4 bits, 80 bytes each (the layout is in compactor.h).  The calls on a paged cache take
+    one of either kind.
+
+    k_pages, v_pages  uint8 [n_pages, page_tokens, 80], same strides, the rows of a page back to back; views along the pages are fine.
+    page_table, mass, positions  as in PagedCache."""
+    _four = 1
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                 mass: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
+        if k_pages.dim() != 3 or k_pages.dtype != torch.uint8 or v_pages.dtype != torch.uint8 or k_pages.shape != v_pages.shape or \
+                k_pages.stride() != v_pages.stride() or k_pages.shape[2] != ROW4_BYTES or k_pages.stride()[1:] != (ROW4_BYTES, 1):
+            raise ValueError(f"k_pages and v_pages: uint8 [n_pages, page_tokens, {ROW4_BYTES}] with the same strides, the rows of a page back to back")
+        super().__init__(k_pages, v_pages, page_table, mass, positions, k_pages.stride(0), k_pages.stride(1), 128)
+
+
+def _expect(x, kind, name: str) -> None:
     """The compiled calls take structs by address: whose they are is settled here."""
     if not isinstance(x, kind):
-        raise TypeError(f"{name}: a {kind.__name__} is expected")
+        raise TypeError(f"{name}: a {' or '.join(k.__name__ for k in (kind if isinstance(kind, tuple) else (kind,)))} is expected")
 
 
-def paged_fill(cache: PagedCache, shape: Shape, k_cache: torch.Tensor, v_cache: torch.Tensor, keep_counts: Sequence[int],
+_EITHER = (PagedCache, PagedCache4)
+
+
+def paged_fill(cache, shape: Shape, k_cache: torch.Tensor, v_cache: torch.Tensor, keep_counts: Sequence[int],
                idx: Optional[torch.Tensor] = None, head_offsets: Optional[torch.Tensor] = None,
                mass_in: Optional[torch.Tensor] = None, first_position: Optional[torch.Tensor] = None,
                lengths: Optional[torch.Tensor] = None, lengths_out: Optional[torch.Tensor] = None, first_layer: int = 0,
                status: Optional[torch.Tensor] = None) -> None:
     """Compaction into pages: the kept rows (`idx`, and `head_offsets` after a selection across heads; without `idx` the first
-    keep_counts[b] rows of every sequence) of k_cache / v_cache [layers, heads, tokens, d] go behind `lengths`."""
-    _expect(cache, PagedCache, "cache")
+    keep_counts[b] rows of every sequence) of k_cache / v_cache [layers, heads, tokens, d] go behind `lengths`; into a PagedCache4
+    in 4 bits."""
+    _expect(cache, _EITHER, "cache")
     _expect(shape, Shape, "shape")
-    _check(_fastcall.fill(cache._address, cache._device, first_layer, ctypes.addressof(shape.c), k_cache, v_cache, keep_counts, idx,
-                          head_offsets, mass_in, first_position, lengths, lengths_out, status), "compactor_paged_fill")
+    _check((_fastcall.fill4 if cache._four else _fastcall.fill)(
+        cache._address, cache._device, first_layer, ctypes.addressof(shape.c), k_cache, v_cache, keep_counts, idx, head_offsets, mass_in,
+        first_position, lengths, lengths_out, status), "compactor_paged4_fill" if cache._four else "compactor_paged_fill")
+
+
+def paged_read(cache, shape: Shape, lengths: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor, first: Optional[torch.Tensor] = None,
+               first_layer: int = 0, status: Optional[torch.Tensor] = None) -> None:
+    """Rows out of the pages: token first[u] + j of every unit into row j of its sequence of k_out / v_out bf16 [layers, heads, tokens, d], as
+    many as `shape` gives the sequence and the unit has; other rows keep what they hold."""
+    _expect(cache, _EITHER, "cache")
+    _expect(shape, Shape, "shape")
+    _check((_fastcall.read4 if cache._four else _fastcall.read)(
+        cache._address, cache._device, first_layer, ctypes.addressof(shape.c), first, lengths, k_out, v_out, status),
+        "compactor_paged4_read" if cache._four else "compactor_paged_read")
 
 
 def decode_options(q_per_kv: int, max_length: int, scale: float = 128 ** -0.5, softcap: float = 0.0,
@@ -447,36 +518,79 @@ def decode_options(q_per_kv: int, max_length: int, scale: float = 128 ** -0.5, s
     return CompactorDecodeOptions(q_per_kv, max_length, scale, softcap, 1 if accumulate else 0)
 
 
-def paged_attention_workspace_bytes(cache: PagedCache, opt: CompactorDecodeOptions) -> int:
-    _expect(cache, PagedCache, "cache")
+def paged_attention_workspace_bytes(cache, opt: CompactorDecodeOptions) -> int:
+    _expect(cache, _EITHER, "cache")
     _expect(opt, CompactorDecodeOptions, "opt")
-    return int(LIB.compactor_paged_attention_workspace_bytes(byref(cache.c), byref(opt)))
+    size = LIB.compactor_paged4_attention_workspace_bytes if cache._four else LIB.compactor_paged_attention_workspace_bytes
+    return int(size(byref(cache.c), byref(opt)))
 
 
-def alloc_paged_attention_workspace(cache: PagedCache, opt: CompactorDecodeOptions) -> torch.Tensor:
+def alloc_paged_attention_workspace(cache, opt: CompactorDecodeOptions) -> torch.Tensor:
     return torch.empty(max(256, paged_attention_workspace_bytes(cache, opt)), dtype=torch.uint8, device=cache.device)
 
 
-def paged_attention(cache: PagedCache, layer: int, opt: CompactorDecodeOptions, q: torch.Tensor, lengths: torch.Tensor,
+def paged_attention(cache, layer: int, opt: CompactorDecodeOptions, q: torch.Tensor, lengths: torch.Tensor,
                     out: torch.Tensor, workspace: torch.Tensor, k_new: Optional[torch.Tensor] = None,
                     v_new: Optional[torch.Tensor] = None, new_positions: Optional[torch.Tensor] = None,
                     lse_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
     """Attention of one new token per sequence: q, out [batch, heads * q_per_kv, d], k_new, v_new [batch, heads, d],
     lse_out fp32 [batch, heads * q_per_kv]; `lengths` [layers, heads, batch] without the new token, left as it is."""
-    _expect(cache, PagedCache, "cache")
+    _expect(cache, _EITHER, "cache")
     _expect(opt, CompactorDecodeOptions, "opt")
-    _check(_fastcall.attention(cache._address, cache._device, layer, ctypes.addressof(opt), q, lengths, out, workspace, k_new, v_new,
-                               new_positions, lse_out, status), "compactor_paged_attention")
+    _check((_fastcall.attention4 if cache._four else _fastcall.attention)(
+        cache._address, cache._device, layer, ctypes.addressof(opt), q, lengths, out, workspace, k_new, v_new, new_positions, lse_out,
+        status), "compactor_paged4_attention" if cache._four else "compactor_paged_attention")
 
 
-def paged_evict(cache: PagedCache, lengths: torch.Tensor, budgets: torch.Tensor, lengths_out: torch.Tensor, max_length: int,
+def paged_evict(cache, lengths: torch.Tensor, budgets: torch.Tensor, lengths_out: torch.Tensor, max_length: int,
                 recent: int = 0, next_position: Optional[torch.Tensor] = None, first_layer: int = 0, layers: Optional[int] = None,
                 status: Optional[torch.Tensor] = None) -> None:
     """Evicts every unit that holds more than its budget down to it: the `recent` newest tokens and those of the greatest
     accumulated weight stay.  lengths, budgets, lengths_out: int32 [layers, heads, batch]; lengths_out may be lengths."""
-    _expect(cache, PagedCache, "cache")
-    _check(_fastcall.evict(cache._address, cache._device, first_layer, cache.layers - first_layer if layers is None else layers, lengths,
-                           budgets, next_position, recent, max_length, lengths_out, status), "compactor_paged_evict")
+    _expect(cache, _EITHER, "cache")
+    _check((_fastcall.evict4 if cache._four else _fastcall.evict)(
+        cache._address, cache._device, first_layer, cache.layers - first_layer if layers is None else layers, lengths, budgets, next_position,
+        recent, max_length, lengths_out, status), "compactor_paged4_evict" if cache._four else "compactor_paged_evict")
+
+
+def paged_bounds(cache, lengths: torch.Tensor, bounds: torch.Tensor, max_length: int, first: Optional[torch.Tensor] = None,
+                 first_layer: int = 0, layers: Optional[int] = None, status: Optional[torch.Tensor] = None) -> None:
+    """Least and greatest key of every page of every unit, from the page of token first[u] on, into bounds bf16 [n_pages, 2, d]."""
+    _expect(cache, _EITHER, "cache")
+    _check((_fastcall.bounds4 if cache._four else _fastcall.bounds)(
+        cache._address, cache._device, first_layer, cache.layers - first_layer if layers is None else layers, first, lengths, max_length,
+        bounds, status), "compactor_paged4_bounds" if cache._four else "compactor_paged_bounds")
+
+
+def paged_select_workspace_bytes(cache, max_length: int) -> int:
+    _expect(cache, _EITHER, "cache")
+    return int(LIB.compactor_paged_select_workspace_bytes(byref(cache.c), max_length))
+
+
+def alloc_paged_select_workspace(cache, max_length: int) -> torch.Tensor:
+    return torch.empty(max(256, paged_select_workspace_bytes(cache, max_length)), dtype=torch.uint8, device=cache.device)
+
+
+def paged_select(cache, layer: int, q_per_kv: int, q: torch.Tensor, lengths: torch.Tensor, bounds: torch.Tensor, table_out: torch.Tensor,
+                 lengths_out: torch.Tensor, workspace: torch.Tensor, max_length: int, first_pages: int = 1, last_pages: int = 1,
+                 k_new: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
+    """The pages that a step attends to: table_out int32 [1, heads, batch, pages] and lengths_out int32 [1, heads, batch] make, with the
+    pools of `cache`, a cache of one layer for `paged_attention`.  `pages` is the size of table_out's last axis; the first
+    first_pages and last last_pages are always taken, the others by their bounds.  max_length counts the new token."""
+    _expect(cache, _EITHER, "cache")
+    _check(_fastcall.select(cache._address, cache._device, layer, q_per_kv, max_length, first_pages, last_pages, q, k_new, lengths, bounds,
+                            table_out, lengths_out, workspace, status), "compactor_paged_select")
+
+
+def norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor],
+              q_out: Optional[torch.Tensor], k_out: Optional[torch.Tensor], k_plain_out: Optional[torch.Tensor] = None,
+              q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+              interleaved: bool = False) -> None:
+    """Norms of queries and keys for each head (where there is a weight, bf16 [d]) and the rotation of their first 2 * inv_freq.numel()
+    channels by positions int32 [tokens] * inv_freq fp32.  q, q_out bf16 [tokens, q_heads, d], k, k_out, k_plain_out [tokens, k_heads, d],
+    any strides with a contiguous last axis (a layer of [heads, tokens, d] transposed, say); q or k may be None."""
+    _check(_fastcall.norm_rope(q, k, positions, inv_freq, q_out, k_out, k_plain_out, q_weight, k_weight, eps, interleaved),
+           "compactor_norm_rope")
 
 
 def wait_selftest() -> int:

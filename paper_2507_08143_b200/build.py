@@ -13,7 +13,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcompactor.so")
 SOURCES = ["api.cu", "tensormap.cu", "sweep.cu", "gram.cu", "factor.cu", "score.cu", "select.cu", "compact.cu", "attention.cu", "nll.cu",
-           "paged.cu", "decode.cu"]
+           "paged.cu", "decode.cu", "decode4.cu", "read.cu", "pages.cu", "rope.cu"]
 HEADER = os.path.join(ROOT, "include", "compactor.h")
 FASTCALL_SOURCE = "fastcall.cpp"
 

@@ -10,6 +10,8 @@
 
 #include "common.cuh"
 #include "paged.cuh"
+#include "quant4.cuh"
+#include "rope.cuh"
 #include "sm100.cuh"
 
 using namespace compactor;
@@ -481,7 +483,7 @@ extern "C" void compactor_debug_set_profile_buffer(long long* device_counters) {
 
 extern "C" {
 
-int compactor_version(void) { return 200; }
+int compactor_version(void) { return 300; }
 
 const char* compactor_error_string(int code) {
     switch (code) {
@@ -1090,7 +1092,8 @@ constexpr int kMaxQPerKv = 64;
 
 bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
-bool cache_ok(const compactor_paged_cache* c, int* err) {
+// `four`: rows of 80 bytes back to back, strides in bytes.
+bool cache_ok(const compactor_paged_cache* c, int* err, bool four = false) {
     *err = COMPACTOR_E_INVALID_ARGUMENT;
     if (c == nullptr || c->k_pages == nullptr || c->v_pages == nullptr || c->page_table == nullptr) return false;
     if (!aligned(c->k_pages, 16) || !aligned(c->v_pages, 16) || !aligned(c->page_table, 4) || !aligned(c->mass, 16) ||
@@ -1100,12 +1103,14 @@ bool cache_ok(const compactor_paged_cache* c, int* err) {
     if ((long long)c->layers * c->heads > 65535 || (long long)c->layers * c->heads * c->batch > 0x7fffffffLL) return false;
     if (c->page_tokens < 8 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1)) != 0) return false;
     if ((long long)c->max_pages * c->page_tokens > 0x7fff0000LL) return false;           // a slot number and one tile more fit an int
+    if (four)
+        return c->stride_token == kRow4 && (c->stride_page & 15) == 0 && c->stride_page >= (long long)c->page_tokens * kRow4 && c->stride_page <= (1LL << 50);
     if (c->stride_token < kD || (c->stride_token & 7) || (c->stride_page & 7) || c->stride_token > (1LL << 40)) return false;
     if (c->stride_page < c->page_tokens * c->stride_token) return false;
     return true;
 }
 
-Paged to_paged(const compactor_paged_cache* c) {
+Paged to_paged(const compactor_paged_cache* c, bool four = false) {
     Paged p;
     p.k = static_cast<__nv_bfloat16*>(c->k_pages); p.v = static_cast<__nv_bfloat16*>(c->v_pages);
     p.stride_page = c->stride_page; p.stride_token = c->stride_token;
@@ -1114,6 +1119,8 @@ Paged to_paged(const compactor_paged_cache* c) {
     p.page_shift = 0;
     while ((1 << p.page_shift) < c->page_tokens) ++p.page_shift;
     p.layers = c->layers; p.heads = c->heads; p.batch = c->batch;
+    p.row_pieces = kD / 8;
+    if (four) { p.stride_page /= 2; p.stride_token /= 2; p.row_pieces = kRow4 / 16; }
     return p;
 }
 
@@ -1123,12 +1130,12 @@ bool rows_ok(const compactor_rows& r) {
 }
 
 struct DecodeLayout {
-    int workers, groups, capacity;
+    int workers, busy_workers, groups, capacity;
     size_t off_ml, off_o, off_scores, total;
 };
 // Workspace of the attention: tile prefix, partial (max, sum) pairs, partial outputs, scores.
-bool decode_layout(const compactor_paged_cache* c, const compactor_decode_options* o, DecodeLayout* l, int* err) {
-    if (!cache_ok(c, err)) return false;
+bool decode_layout(const compactor_paged_cache* c, const compactor_decode_options* o, DecodeLayout* l, int* err, bool four) {
+    if (!cache_ok(c, err, four)) return false;
     *err = COMPACTOR_E_INVALID_ARGUMENT;
     if (o == nullptr || o->q_per_kv < 1 || o->max_length < 1 || !(o->scale > 0.f) || !isfinite(o->scale) ||
         !(o->softcap >= 0.f) || !isfinite(o->softcap)) return false;
@@ -1142,7 +1149,10 @@ bool decode_layout(const compactor_paged_cache* c, const compactor_decode_option
     l->groups = (o->q_per_kv + kDecodeHeads - 1) / kDecodeHeads;
     const long long tiles = units * ((l->capacity + kDecodeTile - 1) / kDecodeTile);
     if ((tiles + units * kDecodeUnitCost) * l->groups > 0x7fffffffLL || tiles + units * kDecodeMassUnitCost > 0x7fffffffLL || units * o->q_per_kv > 0x3fffffffLL) { *err = COMPACTOR_E_TOO_LARGE; return false; }
-    l->workers = (int)std::min<long long>(sm_count(), tiles * l->groups) * kDecodeWarps;
+    const int warps = !four ? kDecodeWarps : o->q_per_kv <= 8 ? kDecode4Warps : kDecode4WarpsWide;
+    const int blocks = (int)std::min<long long>(sm_count(), tiles * l->groups);
+    l->workers = blocks * warps;
+    l->busy_workers = four ? l->workers : blocks * (warps - 1);
     const size_t slots = (size_t)l->workers + (size_t)units * l->groups;
     size_t off = align_up(sizeof(int) * ((size_t)units + 1));
     l->off_ml = off;     off += align_up(sizeof(float) * 32 * slots);
@@ -1154,13 +1164,12 @@ bool decode_layout(const compactor_paged_cache* c, const compactor_decode_option
 
 }  // namespace
 
-extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape,
-                                    compactor_mat k_cache, compactor_mat v_cache, const int32_t* idx,
-                                    const int32_t* head_offsets, const int32_t* keep_counts, const float* mass_in,
-                                    const int32_t* first_position, const int32_t* lengths, int32_t* lengths_out,
-                                    int32_t* status, void* stream) {
+namespace {
+int fill(bool four, const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape, compactor_mat k_cache, compactor_mat v_cache, const int32_t* idx,
+         const int32_t* head_offsets, const int32_t* keep_counts, const float* mass_in, const int32_t* first_position, const int32_t* lengths,
+         int32_t* lengths_out, int32_t* status, void* stream) {
     int err = 0;
-    if (!cache_ok(cache, &err) || !shape_ok(shape, &err)) return err;
+    if (!cache_ok(cache, &err, four) || !shape_ok(shape, &err)) return err;
     const bool some = shape->cu_seqlens[shape->batch] > 0;               // without tokens there is nothing to point to
     if ((some && (!mat_ok(k_cache) || !mat_ok(v_cache))) || keep_counts == nullptr ||
         shape->heads != cache->heads || shape->batch != cache->batch || first_layer < 0 ||
@@ -1176,7 +1185,8 @@ extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     FillArgs a;
     memset(&a, 0, sizeof(a));
-    a.c = to_paged(cache); a.k = to_mat(k_cache); a.v = to_mat(v_cache);
+    a.c = to_paged(cache, four); a.k = to_mat(k_cache); a.v = to_mat(v_cache);
+    a.four = four;
     a.first_layer = first_layer; a.layers = shape->layers;
     a.total_tokens = shape->cu_seqlens[shape->batch]; a.total_keep = (int)kept;
     a.idx = idx; a.head_offsets = head_offsets; a.mass_in = mass_in; a.first_position = first_position;
@@ -1196,17 +1206,17 @@ extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t 
     return COMPACTOR_OK;
 }
 
-extern "C" size_t compactor_paged_attention_workspace_bytes(const compactor_paged_cache* cache, const compactor_decode_options* options) {
+size_t attention_workspace_bytes(bool four, const compactor_paged_cache* cache, const compactor_decode_options* options) {
     DecodeLayout l; int err = 0;
-    return decode_layout(cache, options, &l, &err) ? l.total : 0;
+    return decode_layout(cache, options, &l, &err, four) ? l.total : 0;
 }
 
-extern "C" int compactor_paged_attention(const compactor_paged_cache* cache, int32_t layer, const compactor_decode_options* options,
-                                         compactor_rows q, compactor_rows k_new, compactor_rows v_new, const int32_t* new_positions,
-                                         const int32_t* lengths, compactor_rows out, float* lse_out, int32_t* status,
-                                         void* workspace, size_t workspace_bytes, void* stream) {
+int attention(bool four, const compactor_paged_cache* cache, int32_t layer, const compactor_decode_options* options,
+              compactor_rows q, compactor_rows k_new, compactor_rows v_new, const int32_t* new_positions,
+              const int32_t* lengths, compactor_rows out, float* lse_out, int32_t* status,
+              void* workspace, size_t workspace_bytes, void* stream) {
     DecodeLayout l; int err = 0;
-    if (!decode_layout(cache, options, &l, &err)) return err;
+    if (!decode_layout(cache, options, &l, &err, four)) return err;
     const bool append = k_new.ptr != nullptr;
     if (layer < 0 || layer >= cache->layers || !rows_ok(q) || !rows_ok(out) || append != (v_new.ptr != nullptr) ||
         (append && (!rows_ok(k_new) || !rows_ok(v_new))) || lengths == nullptr || workspace == nullptr || !aligned(workspace, kAlign))
@@ -1218,7 +1228,8 @@ extern "C" int compactor_paged_attention(const compactor_paged_cache* cache, int
     char* ws = static_cast<char*>(workspace);
     DecodeArgs a;
     memset(&a, 0, sizeof(a));
-    a.c = to_paged(cache);
+    a.c = to_paged(cache, four);
+    a.four = four;
     a.units = cache->heads * cache->batch;
     const size_t first = (size_t)layer * a.units;
     a.c.table += first * cache->max_pages;
@@ -1230,7 +1241,7 @@ extern "C" int compactor_paged_attention(const compactor_paged_cache* cache, int
     a.new_positions = new_positions;
     a.out = static_cast<__nv_bfloat16*>(out.ptr); a.out_seq = out.stride_seq; a.out_head = out.stride_head;
     a.lse = lse_out;
-    a.g = options->q_per_kv; a.groups = l.groups; a.capacity = l.capacity; a.workers = l.workers;
+    a.g = options->q_per_kv; a.groups = l.groups; a.capacity = l.capacity; a.workers = l.workers; a.busy_workers = l.busy_workers;
     a.accumulate = options->accumulate != 0; a.scale = options->scale; a.softcap = options->softcap;
     a.prefix = reinterpret_cast<int*>(ws);
     a.ml = reinterpret_cast<float*>(ws + l.off_ml);
@@ -1243,11 +1254,11 @@ extern "C" int compactor_paged_attention(const compactor_paged_cache* cache, int
     return COMPACTOR_OK;
 }
 
-extern "C" int compactor_paged_evict(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* lengths,
-                                     const int32_t* budgets, const int32_t* next_position, int32_t recent, int32_t max_length,
-                                     int32_t* lengths_out, int32_t* status, void* stream) {
+int evict(bool four, const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* lengths,
+          const int32_t* budgets, const int32_t* next_position, int32_t recent, int32_t max_length,
+          int32_t* lengths_out, int32_t* status, void* stream) {
     int err = 0;
-    if (!cache_ok(cache, &err)) return err;
+    if (!cache_ok(cache, &err, four)) return err;
     if (layers < 1 || first_layer < 0 || first_layer > cache->layers - layers || lengths == nullptr || budgets == nullptr ||
         lengths_out == nullptr || recent < 0 || max_length < 1 || cache->mass == nullptr ||
         (recent > 0 && (cache->positions == nullptr || next_position == nullptr)))
@@ -1258,7 +1269,7 @@ extern "C" int compactor_paged_evict(const compactor_paged_cache* cache, int32_t
     const size_t per_layer = (size_t)cache->heads * cache->batch;
     EvictArgs a;
     memset(&a, 0, sizeof(a));
-    a.c = to_paged(cache);
+    a.c = to_paged(cache, four);
     a.first_unit = (int)(first_layer * per_layer); a.units = (int)(layers * per_layer);
     if (a.units > 0x7fffffff / 8) return COMPACTOR_E_TOO_LARGE;          // grid size with clusters of 8
     a.lengths = lengths; a.budgets = budgets; a.next_position = next_position;
@@ -1266,5 +1277,210 @@ extern "C" int compactor_paged_evict(const compactor_paged_cache* cache, int32_t
     if (status != nullptr) CK(cudaMemsetAsync(status + a.first_unit, 0, sizeof(int32_t) * a.units, st));
     compactor::set_chain_for(0);
     CK(launch_paged_evict(a, sm_count(), st));
+    return COMPACTOR_OK;
+}
+
+int read(bool four, const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape, const int32_t* first,
+         const int32_t* lengths, compactor_mat k_out, compactor_mat v_out, int32_t* status, void* stream) {
+    int err = 0;
+    if (!cache_ok(cache, &err, four) || !shape_ok(shape, &err)) return err;
+    const bool some = shape->cu_seqlens[shape->batch] > 0;
+    if ((some && (!mat_ok(k_out) || !mat_ok(v_out))) || lengths == nullptr || shape->heads != cache->heads || shape->batch != cache->batch ||
+        first_layer < 0 || first_layer > cache->layers - shape->layers)
+        return COMPACTOR_E_INVALID_ARGUMENT;
+    for (const compactor_mat* m : {&k_out, &v_out})          // heads and layers on top of each other
+        if (some && ((shape->heads > 1 && m->stride_head < kD) || (shape->layers > 1 && m->stride_layer < kD))) return COMPACTOR_E_INVALID_ARGUMENT;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    ReadArgs a;
+    memset(&a, 0, sizeof(a));
+    a.c = to_paged(cache, four);
+    a.k = static_cast<__nv_bfloat16*>(const_cast<void*>(k_out.ptr)); a.v = static_cast<__nv_bfloat16*>(const_cast<void*>(v_out.ptr));
+    a.k_layer = k_out.stride_layer; a.k_head = k_out.stride_head; a.k_token = k_out.stride_token;
+    a.v_layer = v_out.stride_layer; a.v_head = v_out.stride_head; a.v_token = v_out.stride_token;
+    a.first_layer = first_layer; a.layers = shape->layers; a.first = first; a.lengths = lengths; a.status = status; a.four = four;
+    const size_t per_layer = (size_t)cache->heads * cache->batch;
+    if (status != nullptr) CK(cudaMemsetAsync(status + first_layer * per_layer, 0, sizeof(int32_t) * per_layer * shape->layers, st));
+    compactor::set_chain_for(0);
+    for (a.b0 = 0; a.b0 < shape->batch; a.b0 += kFillSeqs) {
+        a.nb = std::min(kFillSeqs, shape->batch - a.b0);
+        ReadTables t;
+        for (int b = 0; b <= a.nb; ++b) t.cu_seqlens[b] = shape->cu_seqlens[a.b0 + b];
+        CK(launch_paged_read(a, t, st));
+    }
+    return COMPACTOR_OK;
+}
+
+int bounds(bool four, const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* first, const int32_t* lengths,
+           int32_t max_length, void* bounds_out, int32_t* status, void* stream) {
+    int err = 0;
+    if (!cache_ok(cache, &err, four)) return err;
+    if (layers < 1 || first_layer < 0 || first_layer > cache->layers - layers || lengths == nullptr || max_length < 1 || bounds_out == nullptr ||
+        !aligned(bounds_out, 16))
+        return COMPACTOR_E_INVALID_ARGUMENT;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const size_t per_layer = (size_t)cache->heads * cache->batch;
+    BoundsArgs a;
+    memset(&a, 0, sizeof(a));
+    a.c = to_paged(cache, four);
+    a.first_unit = (int)(first_layer * per_layer); a.units = (int)(layers * per_layer);
+    a.capacity = (int)std::min<long long>(max_length, (long long)cache->max_pages * cache->page_tokens);
+    if ((long long)a.units * ((a.capacity + cache->page_tokens - 1) / cache->page_tokens) > 0x7fffffffLL) return COMPACTOR_E_TOO_LARGE;
+    a.first = first; a.lengths = lengths; a.bounds = static_cast<__nv_bfloat16*>(bounds_out); a.status = status; a.four = four;
+    if (status != nullptr) CK(cudaMemsetAsync(status + a.first_unit, 0, sizeof(int32_t) * a.units, st));
+    compactor::set_chain_for(0);
+    CK(launch_paged_bounds(a, st));
+    return COMPACTOR_OK;
+}
+
+// The choice of pages reads no row of the cache, and takes one of either kind.
+bool either_cache_ok(const compactor_paged_cache* c, int* err) { return cache_ok(c, err, c != nullptr && c->stride_token == kRow4); }
+
+}  // namespace
+
+extern "C" int compactor_paged_fill(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape,
+                                    compactor_mat k_cache, compactor_mat v_cache, const int32_t* idx,
+                                    const int32_t* head_offsets, const int32_t* keep_counts, const float* mass_in,
+                                    const int32_t* first_position, const int32_t* lengths, int32_t* lengths_out,
+                                    int32_t* status, void* stream) {
+    return fill(false, cache, first_layer, shape, k_cache, v_cache, idx, head_offsets, keep_counts, mass_in, first_position, lengths,
+                lengths_out, status, stream);
+}
+extern "C" int compactor_paged4_fill(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape,
+                                     compactor_mat k_cache, compactor_mat v_cache, const int32_t* idx,
+                                     const int32_t* head_offsets, const int32_t* keep_counts, const float* mass_in,
+                                     const int32_t* first_position, const int32_t* lengths, int32_t* lengths_out,
+                                     int32_t* status, void* stream) {
+    return fill(true, cache, first_layer, shape, k_cache, v_cache, idx, head_offsets, keep_counts, mass_in, first_position, lengths,
+                lengths_out, status, stream);
+}
+
+extern "C" size_t compactor_paged_attention_workspace_bytes(const compactor_paged_cache* cache, const compactor_decode_options* options) {
+    return attention_workspace_bytes(false, cache, options);
+}
+extern "C" size_t compactor_paged4_attention_workspace_bytes(const compactor_paged_cache* cache, const compactor_decode_options* options) {
+    return attention_workspace_bytes(true, cache, options);
+}
+
+extern "C" int compactor_paged_attention(const compactor_paged_cache* cache, int32_t layer, const compactor_decode_options* options,
+                                         compactor_rows q, compactor_rows k_new, compactor_rows v_new, const int32_t* new_positions,
+                                         const int32_t* lengths, compactor_rows out, float* lse_out, int32_t* status,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+    return attention(false, cache, layer, options, q, k_new, v_new, new_positions, lengths, out, lse_out, status, workspace, workspace_bytes,
+                     stream);
+}
+extern "C" int compactor_paged4_attention(const compactor_paged_cache* cache, int32_t layer, const compactor_decode_options* options,
+                                          compactor_rows q, compactor_rows k_new, compactor_rows v_new, const int32_t* new_positions,
+                                          const int32_t* lengths, compactor_rows out, float* lse_out, int32_t* status,
+                                          void* workspace, size_t workspace_bytes, void* stream) {
+    return attention(true, cache, layer, options, q, k_new, v_new, new_positions, lengths, out, lse_out, status, workspace, workspace_bytes,
+                     stream);
+}
+
+extern "C" int compactor_paged_evict(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* lengths,
+                                     const int32_t* budgets, const int32_t* next_position, int32_t recent, int32_t max_length,
+                                     int32_t* lengths_out, int32_t* status, void* stream) {
+    return evict(false, cache, first_layer, layers, lengths, budgets, next_position, recent, max_length, lengths_out, status, stream);
+}
+extern "C" int compactor_paged4_evict(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* lengths,
+                                      const int32_t* budgets, const int32_t* next_position, int32_t recent, int32_t max_length,
+                                      int32_t* lengths_out, int32_t* status, void* stream) {
+    return evict(true, cache, first_layer, layers, lengths, budgets, next_position, recent, max_length, lengths_out, status, stream);
+}
+
+extern "C" int compactor_paged_read(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape, const int32_t* first,
+                                    const int32_t* lengths, compactor_mat k_out, compactor_mat v_out, int32_t* status, void* stream) {
+    return read(false, cache, first_layer, shape, first, lengths, k_out, v_out, status, stream);
+}
+extern "C" int compactor_paged4_read(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape, const int32_t* first,
+                                     const int32_t* lengths, compactor_mat k_out, compactor_mat v_out, int32_t* status, void* stream) {
+    return read(true, cache, first_layer, shape, first, lengths, k_out, v_out, status, stream);
+}
+
+extern "C" int compactor_paged_bounds(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* first,
+                                      const int32_t* lengths, int32_t max_length, void* bounds_out, int32_t* status, void* stream) {
+    return bounds(false, cache, first_layer, layers, first, lengths, max_length, bounds_out, status, stream);
+}
+extern "C" int compactor_paged4_bounds(const compactor_paged_cache* cache, int32_t first_layer, int32_t layers, const int32_t* first,
+                                       const int32_t* lengths, int32_t max_length, void* bounds_out, int32_t* status, void* stream) {
+    return bounds(true, cache, first_layer, layers, first, lengths, max_length, bounds_out, status, stream);
+}
+
+extern "C" size_t compactor_paged_select_workspace_bytes(const compactor_paged_cache* cache, int32_t max_length) {
+    int err = 0;
+    if (!either_cache_ok(cache, &err) || max_length < 1) return 0;
+    const long long capacity = std::min<long long>(max_length, (long long)cache->max_pages * cache->page_tokens);
+    const long long pages = (capacity + cache->page_tokens - 1) / cache->page_tokens;
+    if (pages > kSelectMaxPages) return 0;
+    return align_up(sizeof(uint32_t) * (size_t)cache->heads * cache->batch * pages);
+}
+extern "C" int compactor_paged_select(const compactor_paged_cache* cache, int32_t layer, const compactor_select_options* options,
+                                      compactor_rows q, compactor_rows k_new, const int32_t* lengths, void* bounds, int32_t* table_out,
+                                      int32_t* lengths_out, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+    int err = 0;
+    if (!either_cache_ok(cache, &err)) return err;
+    if (options == nullptr || options->q_per_kv < 1 || options->max_length < 1 || options->pages < 1 || options->first_pages < 0 ||
+        options->last_pages < 1 || (long long)options->first_pages + options->last_pages > options->pages)
+        return COMPACTOR_E_INVALID_ARGUMENT;
+    if (options->q_per_kv > kMaxQPerKv) return COMPACTOR_E_UNSUPPORTED;
+    if (layer < 0 || layer >= cache->layers || !rows_ok(q) || (k_new.ptr != nullptr && !rows_ok(k_new)) || lengths == nullptr ||
+        bounds == nullptr || !aligned(bounds, 16) || table_out == nullptr || lengths_out == nullptr || lengths_out == lengths ||
+        workspace == nullptr || !aligned(workspace, kAlign))
+        return COMPACTOR_E_INVALID_ARGUMENT;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    SelectArgs a;
+    memset(&a, 0, sizeof(a));
+    a.c = to_paged(cache);
+    a.units = cache->heads * cache->batch;
+    a.capacity = (int)std::min<long long>(options->max_length, (long long)cache->max_pages * cache->page_tokens);
+    a.unit_pages = (a.capacity + cache->page_tokens - 1) / cache->page_tokens;
+    if (a.unit_pages > kSelectMaxPages || (long long)a.units * a.unit_pages > 0x7fffffffLL || (long long)a.units * options->pages > (1LL << 40))
+        return COMPACTOR_E_TOO_LARGE;
+    if (workspace_bytes < sizeof(uint32_t) * (size_t)a.units * a.unit_pages) return COMPACTOR_E_WORKSPACE;
+    const size_t first = (size_t)layer * a.units;
+    a.c.table += first * cache->max_pages;
+    a.lengths = lengths + first;
+    a.status = status != nullptr ? status + first : nullptr;
+    a.q = static_cast<const __nv_bfloat16*>(q.ptr); a.q_seq = q.stride_seq; a.q_head = q.stride_head;
+    a.k_new = static_cast<const __nv_bfloat16*>(k_new.ptr); a.kn_seq = k_new.stride_seq; a.kn_head = k_new.stride_head;
+    a.bounds = static_cast<__nv_bfloat16*>(bounds);
+    a.table_out = table_out; a.lengths_out = lengths_out;
+    a.keys = static_cast<uint32_t*>(workspace);
+    a.g = options->q_per_kv; a.pages = options->pages; a.first_pages = options->first_pages; a.last_pages = options->last_pages;
+    if (status != nullptr) CK(cudaMemsetAsync(a.status, 0, sizeof(int32_t) * a.units, st));
+    compactor::set_chain_for(0);
+    CK(launch_paged_select(a, st));
+    return COMPACTOR_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Norms and rotation.
+extern "C" int compactor_norm_rope(const compactor_norm_rope_options* options, int64_t tokens, compactor_rows q, compactor_rows k,
+                                   const void* q_weight, const void* k_weight, const int32_t* positions, const float* inv_freq,
+                                   compactor_rows q_out, compactor_rows k_out, compactor_rows k_plain_out, void* stream) {
+    const compactor_norm_rope_options* o = options;
+    if (o == nullptr || tokens < 0 || tokens > 0x7fffffffLL || o->q_heads < 0 || o->k_heads < 0 || o->q_heads > 65535 || o->k_heads > 65535 ||
+        o->q_heads + o->k_heads < 1 || !(o->eps >= 0.f) || !isfinite(o->eps) || (o->interleaved != 0 && o->interleaved != 1))
+        return COMPACTOR_E_INVALID_ARGUMENT;
+    if (o->d != kD || o->rotary < 0 || o->rotary > kD || (o->rotary & 15) != 0) return COMPACTOR_E_UNSUPPORTED;
+    if (tokens == 0) return COMPACTOR_OK;                             // (of nothing there are no pointers)
+    if (o->rotary > 0 && (positions == nullptr || inv_freq == nullptr || !aligned(positions, 4) || !aligned(inv_freq, 4))) return COMPACTOR_E_INVALID_ARGUMENT;
+    auto out_ok = [&](const compactor_rows& r, int heads) {  // rows must not overlap
+        return rows_ok(r) && (heads == 1 || r.stride_head >= kD) && (tokens == 1 || r.stride_seq >= kD);
+    };
+    if ((o->q_heads > 0 && (!rows_ok(q) || !out_ok(q_out, o->q_heads))) || (o->k_heads > 0 && (!rows_ok(k) || !out_ok(k_out, o->k_heads))) ||
+        (k_plain_out.ptr != nullptr && (o->k_heads == 0 || !out_ok(k_plain_out, o->k_heads))) || !aligned(q_weight, 16) || !aligned(k_weight, 16))
+        return COMPACTOR_E_INVALID_ARGUMENT;
+    RopeArgs a;
+    memset(&a, 0, sizeof(a));
+    a.tokens = tokens; a.q_heads = o->q_heads; a.k_heads = o->k_heads; a.rotary = o->rotary; a.interleaved = o->interleaved; a.eps = o->eps;
+    a.q = static_cast<const __nv_bfloat16*>(q.ptr); a.q_token = q.stride_seq; a.q_head = q.stride_head;
+    a.k = static_cast<const __nv_bfloat16*>(k.ptr); a.k_token = k.stride_seq; a.k_head = k.stride_head;
+    a.q_weight = static_cast<const __nv_bfloat16*>(q_weight); a.k_weight = static_cast<const __nv_bfloat16*>(k_weight);
+    a.positions = positions; a.inv_freq = inv_freq;
+    a.q_out = static_cast<__nv_bfloat16*>(q_out.ptr); a.qo_token = q_out.stride_seq; a.qo_head = q_out.stride_head;
+    a.k_out = static_cast<__nv_bfloat16*>(k_out.ptr); a.ko_token = k_out.stride_seq; a.ko_head = k_out.stride_head;
+    a.k_plain = static_cast<__nv_bfloat16*>(k_plain_out.ptr); a.p_token = k_plain_out.stride_seq; a.p_head = k_plain_out.stride_head;
+    compactor::set_chain_for(0);
+    CK(launch_rope(a, sm_count(), static_cast<cudaStream_t>(stream)));
     return COMPACTOR_OK;
 }

@@ -1,0 +1,494 @@
+// Attention of one new token per sequence over pages that hold rows in 4 bits (quant4.cuh): the first of the two kernels of decode.cu, which
+// says what is computed and how the tiles of a layer are shared out; the second one is the same for both.
+//
+// A token of a unit costs 160 bytes here, 512 there, and the same 4 g d flops: what bounds the kernel is no longer HBM alone but the
+// instructions that make bf16 of codes (two for every pair, and one for every eight codes to bring them into place).  So that they are few:
+//   - a word's codes i and i + 4, masked and put under the exponent of 128, are the bf16 pair 128 + c; one fused multiply-add with (s, -128 s)
+//     makes s c of it, exactly (s has four significant bits).  Which channel is which of the 16 of a matrix instruction is free as long
+//     as queries and keys agree, so that pairs a nibble apart need no shuffling; for V, whose pairs are tokens, one byte permutation
+//     per two words brings the same channels of two tokens side by side;
+//   - lo enters once for a group, not for every channel.  q.k = sum_c q_c s c + sum_groups lo_g (sum of the group's q): one more
+//     matrix instruction per tile with the least values as rows and the sums of the query, in three bf16 terms (24 bits), as columns.
+//     sum_j p_j v_j likewise gets one more instruction with the least values as rows, whose sums are added to the channels at the end.
+// So every product that a matrix instruction sees is exact but for the weights' two bf16 terms, as in the other kernel.
+//
+// The rows of a page lie back to back, so that a tile of 16 is 1280 bytes in one piece (two on pages of 8): five 16-byte copies per lane for
+// K and V together.
+#include "decode.cuh"
+#include "quant4.cuh"
+
+namespace compactor {
+namespace {
+
+using namespace decode;
+
+constexpr int kTileBytes = kTile * kRow4;              // of K, or of V
+constexpr int kStageBytes = 2 * kTileBytes;
+
+template <int NG> struct Four {
+    static constexpr int kWarps = NG == 1 ? kDecode4Warps : kDecode4WarpsWide;
+    static constexpr int kThreads = kWarps * 32;
+    static constexpr int kStages = NG == 1 ? 4 : 8;    // 164 KB either way
+    static constexpr size_t kSmemBytes = (size_t)kWarps * kStages * kStageBytes;
+};
+
+// The 32 channels that a lane multiplies: 32 g + 8 tig + 0..7, of head t * 8 + gid.
+template <int NG>
+__device__ __forceinline__ void load_queries(const DecodeArgs& a, const Cursor& c, uint4 (&q)[NG][4], int lane) {
+    const int gid = lane >> 2, tig = lane & 3;
+    const int h = c.unit / a.c.batch, b = c.unit - h * a.c.batch;
+    const int head0 = h * a.g + c.grp * kDecodeHeads, heads = min(kDecodeHeads, a.g - c.grp * kDecodeHeads);
+#pragma unroll
+    for (int t = 0; t < NG; ++t) {
+        const bool on = t * 8 + gid < heads;
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + b * a.q_seq + (long long)(head0 + (on ? t * 8 + gid : 0)) * a.q_head);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            q[t][g] = src[4 * g + tig];
+            if (!on) q[t][g] = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+}
+
+// B operands of a unit's queries: channels (2 st, 2 st + 4) and (2 st + 1, 2 st + 5) of the lane's eight of group g, and the sums of a
+// group's channels, group tig, as three bf16 terms.
+template <int NG>
+__device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t (&qf)[NG][4][2][2], uint32_t (&qs)[NG][2], int lane) {
+    const int tig = lane & 3;
+#pragma unroll
+    for (int t = 0; t < NG; ++t) {
+        float mine = 0.f;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint4 x = q[t][g];
+            qf[t][g][0][0] = __byte_perm(x.x, x.z, 0x5410); qf[t][g][0][1] = __byte_perm(x.x, x.z, 0x7632);
+            qf[t][g][1][0] = __byte_perm(x.y, x.w, 0x5410); qf[t][g][1][1] = __byte_perm(x.y, x.w, 0x7632);
+            float sum = ((bf16_lo(x.x) + bf16_hi(x.x)) + (bf16_lo(x.y) + bf16_hi(x.y))) + ((bf16_lo(x.z) + bf16_hi(x.z)) + (bf16_lo(x.w) + bf16_hi(x.w)));
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            if (g == tig) mine = sum;
+        }
+        const float t0 = __bfloat162float(__float2bfloat16_rn(mine)), r0 = mine - t0;
+        const float t1 = __bfloat162float(__float2bfloat16_rn(r0)), t2 = r0 - t1;
+        qs[t][0] = pack_bf16(t0, t1);
+        qs[t][1] = pack_bf16(t2, 0.f);
+    }
+}
+
+template <int NG>
+__global__ void __launch_bounds__(Four<NG>::kThreads, 1)
+decode4_kernel(const __grid_constant__ DecodeArgs a) {
+    constexpr int kWarps = Four<NG>::kWarps, kThreads = Four<NG>::kThreads, kStages = Four<NG>::kStages;
+    extern __shared__ __align__(1024) unsigned char ring[];
+    __shared__ int cum[kThreads + 1];
+    __shared__ int warp_sum[kWarps];
+    __shared__ int bad[kWarps][kStages];
+    __shared__ int new_page[kWarps][kStages];
+    __shared__ int live[kUnitsInSmem];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int gid = lane >> 2, tig = lane & 3;
+    pdl_wait();
+
+    // cost before each thread's run of units
+    const int per = (a.units + kThreads - 1) / kThreads;
+    const int u0 = min(a.units, tid * per), u1 = min(a.units, u0 + per);
+    int mine = 0;
+    for (int u = u0; u < u1; ++u) {
+        const int n = live_tokens(a, u);
+        if (u < kUnitsInSmem) live[u] = n;
+        mine += cost_of(n);
+    }
+    int incl = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+    }
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) before += w < warp ? warp_sum[w] : 0;
+    cum[tid + 1] = before + incl;
+    if (tid == 0) cum[0] = 0;
+    __syncthreads();
+    const int all = cum[kThreads];
+    if (blockIdx.x == 0) {                                   // for the second kernel, and the units that are refused
+        int at = cum[tid];
+        for (int u = u0; u < u1; ++u) {
+            a.prefix[u] = at;
+            at += cost_of(live_tokens(a, u));
+            const int n = __ldcg(a.lengths + u);
+            if (a.status != nullptr && n >= 0 && (long long)n + (a.k_new != nullptr) > a.capacity)
+                atomicOr(a.status + u, COMPACTOR_STATUS_CAPACITY);
+        }
+        if (tid == 0) a.prefix[a.units] = all;
+    }
+    const int total = all * a.groups;
+    const int workers = active_workers(a, total);
+    const int worker = warp * gridDim.x + blockIdx.x;        // neighbouring workers on different SMs: a small call uses them all
+    if (worker >= workers) return;
+    const Share share(total, workers);
+    const int begin = share.begin(worker);
+    int left_p = share.size(worker);                         // cost that the producer has not passed yet
+
+    // the unit that holds place `begin`
+    Cursor start;
+    {
+        int lo = 0, hi = kThreads;                           // cum[lo] * groups <= begin < cum[hi] * groups
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (cum[mid] * a.groups <= begin) lo = mid; else hi = mid;
+        }
+        int left = begin - cum[lo] * a.groups;
+        auto tokens_of = [&](int unit) { return unit < kUnitsInSmem ? live[unit] : live_tokens(a, unit); };
+        int u = lo * per, n = tokens_of(u);
+        while (left >= cost_of(n) * a.groups) {
+            left -= cost_of(n) * a.groups;
+            n = tokens_of(++u);
+        }
+        start.unit = u; start.tokens = n; start.tiles = tiles_of(n);
+        start.grp = left / cost_of(n);
+        start.tile = left - start.grp * cost_of(n) - kUnitCost;
+        if (start.tile < 0) {                                // within the unit's head: the first tile is the next
+            left_p += start.tile;
+            start.tile = 0;
+            if (left_p <= 0) return;
+        }
+    }
+    int left_c = left_p;                                     // cost that the consumer has not passed yet
+
+    unsigned char* my_ring = ring + (size_t)warp * kStages * kStageBytes;
+    const uint32_t ring_s = smem_u32(my_ring);
+
+    // ---- producer: one tile into a stage.  Lane l copies the 16-byte pieces l, l + 32 and l + 64 of the 80 of either tile; pieces 0 .. 39 are rows 0 .. 7.
+    // Page ids and queries are asked for ahead as in the other kernel: 64 page ids of the unit (lane l holds entries e0 + l and e0 + 32 + l), the
+    // first 32 of the unit after it, and the queries of a unit when its first tile is issued.
+    Cursor pc = start, nc = start;
+    int e0 = (pc.tile * kTile) >> a.c.page_shift;
+    int ids = page_ids(a, pc, e0, lane), ids_after = page_ids(a, pc, e0 + 32, lane), ids_next_unit = -1;
+    uint4 qn[NG][4];
+    int q_unit = pc.unit, q_grp = pc.grp;                    // whose queries qn holds
+    bool q_waiting = true;
+    load_queries<NG>(a, pc, qn, lane);
+    if (nc.next_unit(a, live)) ids_next_unit = page_ids(a, nc, 0, lane);
+    const long long v_from_k = reinterpret_cast<const char*>(a.c.v) - reinterpret_cast<const char*>(a.c.k);
+    int in_stage = 0;
+    auto issue = [&]() {
+        if (left_p > 0) {
+            const int stage = in_stage;
+            const int unit = pc.unit, n = pc.tokens, base = pc.tile * kTile;
+            const int cached = n - (a.k_new != nullptr);     // tokens whose rows are in pages
+            const int e = base >> a.c.page_shift;
+            if (e + 1 >= e0 + 32) {                          // (pages of 8 tokens: a tile has two)
+                e0 += 32;
+                if (e < e0) {                                // a tile on the seam keeps one entry of the old run
+                    const int seam = __shfl_sync(0xffffffffu, ids, 31);
+                    const int rest = __shfl_up_sync(0xffffffffu, ids_after, 1);
+                    ids = lane == 0 ? seam : rest;
+                    e0 -= 1;
+                    ids_after = page_ids(a, pc, e0 + 32, lane);
+                } else {
+                    ids = ids_after;
+                    ids_after = page_ids(a, pc, e0 + 32, lane);
+                }
+            }
+            int p0 = __shfl_sync(0xffffffffu, ids, e - e0), p1 = __shfl_sync(0xffffffffu, ids, ((base + 8) >> a.c.page_shift) - e0);
+            if ((unsigned)p0 >= (unsigned)a.c.n_pages) p0 = -1;
+            if ((unsigned)p1 >= (unsigned)a.c.n_pages || base + 8 >= n) p1 = -1;
+            const uint32_t ks = ring_s + stage * kStageBytes + lane * 16;
+            const int fresh_row = cached < n ? cached - base : -1;           // the new token's row of this tile, if it has it
+            // where this lane's pieces are, as if each half's run of 640 bytes went on before and behind it
+            const char* src0 = reinterpret_cast<const char*>(a.c.k + row_in_pool(a.c, max(p0, 0), base)) + lane * 16;
+            const char* src1 = reinterpret_cast<const char*>(a.c.k + row_in_pool(a.c, max(p1, 0), base + 8)) + lane * 16 - 8 * kRow4;
+            const char* mid = lane < 8 ? src0 : src1;
+            if (base + kTile <= cached && p0 >= 0 && p1 >= 0) {              // all rows come from pages
+                cp_async16(ks, src0);
+                cp_async16(ks + kTileBytes, src0 + v_from_k);
+                cp_async16(ks + 512, mid + 512);
+                cp_async16(ks + kTileBytes + 512, mid + 512 + v_from_k);
+                if (lane < 16) {
+                    cp_async16(ks + 1024, src1 + 1024);
+                    cp_async16(ks + kTileBytes + 1024, src1 + 1024 + v_from_k);
+                }
+            } else {                                         // rows that are in no page, or behind the last token, are zeros
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    const int at = lane + 32 * i, tok = base + at / 5;
+                    if (at >= kTileBytes / 16) continue;
+                    const bool on = tok < cached && (at < 40 ? p0 : p1) >= 0;
+                    const char* src = on ? (at < 40 ? src0 : src1) + 512 * i : reinterpret_cast<const char*>(a.c.k);
+                    cp_async16(ks + 512 * i, src, on ? 16 : 0);
+                    cp_async16(ks + kTileBytes + 512 * i, src + v_from_k, on ? 16 : 0);
+                }
+            }
+            if (lane == 0) {
+                const int bits = (p0 < 0 && base < cached ? 1 : 0) | (p1 < 0 && base + 8 < cached ? 2 : 0);
+                const int np = fresh_row < 8 ? p0 : p1;
+                bad[warp][stage] = bits;
+                new_page[warp][stage] = np;
+                if (a.status != nullptr && (bits != 0 || (fresh_row >= 0 && fresh_row < kTile && np < 0)))
+                    atomicOr(a.status + unit, COMPACTOR_STATUS_PAGE);
+            }
+            in_stage = stage + 1 == kStages ? 0 : stage + 1;
+            --left_p;
+            if (++pc.tile == pc.tiles && (left_p -= kUnitCost) > 0) {
+                pc = nc;
+                e0 = 0;
+                ids = ids_next_unit;
+                ids_after = page_ids(a, pc, 32, lane);
+                if (nc.next_unit(a, live)) ids_next_unit = page_ids(a, nc, 0, lane);
+                if (!q_waiting) {
+                    load_queries<NG>(a, pc, qn, lane);
+                    q_unit = pc.unit; q_grp = pc.grp; q_waiting = true;
+                }
+            }
+        }
+        cp_commit();
+    };
+#pragma unroll 1
+    for (int s = 0; s < kStages; ++s) issue();
+
+    // ---- consumer
+    Cursor cc = start;
+    const float scale2 = a.scale * kLog2e;
+    const float cap_in = a.softcap > 0.f ? a.scale / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
+    uint32_t qf[NG][4][2][2], qs[NG][2];
+    float o[NG][8][4], ol[NG][4];
+    float mx[NG][2], sum[NG][2];
+    bool fresh = true;
+    int first_tile = 0, head0 = 0, heads = 0, stage = 0;
+
+    while (true) {
+        if (fresh) {                                         // a new unit or group: its queries
+            fresh = false;
+            first_tile = cc.tile;
+            head0 = cc.unit / a.c.batch * a.g + cc.grp * kDecodeHeads;
+            heads = min(kDecodeHeads, a.g - cc.grp * kDecodeHeads);
+            if (q_waiting && q_unit == cc.unit && q_grp == cc.grp) {
+                q_waiting = false;
+                query_operands<NG>(qn, qf, qs, lane);
+            } else {
+                uint4 q[NG][4];
+                load_queries<NG>(a, cc, q, lane);
+                query_operands<NG>(q, qf, qs, lane);
+            }
+#pragma unroll
+            for (int t = 0; t < NG; ++t) {
+#pragma unroll
+                for (int s = 0; s < 8; ++s) o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.f;
+                ol[t][0] = ol[t][1] = ol[t][2] = ol[t][3] = 0.f;
+                mx[t][0] = mx[t][1] = -INFINITY;
+                sum[t][0] = sum[t][1] = 0.f;
+            }
+        }
+        if (left_c <= kStages) pdl_trigger();                // the second kernel's blocks are let in when the tiles run out
+        cp_wait<kStages - 1>();
+        __syncwarp();
+        unsigned char* tile_k = my_ring + stage * kStageBytes;
+        const int base = cc.tile * kTile;
+        const int bits = bad[warp][stage];
+        const int cached = cc.tokens - (a.k_new != nullptr);
+        // the new token's rows: held in 4 bits first, in the tile and, by the first group, in its page; lanes 0 .. 15 have K's, the others V's
+        const int fresh_row = cached < cc.tokens ? cached - base : -1;
+        if (fresh_row >= 0 && fresh_row < kTile) {
+            const int h = cc.unit / a.c.batch, b = cc.unit - h * a.c.batch, piece = lane & 15;
+            const __nv_bfloat16* src = lane < 16 ? a.k_new + b * a.kn_seq + h * a.kn_head : a.v_new + b * a.vn_seq + h * a.vn_head;
+            uint32_t param;
+            const uint32_t codes = quantise8(*(reinterpret_cast<const uint4*>(src) + piece), param);
+            unsigned char* row = tile_k + (lane < 16 ? 0 : kTileBytes) + fresh_row * kRow4;
+            *reinterpret_cast<uint32_t*>(row + 4 * piece) = codes;
+            if ((piece & 3) == 0) *reinterpret_cast<uint32_t*>(row + kRow4Codes + piece) = param;
+            const int page = new_page[warp][stage];
+            if (page >= 0 && cc.grp == 0) {
+                row = reinterpret_cast<unsigned char*>((lane < 16 ? a.c.k : a.c.v) + row_in_pool(a.c, page, cached));
+                *reinterpret_cast<uint32_t*>(row + 4 * piece) = codes;
+                if ((piece & 3) == 0) *reinterpret_cast<uint32_t*>(row + kRow4Codes + piece) = param;
+                const long long at = slot_in_pool(a.c, page, cached);
+                if (lane == 0 && a.c.positions != nullptr)
+                    a.c.positions[at] = a.new_positions != nullptr ? a.new_positions[cc.unit % a.c.batch] : cached;
+                if (lane == 0 && a.c.mass != nullptr && !a.accumulate) a.c.mass[at] = 0.f;
+            }
+            __syncwarp();
+        }
+
+        // S^T: 16 tokens x 8 NG heads
+        float s[NG][4];
+#pragma unroll
+        for (int t = 0; t < NG; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+        {
+            const unsigned char* ra = tile_k + gid * kRow4;
+            const unsigned char* rb = ra + 8 * kRow4;
+            const uint4 pa = *reinterpret_cast<const uint4*>(ra + kRow4Codes), pb = *reinterpret_cast<const uint4*>(rb + kRow4Codes);
+            const uint32_t para[4] = {pa.x, pa.y, pa.z, pa.w}, parb[4] = {pb.x, pb.y, pb.z, pb.w};
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t wa = *reinterpret_cast<const uint32_t*>(ra + 16 * g + 4 * tig), wb = *reinterpret_cast<const uint32_t*>(rb + 16 * g + 4 * tig);
+                const uint32_t sa = __byte_perm(para[g], 0u, 0x1010), sb = __byte_perm(parb[g], 0u, 0x1010);
+                const uint32_t ma = fma2(sa, 0xc300c300u, 0x80008000u), mb = fma2(sb, 0xc300c300u, 0x80008000u);     // -128 s
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const uint32_t kf[4] = {fma2(codes128(wa, 2 * st), sa, ma), fma2(codes128(wb, 2 * st), sb, mb),
+                                            fma2(codes128(wa, 2 * st + 1), sa, ma), fma2(codes128(wb, 2 * st + 1), sb, mb)};
+#pragma unroll
+                    for (int t = 0; t < NG; ++t) mma(s[t], kf, qf[t][g][st][0], qf[t][g][st][1]);
+                }
+            }
+            const uint32_t la = *reinterpret_cast<const uint32_t*>(ra + kRow4Codes + 4 * tig), lb = *reinterpret_cast<const uint32_t*>(rb + kRow4Codes + 4 * tig);
+            const uint32_t la2 = __byte_perm(la, 0u, 0x3232), lb2 = __byte_perm(lb, 0u, 0x3232);
+            const uint32_t lf[4] = {la2, lb2, la2, lb2};
+#pragma unroll
+            for (int t = 0; t < NG; ++t) mma(s[t], lf, qs[t][0], qs[t][1]);
+        }
+        // scores in base 2; what does not count gets -inf
+        const int ta = base + gid, tb = ta + 8;
+        const bool la = ta < cc.tokens && !((bits & 1) && ta < cached), lb = tb < cc.tokens && !((bits & 2) && tb < cached);
+        uint32_t pf[NG][2], pl[NG][2];                       // weights: first and second term
+        bool grew = false;
+        float scale_by[NG][2];
+#pragma unroll
+        for (int t = 0; t < NG; ++t) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float y = a.softcap > 0.f ? cap_out * tanhf(s[t][c] * cap_in) : s[t][c] * scale2;
+                s[t][c] = (c < 2 ? la : lb) ? y : -INFINITY;
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float m = fmaxf(s[t][c], s[t][c + 2]);
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                m = fmaxf(m, mx[t][c]);
+                grew |= m > mx[t][c];
+                const float ref = m == -INFINITY ? 0.f : m;
+                scale_by[t][c] = ex2f(mx[t][c] - ref);       // 0 for the first tile, 1 where the maximum stays
+                mx[t][c] = m;
+                const float pa = ex2f(s[t][c] - ref), pb = ex2f(s[t][c + 2] - ref);
+                sum[t][c] = sum[t][c] * scale_by[t][c] + (pa + pb);
+                if (c == 0) { pf[t][0] = __float_as_uint(pa); pf[t][1] = __float_as_uint(pb); }
+                else {
+                    split_bf16(__uint_as_float(pf[t][0]), pa, pf[t][0], pl[t][0]);
+                    split_bf16(__uint_as_float(pf[t][1]), pb, pf[t][1], pl[t][1]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { pf[t][i] = transpose8x8(pf[t][i]); pl[t][i] = transpose8x8(pl[t][i]); }
+        }
+        if (a.accumulate) {                                  // kept until the sum over the whole unit is known
+            float* col = a.scores + ((long long)cc.unit * a.g + cc.grp * kDecodeHeads + 2 * tig) * a.unit_rows + base + gid;
+#pragma unroll
+            for (int t = 0; t < NG; ++t)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (t * 8 + 2 * tig + c < heads) {       // 32 bytes of a head's scores per group of eight lanes
+                        float* at = col + (long long)(t * 8 + c) * a.unit_rows;
+                        at[0] = s[t][c];
+                        at[8] = s[t][c + 2];
+                    }
+        }
+        if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+            for (int t = 0; t < NG; ++t) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    o[t][j][0] *= scale_by[t][0]; o[t][j][1] *= scale_by[t][1];
+                    o[t][j][2] *= scale_by[t][0]; o[t][j][3] *= scale_by[t][1];
+                }
+                ol[t][0] *= scale_by[t][0]; ol[t][1] *= scale_by[t][1];
+            }
+        }
+        // O^T += V^T P^T: 128 channels x 8 NG heads.  The lane has the 16 channels 16 gid + 0..15 of tokens 2 tig, + 1, + 8 and + 9; row gid of the j-th
+        // instruction is channel 16 gid + j, row gid + 8 is 16 gid + 8 + j.
+        {
+            const unsigned char* r = tile_k + kTileBytes + 2 * tig * kRow4;
+            uint2 v[4];
+            uint32_t par[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned char* row = r + ((i & 1) + (i >> 1) * 8) * kRow4;
+                v[i] = *reinterpret_cast<const uint2*>(row + 8 * gid);
+                par[i] = *reinterpret_cast<const uint32_t*>(row + kRow4Codes + 4 * (gid >> 1));
+            }
+            const uint32_t s0 = __byte_perm(par[0], par[1], 0x5410), s1 = __byte_perm(par[2], par[3], 0x5410);
+            const uint32_t m0 = fma2(s0, 0xc300c300u, 0x80008000u), m1 = fma2(s1, 0xc300c300u, 0x80008000u);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const unsigned sel = j < 4 ? 0x5410 : 0x7632;
+                const uint32_t vf[4] = {fma2(codes128(__byte_perm(v[0].x, v[1].x, sel), j & 3), s0, m0), fma2(codes128(__byte_perm(v[0].y, v[1].y, sel), j & 3), s0, m0),
+                                        fma2(codes128(__byte_perm(v[2].x, v[3].x, sel), j & 3), s1, m1), fma2(codes128(__byte_perm(v[2].y, v[3].y, sel), j & 3), s1, m1)};
+#pragma unroll
+                for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pf[t][0], pf[t][1]);
+#pragma unroll
+                for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pl[t][0], pl[t][1]);
+            }
+            const uint32_t lf[4] = {__byte_perm(par[0], par[1], 0x7632), 0u, __byte_perm(par[2], par[3], 0x7632), 0u};
+#pragma unroll
+            for (int t = 0; t < NG; ++t) mma(ol[t], lf, pf[t][0], pf[t][1]);
+#pragma unroll
+            for (int t = 0; t < NG; ++t) mma(ol[t], lf, pl[t][0], pl[t][1]);
+        }
+        __syncwarp();
+        issue();
+
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        --left_c;
+        const bool unit_ends = ++cc.tile == cc.tiles;
+        if (unit_ends) left_c -= kUnitCost;
+        if (unit_ends || left_c <= 0) {                      // hand over what this warp has of the unit
+            const long long slot = (long long)worker + cc.unit * a.groups + cc.grp;
+            const bool whole = unit_ends && first_tile == 0;
+            const int b = cc.unit % a.c.batch, gg = min(a.g, kDecodeHeads);
+#pragma unroll
+            for (int t = 0; t < NG; ++t)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float l = sum[t][c];
+                    l += __shfl_xor_sync(0xffffffffu, l, 4);
+                    l += __shfl_xor_sync(0xffffffffu, l, 8);
+                    l += __shfl_xor_sync(0xffffffffu, l, 16);
+                    const int head = t * 8 + 2 * tig + c;
+                    if (head >= heads) continue;
+                    if (gid == 0) {
+                        a.ml[slot * 32 + head] = mx[t][c];
+                        a.ml[slot * 32 + 16 + head] = l;
+                    }
+                    float x[16];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) { x[j] = o[t][j][c] + ol[t][c]; x[8 + j] = o[t][j][c + 2] + ol[t][c]; }
+                    if (whole) {
+                        const float inv = l == 0.f ? 0.f : 1.f / l;
+                        uint4* dst = reinterpret_cast<uint4*>(a.out + b * a.out_seq + (long long)(head0 + head) * a.out_head + 16 * gid);
+#pragma unroll
+                        for (int i = 0; i < 16; i += 8)
+                            dst[i / 8] = make_uint4(pack_bf16(x[i] * inv, x[i + 1] * inv), pack_bf16(x[i + 2] * inv, x[i + 3] * inv),
+                                                    pack_bf16(x[i + 4] * inv, x[i + 5] * inv), pack_bf16(x[i + 6] * inv, x[i + 7] * inv));
+                        if (gid == 0 && a.lse != nullptr)
+                            a.lse[(long long)b * (a.c.heads * a.g) + head0 + head] = l == 0.f ? -INFINITY : kLn2 * (mx[t][c] + log2f(l));
+                    } else {
+                        float4* dst = reinterpret_cast<float4*>(a.o + (slot * gg + head) * kD + 16 * gid);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) dst[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                    }
+                }
+            if (left_c <= 0) return;
+            fresh = true;
+            cc.next_unit(a, live);
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_decode4(const DecodeArgs& a, cudaStream_t stream) {
+    static std::atomic<unsigned long long> done[2];
+    const bool narrow = a.g <= 8;
+    auto kernel = narrow ? decode4_kernel<1> : decode4_kernel<2>;
+    const int warps = narrow ? kDecode4Warps : kDecode4WarpsWide;
+    const size_t smem = narrow ? Four<1>::kSmemBytes : Four<2>::kSmemBytes;
+    const cudaError_t e = allow_smem(kernel, (int)smem, done[narrow ? 0 : 1]);
+    if (e != cudaSuccess) return e;
+    return launch_chained(kPdlOther, kernel, dim3(a.workers / warps), dim3(warps * 32), smem, stream, a);
+}
+
+}  // namespace compactor

@@ -1,6 +1,7 @@
 // The paged cache's two copying operators: filling pages with the rows that a selection kept, and evicting the tokens of
 // least accumulated attention weight.  Both move whole 256-byte rows as 16-byte pieces, bit for bit.
 #include "paged.cuh"
+#include "quant4.cuh"
 
 #include <cooperative_groups.h>
 
@@ -56,7 +57,7 @@ __global__ void fill_lengths_kernel(const __grid_constant__ FillArgs a, const __
     write_lengths(a, t, (long long)blockIdx.x * blockDim.x + threadIdx.x);
 }
 
-template <bool ACROSS>
+template <bool ACROSS, bool FOUR>
 __global__ void __launch_bounds__(kFillThreads)
 fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTables t, int row_blocks) {
     __shared__ long long src_k[kFillRows], src_v[kFillRows], dst[kFillRows];       // elements; dst < 0: the row is skipped
@@ -117,7 +118,8 @@ fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTabl
     const int piece = tid & 15, sub = tid >> 4;
     const int rows_here = (int)min((long long)kFillRows, end - row0);
 #pragma unroll 1
-    for (int r0 = sub; r0 < rows_here; r0 += kFillRowsPerIter * kFillBatch) {
+    for (int first = 0; first < rows_here; first += kFillRowsPerIter * kFillBatch) {
+        const int r0 = first + sub;
         uint4 kv[kFillBatch], vv[kFillBatch];
 #pragma unroll
         for (int u = 0; u < kFillBatch; ++u) {               // without a condition, so that they are in flight together
@@ -128,6 +130,20 @@ fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTabl
 #pragma unroll
         for (int u = 0; u < kFillBatch; ++u) {
             const int r = r0 + u * kFillRowsPerIter;
+            if (FOUR) {
+                uint32_t kp, vp;
+                const uint32_t kc = quantise8(kv[u], kp), vc = quantise8(vv[u], vp);
+                if (r >= rows_here || dst[r] < 0) continue;
+                unsigned char* k = reinterpret_cast<unsigned char*>(a.c.k + dst[r]);
+                unsigned char* v = reinterpret_cast<unsigned char*>(a.c.v + dst[r]);
+                *(reinterpret_cast<uint32_t*>(k) + piece) = kc;
+                *(reinterpret_cast<uint32_t*>(v) + piece) = vc;
+                if ((piece & 3) == 0) {
+                    *reinterpret_cast<uint32_t*>(k + kRow4Codes + piece) = kp;
+                    *reinterpret_cast<uint32_t*>(v + kRow4Codes + piece) = vp;
+                }
+                continue;
+            }
             if (r >= rows_here || dst[r] < 0) continue;
             *(reinterpret_cast<uint4*>(a.c.k + dst[r]) + piece) = kv[u];
             *(reinterpret_cast<uint4*>(a.c.v + dst[r]) + piece) = vv[u];
@@ -425,7 +441,8 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
     int total = 0;
     for (int r = 0; r < ranks; ++r) total += s.rank_holes[r];
     const int j0 = (int)((long long)rank * total / ranks), j1 = (int)((long long)(rank + 1) * total / ranks);
-    const int piece = lane & 15;
+    const bool on = (lane & 15) < a.c.row_pieces;            // (of a row in 4 bits five lanes move the pieces, the others read the last once more)
+    const int piece = min(lane & 15, a.c.row_pieces - 1);
     __nv_bfloat16* pool = lane < 16 ? a.c.k : a.c.v;
     for (int jb = j0; jb < j1; jb += kThreads) {
         const int batch = min(kThreads, j1 - jb);
@@ -456,7 +473,7 @@ __device__ __forceinline__ void evict_unit(const EvictArgs& a, int slice_cap, in
 #pragma unroll
             for (int k = 0; k < kRowBatch; ++k) {
                 if (i + k >= batch) break;
-                *(reinterpret_cast<uint4*>(pool + to[k]) + piece) = x[k];
+                if (on) *(reinterpret_cast<uint4*>(pool + to[k]) + piece) = x[k];
             }
         }
         __syncthreads();
@@ -535,7 +552,9 @@ cudaError_t launch_paged_fill(const FillArgs& a, const FillTables& t, cudaStream
     if (rows > 0) {
         const int row_blocks = (int)((rows + kFillRows - 1) / kFillRows);
         const dim3 grid((unsigned)(row_blocks + (lengths && !apart ? 1 : 0)), across ? a.layers : a.layers * a.c.heads);
-        const cudaError_t e = launch_chained(kPdlOther, across ? fill_kernel<true> : fill_kernel<false>, grid, dim3(kFillThreads), 0, stream,
+        const auto kernel = a.four ? (across ? fill_kernel<true, true> : fill_kernel<false, true>)
+                                   : (across ? fill_kernel<true, false> : fill_kernel<false, false>);
+        const cudaError_t e = launch_chained(kPdlOther, kernel, grid, dim3(kFillThreads), 0, stream,
                                              a, t, row_blocks);
         if (e != cudaSuccess) return e;
     }

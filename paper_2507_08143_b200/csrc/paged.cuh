@@ -16,6 +16,7 @@ struct Paged {
     int n_pages, max_pages;
     int page_shift;                        // page_tokens = 1 << page_shift
     int layers, heads, batch;
+    int row_pieces;                        // 16-byte pieces of a row: 16, or 5 where rows are held in 4 bits (strides are then in units of 2 bytes)
 };
 
 // Chained kernels are already running while their predecessor still writes.  What they read after pdl_wait() they read plainly; never
@@ -69,6 +70,7 @@ struct FillArgs {
     const int* lengths;                    // [units of the cache] or null (all empty)
     int* lengths_out;
     int* status;
+    int four;                              // rows are held in 4 bits
 };
 cudaError_t launch_paged_fill(const FillArgs& a, const FillTables& t, cudaStream_t stream);
 
@@ -93,6 +95,8 @@ struct DecodeArgs {
     float scale, softcap;                  // softcap <= 0: none
     int units;
     int workers;                           // warps that share the tokens
+    int busy_workers;                      // the same where each gets many tiles
+    int four;                              // rows are held in 4 bits
     int* prefix;                           // workspace: [units + 1] cost before each unit
     float* ml;                             // workspace: [workers + units * groups][2][16] running maximum and sum
     float* o;                              // workspace: [workers + units * groups][min(g, 16)][128]
@@ -101,10 +105,61 @@ struct DecodeArgs {
 };
 constexpr int kDecodeTile = 16;            // tokens per tile
 constexpr int kDecodeWarps = 8;
+constexpr int kDecode4Warps = 16;          // of the kernel for rows in 4 bits, up to 8 query heads (registers: 128 each)
+constexpr int kDecode4WarpsWide = 8;       // and beyond
 constexpr int kDecodeUnitCost = 3;         // tiles that entering a unit counts for when the work is shared out
 constexpr int kDecodeHeads = 16;           // query heads that one warp serves at once
 constexpr int kDecodeMassUnitCost = 64;    // the same, in the kernel that adds the weights
 cudaError_t launch_paged_attention(const DecodeArgs& a, int sm_count, cudaStream_t stream);
+cudaError_t launch_decode4(const DecodeArgs& a, cudaStream_t stream);     // its first kernel for rows in 4 bits
+
+// Rows out of the pages into dense tensors.
+struct ReadTables { int cu_seqlens[kFillSeqs + 1]; };
+struct ReadArgs {
+    Paged c;
+    __nv_bfloat16* k;
+    __nv_bfloat16* v;
+    long long k_layer, k_head, k_token, v_layer, v_head, v_token;
+    int first_layer, layers;
+    int b0, nb;                            // sequences of this launch
+    const int* first;                      // [units of the cache] or null (0)
+    const int* lengths;
+    int* status;
+    int four;
+};
+cudaError_t launch_paged_read(const ReadArgs& a, const ReadTables& t, cudaStream_t stream);
+
+// Least and greatest key of every page.
+struct BoundsArgs {
+    Paged c;
+    int first_unit, units;
+    int capacity;                          // most tokens of a unit
+    const int* first;                      // [units of the cache] or null (0): pages before this token's stay as they are
+    const int* lengths;
+    __nv_bfloat16* bounds;                 // [n_pages][2][128]
+    int* status;
+    int four;
+};
+cudaError_t launch_paged_bounds(const BoundsArgs& a, cudaStream_t stream);
+
+// Choice of pages for the queries of one new token per sequence.
+struct SelectArgs {
+    Paged c;                               // table, lengths and status start at the layer's first unit
+    const __nv_bfloat16* q;
+    long long q_seq, q_head;
+    const __nv_bfloat16* k_new;            // null: nothing is going to be appended
+    long long kn_seq, kn_head;
+    const int* lengths;
+    __nv_bfloat16* bounds;
+    int* table_out;                        // [units][pages]
+    int* lengths_out;                      // [units]
+    int* status;
+    uint32_t* keys;                        // workspace: [units][unit_pages]
+    int g, units, capacity, unit_pages;
+    int pages, first_pages, last_pages;
+};
+constexpr int kSelectMaxPages = 49152;     // most pages of a unit: their keys lie in shared memory
+cudaError_t launch_paged_select(const SelectArgs& a, cudaStream_t stream);
 
 struct EvictArgs {
     Paged c;
