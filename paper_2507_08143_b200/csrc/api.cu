@@ -1328,7 +1328,7 @@ int bounds(bool four, const compactor_paged_cache* cache, int32_t first_layer, i
     a.first = first; a.lengths = lengths; a.bounds = static_cast<__nv_bfloat16*>(bounds_out); a.status = status; a.four = four;
     if (status != nullptr) CK(cudaMemsetAsync(status + a.first_unit, 0, sizeof(int32_t) * a.units, st));
     compactor::set_chain_for(0);
-    CK(launch_paged_bounds(a, st));
+    CK(launch_paged_bounds(a, sm_count(), st));
     return COMPACTOR_OK;
 }
 

@@ -50,8 +50,8 @@ __device__ __forceinline__ void load_queries(const DecodeArgs& a, const Cursor& 
     }
 }
 
-// B operands of a unit's queries: channels (2 st, 2 st + 4) and (2 st + 1, 2 st + 5) of the lane's eight of group g, and the sums of a
-// group's channels, group tig, as three bf16 terms.
+// B operands of a unit's queries: channels (st, st + 2) and (st + 4, st + 6) of the lane's eight of group g, and the sums of a group's
+// channels, group tig, as three bf16 terms.
 template <int NG>
 __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t (&qf)[NG][4][2][2], uint32_t (&qs)[NG][2], int lane) {
     const int tig = lane & 3;
@@ -61,8 +61,8 @@ __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const uint4 x = q[t][g];
-            qf[t][g][0][0] = __byte_perm(x.x, x.z, 0x5410); qf[t][g][0][1] = __byte_perm(x.x, x.z, 0x7632);
-            qf[t][g][1][0] = __byte_perm(x.y, x.w, 0x5410); qf[t][g][1][1] = __byte_perm(x.y, x.w, 0x7632);
+            qf[t][g][0][0] = __byte_perm(x.x, x.y, 0x5410); qf[t][g][0][1] = __byte_perm(x.z, x.w, 0x5410);
+            qf[t][g][1][0] = __byte_perm(x.x, x.y, 0x7632); qf[t][g][1][1] = __byte_perm(x.z, x.w, 0x7632);
             float sum = ((bf16_lo(x.x) + bf16_hi(x.x)) + (bf16_lo(x.y) + bf16_hi(x.y))) + ((bf16_lo(x.z) + bf16_hi(x.z)) + (bf16_lo(x.w) + bf16_hi(x.w)));
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
@@ -75,14 +75,19 @@ __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t
     }
 }
 
-template <int NG>
+// Even bytes 0, 1 (or 2, 3) of four codes as 128 + c in bf16, whose last place is 1 there.
+__device__ __forceinline__ uint32_t codes_low(uint32_t x) { return __byte_perm(x, 0x43434343u, 0x4140); }
+__device__ __forceinline__ uint32_t codes_high(uint32_t x) { return __byte_perm(x, 0x43434343u, 0x4342); }
+constexpr uint32_t kNibbles = 0x0f0f0f0fu;
+
+// CAP: scores are capped.  ACC: weights are accumulated.
+template <int NG, bool CAP, bool ACC>
 __global__ void __launch_bounds__(Four<NG>::kThreads, 1)
 decode4_kernel(const __grid_constant__ DecodeArgs a) {
     constexpr int kWarps = Four<NG>::kWarps, kThreads = Four<NG>::kThreads, kStages = Four<NG>::kStages;
     extern __shared__ __align__(1024) unsigned char ring[];
     __shared__ int cum[kThreads + 1];
     __shared__ int warp_sum[kWarps];
-    __shared__ int bad[kWarps][kStages];
     __shared__ int new_page[kWarps][kStages];
     __shared__ int live[kUnitsInSmem];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -162,8 +167,9 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
     const uint32_t ring_s = smem_u32(my_ring);
 
     // ---- producer: one tile into a stage.  Lane l copies the 16-byte pieces l, l + 32 and l + 64 of the 80 of either tile; pieces 0 .. 39 are rows 0 .. 7.
-    // Page ids and queries are asked for ahead as in the other kernel: 64 page ids of the unit (lane l holds entries e0 + l and e0 + 32 + l), the
-    // first 32 of the unit after it, and the queries of a unit when its first tile is issued.
+    // A tile that goes on in the page of the one before it (run > 0) is where that one ended; else its page ids are looked up.  They and the queries are
+    // asked for ahead as in the other kernel: 64 page ids of the unit (lane l holds entries e0 + l and e0 + 32 + l), the first 32 of
+    // the unit after it, and the queries of a unit when its first tile is issued.
     Cursor pc = start, nc = start;
     int e0 = (pc.tile * kTile) >> a.c.page_shift;
     int ids = page_ids(a, pc, e0, lane), ids_after = page_ids(a, pc, e0 + 32, lane), ids_next_unit = -1;
@@ -172,69 +178,86 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
     bool q_waiting = true;
     load_queries<NG>(a, pc, qn, lane);
     if (nc.next_unit(a, live)) ids_next_unit = page_ids(a, nc, 0, lane);
+    const int appended = a.k_new != nullptr ? 1 : 0;
     const long long v_from_k = reinterpret_cast<const char*>(a.c.v) - reinterpret_cast<const char*>(a.c.k);
+    const char* src = nullptr;                               // where the next tile of the page begins, for this lane
+    int run = 0;                                             // tiles left in the page
+    int full = (pc.tokens - appended) / kTile;               // tiles of the unit whose rows are all in pages
+    uint32_t bad = 0;                                        // two bits per stage: a half of its tile is on a page that is none
     int in_stage = 0;
     auto issue = [&]() {
         if (left_p > 0) {
-            const int stage = in_stage;
-            const int unit = pc.unit, n = pc.tokens, base = pc.tile * kTile;
-            const int cached = n - (a.k_new != nullptr);     // tokens whose rows are in pages
-            const int e = base >> a.c.page_shift;
-            if (e + 1 >= e0 + 32) {                          // (pages of 8 tokens: a tile has two)
-                e0 += 32;
-                if (e < e0) {                                // a tile on the seam keeps one entry of the old run
-                    const int seam = __shfl_sync(0xffffffffu, ids, 31);
-                    const int rest = __shfl_up_sync(0xffffffffu, ids_after, 1);
-                    ids = lane == 0 ? seam : rest;
-                    e0 -= 1;
-                    ids_after = page_ids(a, pc, e0 + 32, lane);
-                } else {
-                    ids = ids_after;
-                    ids_after = page_ids(a, pc, e0 + 32, lane);
+            const uint32_t ks = ring_s + in_stage * kStageBytes + lane * 16;
+            bad &= ~(3u << (2 * in_stage));
+            bool whole = pc.tile < full;
+            if (run > 0 && whole) {
+                --run;
+            } else {
+                run = 0;
+                const int base = pc.tile * kTile, n = pc.tokens, cached = n - appended;
+                const int e = base >> a.c.page_shift;
+                if (e + 1 >= e0 + 32) {                      // (pages of 8 tokens: a tile has two)
+                    e0 += 32;
+                    if (e < e0) {                            // a tile on the seam keeps one entry of the old run
+                        const int seam = __shfl_sync(0xffffffffu, ids, 31);
+                        const int rest = __shfl_up_sync(0xffffffffu, ids_after, 1);
+                        ids = lane == 0 ? seam : rest;
+                        e0 -= 1;
+                        ids_after = page_ids(a, pc, e0 + 32, lane);
+                    } else {
+                        ids = ids_after;
+                        ids_after = page_ids(a, pc, e0 + 32, lane);
+                    }
                 }
-            }
-            int p0 = __shfl_sync(0xffffffffu, ids, e - e0), p1 = __shfl_sync(0xffffffffu, ids, ((base + 8) >> a.c.page_shift) - e0);
-            if ((unsigned)p0 >= (unsigned)a.c.n_pages) p0 = -1;
-            if ((unsigned)p1 >= (unsigned)a.c.n_pages || base + 8 >= n) p1 = -1;
-            const uint32_t ks = ring_s + stage * kStageBytes + lane * 16;
-            const int fresh_row = cached < n ? cached - base : -1;           // the new token's row of this tile, if it has it
-            // where this lane's pieces are, as if each half's run of 640 bytes went on before and behind it
-            const char* src0 = reinterpret_cast<const char*>(a.c.k + row_in_pool(a.c, max(p0, 0), base)) + lane * 16;
-            const char* src1 = reinterpret_cast<const char*>(a.c.k + row_in_pool(a.c, max(p1, 0), base + 8)) + lane * 16 - 8 * kRow4;
-            const char* mid = lane < 8 ? src0 : src1;
-            if (base + kTile <= cached && p0 >= 0 && p1 >= 0) {              // all rows come from pages
-                cp_async16(ks, src0);
-                cp_async16(ks + kTileBytes, src0 + v_from_k);
-                cp_async16(ks + 512, mid + 512);
-                cp_async16(ks + kTileBytes + 512, mid + 512 + v_from_k);
-                if (lane < 16) {
-                    cp_async16(ks + 1024, src1 + 1024);
-                    cp_async16(ks + kTileBytes + 1024, src1 + 1024 + v_from_k);
-                }
-            } else {                                         // rows that are in no page, or behind the last token, are zeros
+                int p0 = __shfl_sync(0xffffffffu, ids, e - e0), p1 = __shfl_sync(0xffffffffu, ids, ((base + 8) >> a.c.page_shift) - e0);
+                if ((unsigned)p0 >= (unsigned)a.c.n_pages) p0 = -1;
+                if ((unsigned)p1 >= (unsigned)a.c.n_pages || base + 8 >= n) p1 = -1;
+                src = reinterpret_cast<const char*>(a.c.k + row_in_pool(a.c, max(p0, 0), base)) + lane * 16;
+                if (whole && p0 >= 0 && a.c.page_shift >= 4) {
+                    run = ((1 << a.c.page_shift) - (base & ((1 << a.c.page_shift) - 1))) / kTile - 1;
+                } else {                                     // two pages of 8, or rows that are in no page or behind the last token: zeros
+                    whole = false;
+                    // pieces of the second half, as if its run of 640 bytes had begun before it
+                    const char* src1 = reinterpret_cast<const char*>(a.c.k + row_in_pool(a.c, max(p1, 0), base + 8)) + lane * 16 - 8 * kRow4;
 #pragma unroll
-                for (int i = 0; i < 3; ++i) {
-                    const int at = lane + 32 * i, tok = base + at / 5;
-                    if (at >= kTileBytes / 16) continue;
-                    const bool on = tok < cached && (at < 40 ? p0 : p1) >= 0;
-                    const char* src = on ? (at < 40 ? src0 : src1) + 512 * i : reinterpret_cast<const char*>(a.c.k);
-                    cp_async16(ks + 512 * i, src, on ? 16 : 0);
-                    cp_async16(ks + kTileBytes + 512 * i, src + v_from_k, on ? 16 : 0);
+                    for (int i = 0; i < 3; ++i) {
+                        const int at = lane + 32 * i, tok = base + at / 5;
+                        if (at >= kTileBytes / 16) continue;
+                        const bool on = tok < cached && (at < 40 ? p0 : p1) >= 0;
+                        const char* from = on ? (at < 40 ? src : src1) + 512 * i : reinterpret_cast<const char*>(a.c.k);
+                        cp_async16(ks + 512 * i, from, on ? 16 : 0);
+                        cp_async16(ks + kTileBytes + 512 * i, from + v_from_k, on ? 16 : 0);
+                    }
+                    const int fresh_row = cached < n ? cached - base : -1;   // the new token's row of this tile, if it has it
+                    const uint32_t bits = (p0 < 0 && base < cached ? 1u : 0u) | (p1 < 0 && base + 8 < cached ? 2u : 0u);
+                    const int np = fresh_row < 8 ? p0 : p1;
+                    bad |= bits << (2 * in_stage);
+                    if (lane == 0) {
+                        new_page[warp][in_stage] = np;
+                        if (a.status != nullptr && (bits != 0 || (fresh_row >= 0 && fresh_row < kTile && np < 0)))
+                            atomicOr(a.status + pc.unit, COMPACTOR_STATUS_PAGE);
+                    }
                 }
             }
-            if (lane == 0) {
-                const int bits = (p0 < 0 && base < cached ? 1 : 0) | (p1 < 0 && base + 8 < cached ? 2 : 0);
-                const int np = fresh_row < 8 ? p0 : p1;
-                bad[warp][stage] = bits;
-                new_page[warp][stage] = np;
-                if (a.status != nullptr && (bits != 0 || (fresh_row >= 0 && fresh_row < kTile && np < 0)))
-                    atomicOr(a.status + unit, COMPACTOR_STATUS_PAGE);
+            if (whole) {
+                const char* sv = src + v_from_k;
+                cp_async16(ks, src);
+                cp_async16(ks + kTileBytes, sv);
+                cp_async16(ks + 512, src + 512);
+                cp_async16(ks + kTileBytes + 512, sv + 512);
+                if (lane < 16) {
+                    cp_async16(ks + 1024, src + 1024);
+                    cp_async16(ks + kTileBytes + 1024, sv + 1024);
+                }
+                src += kTileBytes;
             }
-            in_stage = stage + 1 == kStages ? 0 : stage + 1;
+            in_stage = in_stage + 1 == kStages ? 0 : in_stage + 1;
             --left_p;
             if (++pc.tile == pc.tiles && (left_p -= kUnitCost) > 0) {
                 pc = nc;
                 e0 = 0;
+                run = 0;
+                full = (pc.tokens - appended) / kTile;
                 ids = ids_next_unit;
                 ids_after = page_ids(a, pc, 32, lane);
                 if (nc.next_unit(a, live)) ids_next_unit = page_ids(a, nc, 0, lane);
@@ -250,12 +273,15 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
     for (int s = 0; s < kStages; ++s) issue();
 
     // ---- consumer
+    // The exponentials are taken against a reference that follows a head's maximum only when a score is more than 2^kSlack above it, so that most
+    // tiles need neither the maximum over the warp's lanes nor a new scale of what is summed.
+    constexpr float kSlack = 8.f;
     Cursor cc = start;
-    const float scale2 = a.scale * kLog2e;
-    const float cap_in = a.softcap > 0.f ? a.scale / a.softcap : 0.f, cap_out = a.softcap * kLog2e;
+    const float scale2 = CAP ? 1.f : a.scale * kLog2e, from_base2 = 1.f / scale2;
+    const float cap_in = CAP ? a.scale / a.softcap : 0.f, cap_out = CAP ? a.softcap * kLog2e : 0.f;
     uint32_t qf[NG][4][2][2], qs[NG][2];
     float o[NG][8][4], ol[NG][4];
-    float mx[NG][2], sum[NG][2];
+    float ref[NG][2], most[NG][2], sum[NG][2];               // reference in base 2; score above which it has to follow (-inf: none yet)
     bool fresh = true;
     int first_tile = 0, head0 = 0, heads = 0, stage = 0;
 
@@ -278,7 +304,8 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
 #pragma unroll
                 for (int s = 0; s < 8; ++s) o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.f;
                 ol[t][0] = ol[t][1] = ol[t][2] = ol[t][3] = 0.f;
-                mx[t][0] = mx[t][1] = -INFINITY;
+                ref[t][0] = ref[t][1] = 0.f;
+                most[t][0] = most[t][1] = -INFINITY;
                 sum[t][0] = sum[t][1] = 0.f;
             }
         }
@@ -287,15 +314,16 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
         __syncwarp();
         unsigned char* tile_k = my_ring + stage * kStageBytes;
         const int base = cc.tile * kTile;
-        const int bits = bad[warp][stage];
-        const int cached = cc.tokens - (a.k_new != nullptr);
-        // the new token's rows: held in 4 bits first, in the tile and, by the first group, in its page; lanes 0 .. 15 have K's, the others V's
-        const int fresh_row = cached < cc.tokens ? cached - base : -1;
-        if (fresh_row >= 0 && fresh_row < kTile) {
+        const uint32_t bits = (bad >> (2 * stage)) & 3u;
+        const int cached = cc.tokens - appended;
+        const bool ragged = base + kTile > cached || bits != 0;              // (some rows are not the cache's)
+        if (ragged && cached < cc.tokens && cached - base < kTile) {
+            // the new token's rows: held in 4 bits first, in the tile and, by the first group, in its page; lanes 0 .. 15 have K's, the others V's
+            const int fresh_row = cached - base;
             const int h = cc.unit / a.c.batch, b = cc.unit - h * a.c.batch, piece = lane & 15;
-            const __nv_bfloat16* src = lane < 16 ? a.k_new + b * a.kn_seq + h * a.kn_head : a.v_new + b * a.vn_seq + h * a.vn_head;
+            const __nv_bfloat16* from = lane < 16 ? a.k_new + b * a.kn_seq + h * a.kn_head : a.v_new + b * a.vn_seq + h * a.vn_head;
             uint32_t param;
-            const uint32_t codes = quantise8(*(reinterpret_cast<const uint4*>(src) + piece), param);
+            const uint32_t codes = quantise8(*(reinterpret_cast<const uint4*>(from) + piece), param);
             unsigned char* row = tile_k + (lane < 16 ? 0 : kTileBytes) + fresh_row * kRow4;
             *reinterpret_cast<uint32_t*>(row + 4 * piece) = codes;
             if ((piece & 3) == 0) *reinterpret_cast<uint32_t*>(row + kRow4Codes + piece) = param;
@@ -307,7 +335,7 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                 const long long at = slot_in_pool(a.c, page, cached);
                 if (lane == 0 && a.c.positions != nullptr)
                     a.c.positions[at] = a.new_positions != nullptr ? a.new_positions[cc.unit % a.c.batch] : cached;
-                if (lane == 0 && a.c.mass != nullptr && !a.accumulate) a.c.mass[at] = 0.f;
+                if (lane == 0 && a.c.mass != nullptr && !ACC) a.c.mass[at] = 0.f;
             }
             __syncwarp();
         }
@@ -323,13 +351,13 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
             const uint32_t para[4] = {pa.x, pa.y, pa.z, pa.w}, parb[4] = {pb.x, pb.y, pb.z, pb.w};
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const uint32_t wa = *reinterpret_cast<const uint32_t*>(ra + 16 * g + 4 * tig), wb = *reinterpret_cast<const uint32_t*>(rb + 16 * g + 4 * tig);
+                uint32_t wa = *reinterpret_cast<const uint32_t*>(ra + 16 * g + 4 * tig), wb = *reinterpret_cast<const uint32_t*>(rb + 16 * g + 4 * tig);
                 const uint32_t sa = __byte_perm(para[g], 0u, 0x1010), sb = __byte_perm(parb[g], 0u, 0x1010);
                 const uint32_t ma = fma2(sa, 0xc300c300u, 0x80008000u), mb = fma2(sb, 0xc300c300u, 0x80008000u);     // -128 s
 #pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    const uint32_t kf[4] = {fma2(codes128(wa, 2 * st), sa, ma), fma2(codes128(wb, 2 * st), sb, mb),
-                                            fma2(codes128(wa, 2 * st + 1), sa, ma), fma2(codes128(wb, 2 * st + 1), sb, mb)};
+                for (int st = 0; st < 2; ++st) {             // the even channels, the odd ones
+                    const uint32_t ca = (st == 0 ? wa : wa >> 4) & kNibbles, cb = (st == 0 ? wb : wb >> 4) & kNibbles;
+                    const uint32_t kf[4] = {fma2(codes_low(ca), sa, ma), fma2(codes_low(cb), sb, mb), fma2(codes_high(ca), sa, ma), fma2(codes_high(cb), sb, mb)};
 #pragma unroll
                     for (int t = 0; t < NG; ++t) mma(s[t], kf, qf[t][g][st][0], qf[t][g][st][1]);
                 }
@@ -340,42 +368,22 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
 #pragma unroll
             for (int t = 0; t < NG; ++t) mma(s[t], lf, qs[t][0], qs[t][1]);
         }
-        // scores in base 2; what does not count gets -inf
-        const int ta = base + gid, tb = ta + 8;
-        const bool la = ta < cc.tokens && !((bits & 1) && ta < cached), lb = tb < cc.tokens && !((bits & 2) && tb < cached);
-        uint32_t pf[NG][2], pl[NG][2];                       // weights: first and second term
-        bool grew = false;
-        float scale_by[NG][2];
+        if (CAP) {
 #pragma unroll
-        for (int t = 0; t < NG; ++t) {
+            for (int t = 0; t < NG; ++t)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                float y = a.softcap > 0.f ? cap_out * tanhf(s[t][c] * cap_in) : s[t][c] * scale2;
-                s[t][c] = (c < 2 ? la : lb) ? y : -INFINITY;
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                float m = fmaxf(s[t][c], s[t][c + 2]);
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                m = fmaxf(m, mx[t][c]);
-                grew |= m > mx[t][c];
-                const float ref = m == -INFINITY ? 0.f : m;
-                scale_by[t][c] = ex2f(mx[t][c] - ref);       // 0 for the first tile, 1 where the maximum stays
-                mx[t][c] = m;
-                const float pa = ex2f(s[t][c] - ref), pb = ex2f(s[t][c + 2] - ref);
-                sum[t][c] = sum[t][c] * scale_by[t][c] + (pa + pb);
-                if (c == 0) { pf[t][0] = __float_as_uint(pa); pf[t][1] = __float_as_uint(pb); }
-                else {
-                    split_bf16(__uint_as_float(pf[t][0]), pa, pf[t][0], pl[t][0]);
-                    split_bf16(__uint_as_float(pf[t][1]), pb, pf[t][1], pl[t][1]);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) { pf[t][i] = transpose8x8(pf[t][i]); pl[t][i] = transpose8x8(pl[t][i]); }
+                for (int c = 0; c < 4; ++c) s[t][c] = cap_out * tanhf(s[t][c] * cap_in);
         }
-        if (a.accumulate) {                                  // kept until the sum over the whole unit is known
+        if (ragged) {                                        // what does not count gets -inf
+            const int ta = base + gid, tb = ta + 8;
+            const bool la = ta < cc.tokens && !((bits & 1) && ta < cached), lb = tb < cc.tokens && !((bits & 2) && tb < cached);
+#pragma unroll
+            for (int t = 0; t < NG; ++t) {
+                if (!la) s[t][0] = s[t][1] = -INFINITY;
+                if (!lb) s[t][2] = s[t][3] = -INFINITY;
+            }
+        }
+        if (ACC) {                                           // kept, in base 2, until the sum over the whole unit is known
             float* col = a.scores + ((long long)cc.unit * a.g + cc.grp * kDecodeHeads + 2 * tig) * a.unit_rows + base + gid;
 #pragma unroll
             for (int t = 0; t < NG; ++t)
@@ -383,19 +391,50 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                 for (int c = 0; c < 2; ++c)
                     if (t * 8 + 2 * tig + c < heads) {       // 32 bytes of a head's scores per group of eight lanes
                         float* at = col + (long long)(t * 8 + c) * a.unit_rows;
-                        at[0] = s[t][c];
-                        at[8] = s[t][c + 2];
+                        at[0] = s[t][c] * scale2;
+                        at[8] = s[t][c + 2] * scale2;
                     }
         }
-        if (__any_sync(0xffffffffu, grew)) {
+        bool above = false;
+#pragma unroll
+        for (int t = 0; t < NG; ++t)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) above |= s[t][c] > most[t][c & 1];
+        if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
             for (int t = 0; t < NG; ++t) {
+                float by[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float m = fmaxf(s[t][c], s[t][c + 2]);
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) * scale2;
+                    const bool none = most[t][c] == -INFINITY;               // nothing summed yet
+                    const float now = m == -INFINITY ? ref[t][c] : none ? m : fmaxf(m, ref[t][c]);
+                    by[c] = none ? 1.f : ex2f(ref[t][c] - now);
+                    ref[t][c] = now;
+                    sum[t][c] *= by[c];
+                    if (m != -INFINITY) most[t][c] = (now + kSlack) * from_base2;
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    o[t][j][0] *= scale_by[t][0]; o[t][j][1] *= scale_by[t][1];
-                    o[t][j][2] *= scale_by[t][0]; o[t][j][3] *= scale_by[t][1];
+                    o[t][j][0] *= by[0]; o[t][j][1] *= by[1];
+                    o[t][j][2] *= by[0]; o[t][j][3] *= by[1];
                 }
-                ol[t][0] *= scale_by[t][0]; ol[t][1] *= scale_by[t][1];
+                ol[t][0] *= by[0]; ol[t][1] *= by[1];
+            }
+        }
+        uint32_t pf[NG][2], pl[NG][2];                       // weights as two bf16 terms, the first cut off, the second rounded: within 2^-16
+#pragma unroll
+        for (int t = 0; t < NG; ++t) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float x = ex2f(fmaf(s[t][2 * i], scale2, -ref[t][0])), y = ex2f(fmaf(s[t][2 * i + 1], scale2, -ref[t][1]));
+                sum[t][0] += x; sum[t][1] += y;
+                const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
+                pf[t][i] = transpose8x8(__byte_perm(xb, yb, 0x7632));
+                pl[t][i] = transpose8x8(pack_bf16(x - __uint_as_float(xb & 0xffff0000u), y - __uint_as_float(yb & 0xffff0000u)));
             }
         }
         // O^T += V^T P^T: 128 channels x 8 NG heads.  The lane has the 16 channels 16 gid + 0..15 of tokens 2 tig, + 1, + 8 and + 9; row gid of the j-th
@@ -413,14 +452,26 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
             const uint32_t s0 = __byte_perm(par[0], par[1], 0x5410), s1 = __byte_perm(par[2], par[3], 0x5410);
             const uint32_t m0 = fma2(s0, 0xc300c300u, 0x80008000u), m1 = fma2(s1, 0xc300c300u, 0x80008000u);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const unsigned sel = j < 4 ? 0x5410 : 0x7632;
-                const uint32_t vf[4] = {fma2(codes128(__byte_perm(v[0].x, v[1].x, sel), j & 3), s0, m0), fma2(codes128(__byte_perm(v[0].y, v[1].y, sel), j & 3), s0, m0),
-                                        fma2(codes128(__byte_perm(v[2].x, v[3].x, sel), j & 3), s1, m1), fma2(codes128(__byte_perm(v[2].y, v[3].y, sel), j & 3), s1, m1)};
+            for (int j4 = 0; j4 < 8; j4 += 4) {              // the same bytes of two tokens side by side: channels j4, j4 + 2 in the lower halves of the bytes
+                const unsigned sel = j4 == 0 ? 0x5140 : 0x7362;
+                const uint32_t x[4] = {__byte_perm(v[0].x, v[1].x, sel), __byte_perm(v[0].y, v[1].y, sel), __byte_perm(v[2].x, v[3].x, sel), __byte_perm(v[2].y, v[3].y, sel)};
 #pragma unroll
-                for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pf[t][0], pf[t][1]);
+                for (int odd = 0; odd < 2; ++odd) {
+                    uint32_t c[4];
 #pragma unroll
-                for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pl[t][0], pl[t][1]);
+                    for (int i = 0; i < 4; ++i) c[i] = (odd == 0 ? x[i] : x[i] >> 4) & kNibbles;
+#pragma unroll
+                    for (int two = 0; two < 2; ++two) {
+                        const int j = j4 + odd + 2 * two;
+                        uint32_t vf[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) vf[i] = fma2(two == 0 ? codes_low(c[i]) : codes_high(c[i]), i < 2 ? s0 : s1, i < 2 ? m0 : m1);
+#pragma unroll
+                        for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pf[t][0], pf[t][1]);
+#pragma unroll
+                        for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pl[t][0], pl[t][1]);
+                    }
+                }
             }
             const uint32_t lf[4] = {__byte_perm(par[0], par[1], 0x7632), 0u, __byte_perm(par[2], par[3], 0x7632), 0u};
 #pragma unroll
@@ -450,7 +501,7 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                     const int head = t * 8 + 2 * tig + c;
                     if (head >= heads) continue;
                     if (gid == 0) {
-                        a.ml[slot * 32 + head] = mx[t][c];
+                        a.ml[slot * 32 + head] = most[t][c] == -INFINITY ? -INFINITY : ref[t][c];
                         a.ml[slot * 32 + 16 + head] = l;
                     }
                     float x[16];
@@ -464,7 +515,7 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                             dst[i / 8] = make_uint4(pack_bf16(x[i] * inv, x[i + 1] * inv), pack_bf16(x[i + 2] * inv, x[i + 3] * inv),
                                                     pack_bf16(x[i + 4] * inv, x[i + 5] * inv), pack_bf16(x[i + 6] * inv, x[i + 7] * inv));
                         if (gid == 0 && a.lse != nullptr)
-                            a.lse[(long long)b * (a.c.heads * a.g) + head0 + head] = l == 0.f ? -INFINITY : kLn2 * (mx[t][c] + log2f(l));
+                            a.lse[(long long)b * (a.c.heads * a.g) + head0 + head] = l == 0.f ? -INFINITY : kLn2 * (ref[t][c] + log2f(l));
                     } else {
                         float4* dst = reinterpret_cast<float4*>(a.o + (slot * gg + head) * kD + 16 * gid);
 #pragma unroll
@@ -480,15 +531,21 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
 
 }  // namespace
 
-cudaError_t launch_decode4(const DecodeArgs& a, cudaStream_t stream) {
-    static std::atomic<unsigned long long> done[2];
-    const bool narrow = a.g <= 8;
-    auto kernel = narrow ? decode4_kernel<1> : decode4_kernel<2>;
-    const int warps = narrow ? kDecode4Warps : kDecode4WarpsWide;
-    const size_t smem = narrow ? Four<1>::kSmemBytes : Four<2>::kSmemBytes;
-    const cudaError_t e = allow_smem(kernel, (int)smem, done[narrow ? 0 : 1]);
+namespace {
+template <int NG, bool CAP, bool ACC>
+cudaError_t launch(const DecodeArgs& a, cudaStream_t stream) {
+    static std::atomic<unsigned long long> done;
+    const cudaError_t e = allow_smem(decode4_kernel<NG, CAP, ACC>, (int)Four<NG>::kSmemBytes, done);
     if (e != cudaSuccess) return e;
-    return launch_chained(kPdlOther, kernel, dim3(a.workers / warps), dim3(warps * 32), smem, stream, a);
+    return launch_chained(kPdlOther, decode4_kernel<NG, CAP, ACC>, dim3(a.workers / Four<NG>::kWarps), dim3(Four<NG>::kThreads), Four<NG>::kSmemBytes, stream, a);
 }
+template <int NG>
+cudaError_t launch(const DecodeArgs& a, cudaStream_t stream) {
+    if (a.softcap > 0.f) return a.accumulate ? launch<NG, true, true>(a, stream) : launch<NG, true, false>(a, stream);
+    return a.accumulate ? launch<NG, false, true>(a, stream) : launch<NG, false, false>(a, stream);
+}
+}  // namespace
+
+cudaError_t launch_decode4(const DecodeArgs& a, cudaStream_t stream) { return a.g <= 8 ? launch<1>(a, stream) : launch<2>(a, stream); }
 
 }  // namespace compactor

@@ -140,7 +140,7 @@ struct BoundsArgs {
     int* status;
     int four;
 };
-cudaError_t launch_paged_bounds(const BoundsArgs& a, cudaStream_t stream);
+cudaError_t launch_paged_bounds(const BoundsArgs& a, int sm_count, cudaStream_t stream);
 
 // Choice of pages for the queries of one new token per sequence.
 struct SelectArgs {

@@ -74,8 +74,9 @@ read_kernel(const __grid_constant__ ReadArgs a, const __grid_constant__ ReadTabl
 
 // ------------------------------------------------------------------------------------------ bounds
 // Least and greatest key of a page, channel by channel, over its tokens: what the choice of pages goes by.  Bound by HBM: 256 (80) bytes per
-// token.  Up to eight warps share a page, 16 tokens each, 16 lanes a row; a warp has 16 rows in flight, and the least and greatest of a lane's eight
-// channels stay packed (min and max of bf16 are exact; they keep a not-a-number).
+// token.  16 lanes hold a row; a warp has 16 rows in flight (32 in 4 bits, which are fewer bytes), and the least and greatest of a lane's eight
+// channels stay packed (min and max of bf16 are exact; they keep a not-a-number).  A warp takes a whole page where there are enough pages for all
+// warps of the GPU, so that its chain of reads (length, page id, rows) is made once; up to eight share one where there are few.
 constexpr int kBoundsThreads = 256;
 
 template <bool FOUR>
@@ -106,13 +107,14 @@ bounds_kernel(const __grid_constant__ BoundsArgs a, int chunks, int warps_per_pa
     for (int i = 0; i < 4; ++i) { least[i] = 0x7f807f80u; most[i] = 0xff80ff80u; }
     if (page >= 0) {
         const int tokens = (int)min((long long)1 << a.c.page_shift, n - slot0);
-        const int way = warp % warps_per_page;               // rows 16 way .. + 15, then 16 warps_per_page further on
+        constexpr int kBatch = FOUR ? 16 : 8;                // pairs of rows in flight
+        const int way = warp % warps_per_page;               // every warps_per_page-th run of rows, from the way-th on
         const long long row0 = row_in_pool(a.c, page, 0);
 #pragma unroll 1
-        for (int r0 = 16 * way; r0 < tokens; r0 += 16 * warps_per_page) {
-            uint4 x[8];
+        for (int r0 = 2 * kBatch * way; r0 < tokens; r0 += 2 * kBatch * warps_per_page) {
+            uint4 x[kBatch];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {                    // (a row behind the last: the last once more)
+            for (int i = 0; i < kBatch; ++i) {               // (a row behind the last: the last once more)
                 const __nv_bfloat16* row = a.c.k + row0 + min(r0 + 2 * i + (lane >> 4), tokens - 1) * a.c.stride_token;
                 if (FOUR) {
                     const unsigned char* src = reinterpret_cast<const unsigned char*>(row);
@@ -123,7 +125,7 @@ bounds_kernel(const __grid_constant__ BoundsArgs a, int chunks, int warps_per_pa
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kBatch; ++i) {
                 uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
                 if (FOUR) {                                  // pairs of channels four apart
                     const uint32_t s = __byte_perm(x[i].y, 0u, 0x1010), lo = __byte_perm(x[i].y, 0u, 0x3232);
@@ -169,9 +171,11 @@ cudaError_t launch_paged_read(const ReadArgs& a, const ReadTables& t, cudaStream
     return launch_chained(kPdlOther, a.four ? read_kernel<true> : read_kernel<false>, grid, dim3(kThreads), 0, stream, a, t);
 }
 
-cudaError_t launch_paged_bounds(const BoundsArgs& a, cudaStream_t stream) {
+cudaError_t launch_paged_bounds(const BoundsArgs& a, int sm_count, cudaStream_t stream) {
     const int page = 1 << a.c.page_shift, pages = (a.capacity + page - 1) / page;
-    const int warps_per_page = min(8, max(1, page / 16)), per_block = 8 / warps_per_page, chunks = (pages + per_block - 1) / per_block;
+    int warps_per_page = 1;
+    while (warps_per_page < 8 && page > (a.four ? 32 : 16) * warps_per_page && (long long)a.units * pages * warps_per_page < 64LL * sm_count) warps_per_page *= 2;
+    const int per_block = 8 / warps_per_page, chunks = (pages + per_block - 1) / per_block;
     return launch_chained(kPdlOther, a.four ? bounds_kernel<true> : bounds_kernel<false>, dim3((unsigned)(a.units * chunks)), dim3(kBoundsThreads), 0,
                           stream, a, chunks, warps_per_page);
 }

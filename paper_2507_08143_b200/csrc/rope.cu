@@ -1,22 +1,24 @@
 // Norms of queries and keys for each head with the rotation by position in the same pass: what a prefill is scored by (keys without
 // rotation), held as (keys with it) and asked with, and the rows of a decoding step.
 //
-//   y = x w / sqrt(mean(x^2) + eps)  (y = x without w);   a_i = position * f_i, i < R / 2;
+//   y = x w r, r = 1 / sqrt(mean(x^2) + eps)  (y = x without w);   a_i = position * f_i, i < R / 2;
 //   (y_i, y_j) -> (y_i cos a_i - y_j sin a_i, y_j cos a_i + y_i sin a_i) with (i, j) = (i, i + R / 2) or (2 i, 2 i + 1); channels from R on stay.
 //
-// Bound by HBM: a row is read once and written once or twice.  16 lanes hold a row, eight channels each, and a half-warp has up to four
-// rows in flight.  The angles of a token are the same for all its heads: the block works them out once, in 64 bits, because
-// a far position times a frequency has more digits before the point than 32 bits leave behind it (at position 131072 the angle
-// would be off by 0.004), taken to a fraction of a turn and then to 32 bits.
-#include "common.cuh"
+// Bound by HBM: a row is read once and written once or twice, and the instructions for it have to be few (about three per channel would be as long as
+// its bytes).  So a warp stays with one token: 16 lanes hold a row, eight channels each, and every lane keeps, for all heads of the token,
+//   out_c = r (x_c A_c + x_partner B_c),   A_c = w_c cos a,  B_c = -+ w_partner sin a;
+// the partner's channel comes from the lane half a rotation away as it was read, two to a register.  Up to four rows of a lane are in flight.
+// The angles are worked out in 64 bits, because a far position times a frequency has more digits before the point than 32 bits leave
+// behind it (at position 131072 the angle would be off by 0.004), taken to a fraction of a turn and then to 32 bits; each lane works out two and
+// the warp shares them.
 #include "rope.cuh"
 
 namespace compactor {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kHalfWarps = kThreads / 16;
-constexpr int kRows = 4;                       // rows of a half-warp in flight
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kRows = 4;                       // pairs of rows of a warp in flight
 
 __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -36,105 +38,122 @@ __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-__global__ void __launch_bounds__(kThreads)
-rope_kernel(const __grid_constant__ RopeArgs a) {
-    __shared__ __align__(16) float cosines[kRopeTokens][kD / 2], sines[kRopeTokens][kD / 2];
-    const int tid = threadIdx.x, l = tid & 15, hw = tid >> 4;
-    pdl_trigger();
-    pdl_wait();
-    const long long token0 = (long long)blockIdx.x * a.tokens_per_block;
-    const int tokens = (int)min((long long)a.tokens_per_block, a.tokens - token0);
-    const int per_token = a.q_heads + a.k_heads, items = tokens * per_token, half = a.rotary / 2;
-    // rows of the first round are on their way while the angles are worked out
-    uint4 in[kRows];
-    int token[kRows], row[kRows];
-    auto fetch = [&](int first) {
+// One kind of rows (queries or keys) of a token: heads first, first + 2 step, ... of `heads`, two at a time (one for each half of the warp).
+struct Rows {
+    const __nv_bfloat16* in;                   // of the token
+    __nv_bfloat16* out;
+    __nv_bfloat16* plain;                      // or null
+    long long in_head, out_head, plain_head;
+    int heads;
+    bool norm;
+};
+
+// FULL: all channels are rotated.
+template <bool INTERLEAVED, bool FULL>
+__device__ __forceinline__ void rotate_rows(const Rows& r, const float (&a)[8], const float (&b)[8], const float (&w)[8], float eps, int other,
+                                            bool turned, int first, int step) {
+    const int l = threadIdx.x & 15, sub = (threadIdx.x >> 4) & 1;
+    for (int h0 = first; h0 < r.heads; h0 += kRows * step) {
+        uint4 in[kRows];
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)        // (behind the last row: the last once more, not written)
+            in[u] = *(reinterpret_cast<const uint4*>(r.in + min(h0 + u * step + sub, r.heads - 1) * r.in_head) + l);
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            const int item = min(first + u * kHalfWarps, items - 1);
-            token[u] = item / per_token;
-            row[u] = item - token[u] * per_token;
-            const long long t = token0 + token[u];
-            const __nv_bfloat16* src = row[u] < a.q_heads ? a.q + t * a.q_token + row[u] * a.q_head
-                                                          : a.k + t * a.k_token + (row[u] - a.q_heads) * a.k_head;
-            in[u] = *(reinterpret_cast<const uint4*>(src) + l);
-        }
-    };
-    fetch(hw);
-    float qw[8], kw[8];
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-    unpack(a.q_weight != nullptr ? *(reinterpret_cast<const uint4*>(a.q_weight) + l) : none, qw);
-    unpack(a.k_weight != nullptr ? *(reinterpret_cast<const uint4*>(a.k_weight) + l) : none, kw);
-    for (int i = tid; i < tokens * half; i += kThreads) {
-        const int t = i / half, f = i - t * half;
-        const double turns = (double)a.positions[token0 + t] * (double)a.inv_freq[f] * 0.15915494309189533577;    // 1 / (2 pi)
-        sincospif(2.f * (float)(turns - rint(turns)), &sines[t][f], &cosines[t][f]);
-    }
-    __syncthreads();
-    const unsigned mine = 0xffffu << (tid & 16);             // the lanes of this half-warp
-    for (int first = hw; first < items; first += kHalfWarps * kRows) {
-        if (first != hw) fetch(first);
-#pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            if (first + u * kHalfWarps >= items) break;
-            const bool is_q = row[u] < a.q_heads;
-            float x[8];
+            if (h0 + u * step >= r.heads) break;
+            const int head = h0 + u * step + sub;
+            float x[8], y[8], z[8];
             unpack(in[u], x);
-            if ((is_q ? a.q_weight : a.k_weight) != nullptr) {
-                float sum = 0.f;
+            float inv = 1.f;
+            if (r.norm) {
+                float sum = x[0] * x[0];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
+                for (int i = 1; i < 8; ++i) sum += x[i] * x[i];
 #pragma unroll
-                for (int d = 1; d < 16; d *= 2) sum += __shfl_xor_sync(mine, sum, d);
-                const float r = rsqrtf(sum * (1.f / kD) + a.eps);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (is_q ? qw[i] : kw[i]);
+                for (int d = 1; d < 16; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                inv = rsqrtf(sum * (1.f / kD) + eps);
             }
-            const long long t = token0 + token[u];
-            const int head = is_q ? row[u] : row[u] - a.q_heads;
-            if (!is_q && a.k_plain != nullptr) *(reinterpret_cast<uint4*>(a.k_plain + t * a.p_token + head * a.p_head) + l) = pack(x);
-            if (a.interleaved) {
-                if (8 * l < a.rotary) {
-                    const float4 c = *reinterpret_cast<const float4*>(&cosines[token[u]][4 * l]), s = *reinterpret_cast<const float4*>(&sines[token[u]][4 * l]);
-                    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+            if (INTERLEAVED) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float y0 = x[2 * i], y1 = x[2 * i + 1];
-                        x[2 * i] = y0 * cc[i] - y1 * ss[i];
-                        x[2 * i + 1] = y1 * cc[i] + y0 * ss[i];
-                    }
-                }
-            } else if (half > 0) {                           // the other of each pair is in the lane half a rotation away
-                const int away = half / 8;
-                const bool lower = l < away, turned = l < 2 * away;
-                const int other = lower ? l + away : turned ? l - away : l;
-                const int f = turned ? 8 * (lower ? l : l - away) : 0;
+                for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
+            } else {
+                unpack(make_uint4(__shfl_sync(0xffffffffu, in[u].x, other), __shfl_sync(0xffffffffu, in[u].y, other),
+                                  __shfl_sync(0xffffffffu, in[u].z, other), __shfl_sync(0xffffffffu, in[u].w, other)), y);
+            }
 #pragma unroll
-                for (int i = 0; i < 8; i += 4) {
-                    const float4 c = *reinterpret_cast<const float4*>(&cosines[token[u]][f + i]), s = *reinterpret_cast<const float4*>(&sines[token[u]][f + i]);
-                    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+            for (int i = 0; i < 8; ++i) z[i] = (FULL || turned ? x[i] * a[i] + y[i] * b[i] : x[i] * a[i]) * inv;
+            if (head < r.heads) {
+                *(reinterpret_cast<uint4*>(r.out + head * r.out_head) + l) = pack(z);
+                if (r.plain != nullptr) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float y = __shfl_sync(mine, x[i + k], other, 16);
-                        if (turned) x[i + k] = lower ? x[i + k] * cc[k] - y * ss[k] : x[i + k] * cc[k] + y * ss[k];
-                    }
+                    for (int i = 0; i < 8; ++i) z[i] = x[i] * w[i] * inv;
+                    *(reinterpret_cast<uint4*>(r.plain + head * r.plain_head) + l) = pack(z);
                 }
             }
-            __nv_bfloat16* dst = is_q ? a.q_out + t * a.qo_token + head * a.qo_head : a.k_out + t * a.ko_token + head * a.ko_head;
-            *(reinterpret_cast<uint4*>(dst) + l) = pack(x);
         }
     }
 }
 
+// `parts` warps share a token's heads.
+template <bool INTERLEAVED, bool FULL>
+__global__ void __launch_bounds__(kThreads)
+rope_kernel(const __grid_constant__ RopeArgs a, int parts) {
+    __shared__ __align__(16) float turn[kWarps][2][kD / 2];  // cosines and sines
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & 15;
+    pdl_trigger();
+    pdl_wait();
+    const long long at = (long long)blockIdx.x * kWarps + warp, token = at / parts;
+    const int part = (int)(at - token * parts);
+    if (token >= a.tokens) return;
+    const int half = a.rotary / 2;
+    const double position = half > 0 ? (double)a.positions[token] : 0.;
+    for (int f = lane; f < half; f += 32) {
+        const double turns = position * (double)a.inv_freq[f] * 0.15915494309189533577;      // 1 / (2 pi)
+        sincospif(2.f * (float)(turns - rint(turns)), &turn[warp][1][f], &turn[warp][0][f]);
+    }
+    __syncwarp();
+    // the partner's lane, the first of this lane's frequencies, and on which side of the pair it is
+    const int away = half / 8;
+    const bool turned = 8 * l < a.rotary, lower = l < away;
+    const int other = INTERLEAVED || !turned ? lane : lower ? lane + away : lane - away;
+    float cosine[8], sine[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int f = !turned ? 0 : INTERLEAVED ? 4 * l + i / 2 : 8 * (lower ? l : l - away) + i;
+        const float s = turned ? turn[warp][1][f] : 0.f;
+        cosine[i] = turned ? turn[warp][0][f] : 1.f;
+        sine[i] = (INTERLEAVED ? (i & 1) == 0 : lower) ? -s : s;
+    }
+    auto rows = [&](const Rows& r, const __nv_bfloat16* weight) {
+        float w[8], v[8], ca[8], cb[8];
+        const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+        unpack(weight != nullptr ? *(reinterpret_cast<const uint4*>(weight) + l) : ones, w);
+        unpack(weight != nullptr ? *(reinterpret_cast<const uint4*>(weight) + (other & 15)) : ones, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            ca[i] = cosine[i] * w[i];
+            cb[i] = sine[i] * v[INTERLEAVED ? i ^ 1 : i];
+        }
+        rotate_rows<INTERLEAVED, FULL>(r, ca, cb, w, a.eps, other, turned, 2 * part, 2 * parts);
+    };
+    if (a.q_heads > 0)
+        rows({a.q + token * a.q_token, a.q_out + token * a.qo_token, nullptr, a.q_head, a.qo_head, 0, a.q_heads, a.q_weight != nullptr}, a.q_weight);
+    if (a.k_heads > 0)
+        rows({a.k + token * a.k_token, a.k_out + token * a.ko_token, a.k_plain != nullptr ? a.k_plain + token * a.p_token : nullptr, a.k_head, a.ko_head,
+              a.p_head, a.k_heads, a.k_weight != nullptr}, a.k_weight);
+}
+
 }  // namespace
 
-cudaError_t launch_rope(RopeArgs a, int sm_count, cudaStream_t stream) {
-    // About 20 rows per half-warp, and fewer tokens a block where there would not be a few blocks for every SM.
-    const int per_token = a.q_heads + a.k_heads;
-    int n = min(kRopeTokens, max(1, 20 * kHalfWarps / per_token));
-    while (n > 1 && (a.tokens + n - 1) / n < 4LL * sm_count) n /= 2;
-    a.tokens_per_block = n;
-    return launch_chained(kPdlOther, rope_kernel, dim3((unsigned)((a.tokens + n - 1) / n)), dim3(kThreads), 0, stream, a);
+cudaError_t launch_rope(const RopeArgs& a, int sm_count, cudaStream_t stream) {
+    // A warp for a token where that makes enough warps, else as many as there are pairs of heads.
+    const int most = max(1, (max(a.q_heads, a.k_heads) + 1) / 2);
+    int parts = 1;
+    while (parts * 2 <= most && a.tokens * parts < 16LL * sm_count) parts *= 2;
+    const long long blocks = (a.tokens * parts + kWarps - 1) / kWarps;
+    const auto kernel = a.rotary == kD ? (a.interleaved ? rope_kernel<true, true> : rope_kernel<false, true>)
+                                       : (a.interleaved ? rope_kernel<true, false> : rope_kernel<false, false>);
+    return launch_chained(kPdlOther, kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, parts);
 }
 
 }  // namespace compactor

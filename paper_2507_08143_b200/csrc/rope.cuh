@@ -4,7 +4,6 @@
 
 namespace compactor {
 
-constexpr int kRopeTokens = 8;                 // most tokens of a block
 struct RopeArgs {
     long long tokens;
     int q_heads, k_heads;
@@ -20,8 +19,7 @@ struct RopeArgs {
     __nv_bfloat16* k_out;
     __nv_bfloat16* k_plain;                    // keys before the rotation, or null
     long long q_token, q_head, k_token, k_head, qo_token, qo_head, ko_token, ko_head, p_token, p_head;     // strides in elements
-    int tokens_per_block;
 };
-cudaError_t launch_rope(RopeArgs a, int sm_count, cudaStream_t stream);
+cudaError_t launch_rope(const RopeArgs& a, int sm_count, cudaStream_t stream);
 
 }  // namespace compactor
