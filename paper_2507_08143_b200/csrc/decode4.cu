@@ -28,7 +28,7 @@ constexpr int kStageBytes = 2 * kTileBytes;
 template <int NG> struct Four {
     static constexpr int kWarps = NG == 1 ? kDecode4Warps : kDecode4WarpsWide;
     static constexpr int kThreads = kWarps * 32;
-    static constexpr int kStages = NG == 1 ? 4 : 8;    // 164 KB either way
+    static constexpr int kStages = NG == 1 ? 5 : 8;    // 154 KB, 164 KB
     static constexpr size_t kSmemBytes = (size_t)kWarps * kStages * kStageBytes;
 };
 
@@ -79,6 +79,13 @@ __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t
 __device__ __forceinline__ uint32_t codes_low(uint32_t x) { return __byte_perm(x, 0x43434343u, 0x4140); }
 __device__ __forceinline__ uint32_t codes_high(uint32_t x) { return __byte_perm(x, 0x43434343u, 0x4342); }
 constexpr uint32_t kNibbles = 0x0f0f0f0fu;
+
+// The instruction of decode.cuh, free to be placed where its operands are ready.
+__device__ __forceinline__ void mma4(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 
 // CAP: scores are capped.  ACC: weights are accumulated.
 template <int NG, bool CAP, bool ACC>
@@ -359,14 +366,14 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                     const uint32_t ca = (st == 0 ? wa : wa >> 4) & kNibbles, cb = (st == 0 ? wb : wb >> 4) & kNibbles;
                     const uint32_t kf[4] = {fma2(codes_low(ca), sa, ma), fma2(codes_low(cb), sb, mb), fma2(codes_high(ca), sa, ma), fma2(codes_high(cb), sb, mb)};
 #pragma unroll
-                    for (int t = 0; t < NG; ++t) mma(s[t], kf, qf[t][g][st][0], qf[t][g][st][1]);
+                    for (int t = 0; t < NG; ++t) mma4(s[t], kf, qf[t][g][st][0], qf[t][g][st][1]);
                 }
             }
             const uint32_t la = *reinterpret_cast<const uint32_t*>(ra + kRow4Codes + 4 * tig), lb = *reinterpret_cast<const uint32_t*>(rb + kRow4Codes + 4 * tig);
             const uint32_t la2 = __byte_perm(la, 0u, 0x3232), lb2 = __byte_perm(lb, 0u, 0x3232);
             const uint32_t lf[4] = {la2, lb2, la2, lb2};
 #pragma unroll
-            for (int t = 0; t < NG; ++t) mma(s[t], lf, qs[t][0], qs[t][1]);
+            for (int t = 0; t < NG; ++t) mma4(s[t], lf, qs[t][0], qs[t][1]);
         }
         if (CAP) {
 #pragma unroll
@@ -467,17 +474,17 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) vf[i] = fma2(two == 0 ? codes_low(c[i]) : codes_high(c[i]), i < 2 ? s0 : s1, i < 2 ? m0 : m1);
 #pragma unroll
-                        for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pf[t][0], pf[t][1]);
+                        for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pf[t][0], pf[t][1]);
 #pragma unroll
-                        for (int t = 0; t < NG; ++t) mma(o[t][j], vf, pl[t][0], pl[t][1]);
+                        for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pl[t][0], pl[t][1]);
                     }
                 }
             }
             const uint32_t lf[4] = {__byte_perm(par[0], par[1], 0x7632), 0u, __byte_perm(par[2], par[3], 0x7632), 0u};
 #pragma unroll
-            for (int t = 0; t < NG; ++t) mma(ol[t], lf, pf[t][0], pf[t][1]);
+            for (int t = 0; t < NG; ++t) mma4(ol[t], lf, pf[t][0], pf[t][1]);
 #pragma unroll
-            for (int t = 0; t < NG; ++t) mma(ol[t], lf, pl[t][0], pl[t][1]);
+            for (int t = 0; t < NG; ++t) mma4(ol[t], lf, pl[t][0], pl[t][1]);
         }
         __syncwarp();
         issue();
