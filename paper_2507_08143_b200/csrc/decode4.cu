@@ -17,6 +17,8 @@
 #include "decode.cuh"
 #include "quant4.cuh"
 
+#include <type_traits>
+
 namespace compactor {
 namespace {
 
@@ -317,181 +319,214 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
             }
         }
         if (left_c <= kStages) pdl_trigger();                // the second kernel's blocks are let in when the tiles run out
-        cp_wait<kStages - 1>();
-        __syncwarp();
-        unsigned char* tile_k = my_ring + stage * kStageBytes;
-        const int base = cc.tile * kTile;
-        const uint32_t bits = (bad >> (2 * stage)) & 3u;
         const int cached = cc.tokens - appended;
-        const bool ragged = base + kTile > cached || bits != 0;              // (some rows are not the cache's)
-        if (ragged && cached < cc.tokens && cached - base < kTile) {
-            // the new token's rows: held in 4 bits first, in the tile and, by the first group, in its page; lanes 0 .. 15 have K's, the others V's
-            const int fresh_row = cached - base;
-            const int h = cc.unit / a.c.batch, b = cc.unit - h * a.c.batch, piece = lane & 15;
-            const __nv_bfloat16* from = lane < 16 ? a.k_new + b * a.kn_seq + h * a.kn_head : a.v_new + b * a.vn_seq + h * a.vn_head;
-            uint32_t param;
-            const uint32_t codes = quantise8(*(reinterpret_cast<const uint4*>(from) + piece), param);
-            unsigned char* row = tile_k + (lane < 16 ? 0 : kTileBytes) + fresh_row * kRow4;
-            *reinterpret_cast<uint32_t*>(row + 4 * piece) = codes;
-            if ((piece & 3) == 0) *reinterpret_cast<uint32_t*>(row + kRow4Codes + piece) = param;
-            const int page = new_page[warp][stage];
-            if (page >= 0 && cc.grp == 0) {
-                row = reinterpret_cast<unsigned char*>((lane < 16 ? a.c.k : a.c.v) + row_in_pool(a.c, page, cached));
+        // COUNT tiles of the unit, whose steps the compiler interleaves
+        auto attend = [&](auto count) {
+            constexpr int COUNT = decltype(count)::value;
+            cp_wait<kStages - COUNT>();
+            __syncwarp();
+            unsigned char* tile[COUNT];
+            int base[COUNT];
+            uint32_t bits[COUNT];
+            bool ragged = false;                             // some rows are not the cache's
+#pragma unroll
+            for (int u = 0; u < COUNT; ++u) {
+                const int at = stage + u < kStages ? stage + u : stage + u - kStages;
+                tile[u] = my_ring + at * kStageBytes;
+                base[u] = (cc.tile + u) * kTile;
+                bits[u] = (bad >> (2 * at)) & 3u;
+                ragged |= base[u] + kTile > cached || bits[u] != 0;
+            }
+            if (ragged && cached < cc.tokens && cached < base[COUNT - 1] + kTile && cached >= base[0]) {
+                // the new token's rows: held in 4 bits first, in the tile and, by the first group, in its page; lanes 0 .. 15 have K's, the others V's
+                const int which = COUNT > 1 && cached >= base[COUNT - 1] ? COUNT - 1 : 0;
+                const int at_stage = stage + which < kStages ? stage + which : stage + which - kStages;
+                const int h = cc.unit / a.c.batch, b = cc.unit - h * a.c.batch, piece = lane & 15;
+                const __nv_bfloat16* from = lane < 16 ? a.k_new + b * a.kn_seq + h * a.kn_head : a.v_new + b * a.vn_seq + h * a.vn_head;
+                uint32_t param;
+                const uint32_t codes = quantise8(*(reinterpret_cast<const uint4*>(from) + piece), param);
+                unsigned char* row = my_ring + at_stage * kStageBytes + (lane < 16 ? 0 : kTileBytes) + (cached & (kTile - 1)) * kRow4;
                 *reinterpret_cast<uint32_t*>(row + 4 * piece) = codes;
                 if ((piece & 3) == 0) *reinterpret_cast<uint32_t*>(row + kRow4Codes + piece) = param;
-                const long long at = slot_in_pool(a.c, page, cached);
-                if (lane == 0 && a.c.positions != nullptr)
-                    a.c.positions[at] = a.new_positions != nullptr ? a.new_positions[cc.unit % a.c.batch] : cached;
-                if (lane == 0 && a.c.mass != nullptr && !ACC) a.c.mass[at] = 0.f;
+                const int page = new_page[warp][at_stage];
+                if (page >= 0 && cc.grp == 0) {
+                    row = reinterpret_cast<unsigned char*>((lane < 16 ? a.c.k : a.c.v) + row_in_pool(a.c, page, cached));
+                    *reinterpret_cast<uint32_t*>(row + 4 * piece) = codes;
+                    if ((piece & 3) == 0) *reinterpret_cast<uint32_t*>(row + kRow4Codes + piece) = param;
+                    const long long at = slot_in_pool(a.c, page, cached);
+                    if (lane == 0 && a.c.positions != nullptr)
+                        a.c.positions[at] = a.new_positions != nullptr ? a.new_positions[cc.unit % a.c.batch] : cached;
+                    if (lane == 0 && a.c.mass != nullptr && !ACC) a.c.mass[at] = 0.f;
+                }
+                __syncwarp();
+            }
+
+            // S^T: 16 tokens x 8 NG heads
+            float s[COUNT][NG][4];
+#pragma unroll
+            for (int u = 0; u < COUNT; ++u) {
+#pragma unroll
+                for (int t = 0; t < NG; ++t) s[u][t][0] = s[u][t][1] = s[u][t][2] = s[u][t][3] = 0.f;
+                const unsigned char* ra = tile[u] + gid * kRow4;
+                const unsigned char* rb = ra + 8 * kRow4;
+                const uint4 pa = *reinterpret_cast<const uint4*>(ra + kRow4Codes), pb = *reinterpret_cast<const uint4*>(rb + kRow4Codes);
+                const uint32_t para[4] = {pa.x, pa.y, pa.z, pa.w}, parb[4] = {pb.x, pb.y, pb.z, pb.w};
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const uint32_t wa = *reinterpret_cast<const uint32_t*>(ra + 16 * g + 4 * tig), wb = *reinterpret_cast<const uint32_t*>(rb + 16 * g + 4 * tig);
+                    const uint32_t sa = __byte_perm(para[g], 0u, 0x1010), sb = __byte_perm(parb[g], 0u, 0x1010);
+                    const uint32_t ma = fma2(sa, 0xc300c300u, 0x80008000u), mb = fma2(sb, 0xc300c300u, 0x80008000u);     // -128 s
+#pragma unroll
+                    for (int st = 0; st < 2; ++st) {         // the even channels, the odd ones
+                        const uint32_t ca = (st == 0 ? wa : wa >> 4) & kNibbles, cb = (st == 0 ? wb : wb >> 4) & kNibbles;
+                        const uint32_t kf[4] = {fma2(codes_low(ca), sa, ma), fma2(codes_low(cb), sb, mb), fma2(codes_high(ca), sa, ma), fma2(codes_high(cb), sb, mb)};
+#pragma unroll
+                        for (int t = 0; t < NG; ++t) mma4(s[u][t], kf, qf[t][g][st][0], qf[t][g][st][1]);
+                    }
+                }
+                const uint32_t la = *reinterpret_cast<const uint32_t*>(ra + kRow4Codes + 4 * tig), lb = *reinterpret_cast<const uint32_t*>(rb + kRow4Codes + 4 * tig);
+                const uint32_t la2 = __byte_perm(la, 0u, 0x3232), lb2 = __byte_perm(lb, 0u, 0x3232);
+                const uint32_t lf[4] = {la2, lb2, la2, lb2};
+#pragma unroll
+                for (int t = 0; t < NG; ++t) mma4(s[u][t], lf, qs[t][0], qs[t][1]);
+            }
+            if (CAP) {
+#pragma unroll
+                for (int u = 0; u < COUNT; ++u)
+#pragma unroll
+                    for (int t = 0; t < NG; ++t)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) s[u][t][c] = cap_out * tanhf(s[u][t][c] * cap_in);
+            }
+            if (ragged) {                                    // what does not count gets -inf
+#pragma unroll
+                for (int u = 0; u < COUNT; ++u) {
+                    const int ta = base[u] + gid, tb = ta + 8;
+                    const bool la = ta < cc.tokens && !((bits[u] & 1) && ta < cached), lb = tb < cc.tokens && !((bits[u] & 2) && tb < cached);
+#pragma unroll
+                    for (int t = 0; t < NG; ++t) {
+                        if (!la) s[u][t][0] = s[u][t][1] = -INFINITY;
+                        if (!lb) s[u][t][2] = s[u][t][3] = -INFINITY;
+                    }
+                }
+            }
+            if (ACC) {                                       // kept, in base 2, until the sum over the whole unit is known
+                float* col = a.scores + ((long long)cc.unit * a.g + cc.grp * kDecodeHeads + 2 * tig) * a.unit_rows + base[0] + gid;
+#pragma unroll
+                for (int t = 0; t < NG; ++t)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        if (t * 8 + 2 * tig + c < heads) {   // 32 bytes of a head's scores per group of eight lanes
+                            float* at = col + (long long)(t * 8 + c) * a.unit_rows;
+#pragma unroll
+                            for (int u = 0; u < COUNT; ++u) {
+                                at[kTile * u] = s[u][t][c] * scale2;
+                                at[kTile * u + 8] = s[u][t][c + 2] * scale2;
+                            }
+                        }
+            }
+            bool above = false;
+#pragma unroll
+            for (int u = 0; u < COUNT; ++u)
+#pragma unroll
+                for (int t = 0; t < NG; ++t)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) above |= s[u][t][c] > most[t][c & 1];
+            if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+                for (int t = 0; t < NG; ++t) {
+                    float by[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float m = fmaxf(s[0][t][c], s[0][t][c + 2]);
+#pragma unroll
+                        for (int u = 1; u < COUNT; ++u) m = fmaxf(m, fmaxf(s[u][t][c], s[u][t][c + 2]));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) * scale2;
+                        const bool none = most[t][c] == -INFINITY;           // nothing summed yet
+                        const float now = m == -INFINITY ? ref[t][c] : none ? m : fmaxf(m, ref[t][c]);
+                        by[c] = none ? 1.f : ex2f(ref[t][c] - now);
+                        ref[t][c] = now;
+                        sum[t][c] *= by[c];
+                        if (m != -INFINITY) most[t][c] = (now + kSlack) * from_base2;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        o[t][j][0] *= by[0]; o[t][j][1] *= by[1];
+                        o[t][j][2] *= by[0]; o[t][j][3] *= by[1];
+                    }
+                    ol[t][0] *= by[0]; ol[t][1] *= by[1];
+                }
+            }
+            uint32_t pf[COUNT][NG][2], pl[COUNT][NG][2];     // weights as two bf16 terms, the first cut off, the second rounded: within 2^-16
+#pragma unroll
+            for (int u = 0; u < COUNT; ++u)
+#pragma unroll
+                for (int t = 0; t < NG; ++t)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float x = ex2f(fmaf(s[u][t][2 * i], scale2, -ref[t][0])), y = ex2f(fmaf(s[u][t][2 * i + 1], scale2, -ref[t][1]));
+                        sum[t][0] += x; sum[t][1] += y;
+                        const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
+                        pf[u][t][i] = transpose8x8(__byte_perm(xb, yb, 0x7632));
+                        pl[u][t][i] = transpose8x8(pack_bf16(x - __uint_as_float(xb & 0xffff0000u), y - __uint_as_float(yb & 0xffff0000u)));
+                    }
+            // O^T += V^T P^T: 128 channels x 8 NG heads.  The lane has the 16 channels 16 gid + 0..15 of tokens 2 tig, + 1, + 8 and + 9; row gid of the
+            // j-th instruction is channel 16 gid + j, row gid + 8 is 16 gid + 8 + j.
+#pragma unroll
+            for (int u = 0; u < COUNT; ++u) {
+                const unsigned char* r = tile[u] + kTileBytes + 2 * tig * kRow4;
+                uint2 v[4];
+                uint32_t par[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const unsigned char* row = r + ((i & 1) + (i >> 1) * 8) * kRow4;
+                    v[i] = *reinterpret_cast<const uint2*>(row + 8 * gid);
+                    par[i] = *reinterpret_cast<const uint32_t*>(row + kRow4Codes + 4 * (gid >> 1));
+                }
+                const uint32_t s0 = __byte_perm(par[0], par[1], 0x5410), s1 = __byte_perm(par[2], par[3], 0x5410);
+                const uint32_t m0 = fma2(s0, 0xc300c300u, 0x80008000u), m1 = fma2(s1, 0xc300c300u, 0x80008000u);
+#pragma unroll
+                for (int j4 = 0; j4 < 8; j4 += 4) {          // the same bytes of two tokens side by side: channels j4, j4 + 2 in the lower halves of the bytes
+                    const unsigned sel = j4 == 0 ? 0x5140 : 0x7362;
+                    const uint32_t x[4] = {__byte_perm(v[0].x, v[1].x, sel), __byte_perm(v[0].y, v[1].y, sel), __byte_perm(v[2].x, v[3].x, sel), __byte_perm(v[2].y, v[3].y, sel)};
+#pragma unroll
+                    for (int odd = 0; odd < 2; ++odd) {
+                        uint32_t c[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) c[i] = (odd == 0 ? x[i] : x[i] >> 4) & kNibbles;
+#pragma unroll
+                        for (int two = 0; two < 2; ++two) {
+                            const int j = j4 + odd + 2 * two;
+                            uint32_t vf[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) vf[i] = fma2(two == 0 ? codes_low(c[i]) : codes_high(c[i]), i < 2 ? s0 : s1, i < 2 ? m0 : m1);
+#pragma unroll
+                            for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pf[u][t][0], pf[u][t][1]);
+#pragma unroll
+                            for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pl[u][t][0], pl[u][t][1]);
+                        }
+                    }
+                }
+                const uint32_t lf[4] = {__byte_perm(par[0], par[1], 0x7632), 0u, __byte_perm(par[2], par[3], 0x7632), 0u};
+#pragma unroll
+                for (int t = 0; t < NG; ++t) mma4(ol[t], lf, pf[u][t][0], pf[u][t][1]);
+#pragma unroll
+                for (int t = 0; t < NG; ++t) mma4(ol[t], lf, pl[u][t][0], pl[u][t][1]);
             }
             __syncwarp();
-        }
+#pragma unroll 1
+            for (int u = 0; u < COUNT; ++u) issue();
+            stage += COUNT;
+            if (stage >= kStages) stage -= kStages;
+            left_c -= COUNT;
+            cc.tile += COUNT;
+        };
+        if (left_c >= 2 && cc.tile + 1 < cc.tiles) attend(std::integral_constant<int, 2>());
+        else attend(std::integral_constant<int, 1>());
 
-        // S^T: 16 tokens x 8 NG heads
-        float s[NG][4];
-#pragma unroll
-        for (int t = 0; t < NG; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
-        {
-            const unsigned char* ra = tile_k + gid * kRow4;
-            const unsigned char* rb = ra + 8 * kRow4;
-            const uint4 pa = *reinterpret_cast<const uint4*>(ra + kRow4Codes), pb = *reinterpret_cast<const uint4*>(rb + kRow4Codes);
-            const uint32_t para[4] = {pa.x, pa.y, pa.z, pa.w}, parb[4] = {pb.x, pb.y, pb.z, pb.w};
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                uint32_t wa = *reinterpret_cast<const uint32_t*>(ra + 16 * g + 4 * tig), wb = *reinterpret_cast<const uint32_t*>(rb + 16 * g + 4 * tig);
-                const uint32_t sa = __byte_perm(para[g], 0u, 0x1010), sb = __byte_perm(parb[g], 0u, 0x1010);
-                const uint32_t ma = fma2(sa, 0xc300c300u, 0x80008000u), mb = fma2(sb, 0xc300c300u, 0x80008000u);     // -128 s
-#pragma unroll
-                for (int st = 0; st < 2; ++st) {             // the even channels, the odd ones
-                    const uint32_t ca = (st == 0 ? wa : wa >> 4) & kNibbles, cb = (st == 0 ? wb : wb >> 4) & kNibbles;
-                    const uint32_t kf[4] = {fma2(codes_low(ca), sa, ma), fma2(codes_low(cb), sb, mb), fma2(codes_high(ca), sa, ma), fma2(codes_high(cb), sb, mb)};
-#pragma unroll
-                    for (int t = 0; t < NG; ++t) mma4(s[t], kf, qf[t][g][st][0], qf[t][g][st][1]);
-                }
-            }
-            const uint32_t la = *reinterpret_cast<const uint32_t*>(ra + kRow4Codes + 4 * tig), lb = *reinterpret_cast<const uint32_t*>(rb + kRow4Codes + 4 * tig);
-            const uint32_t la2 = __byte_perm(la, 0u, 0x3232), lb2 = __byte_perm(lb, 0u, 0x3232);
-            const uint32_t lf[4] = {la2, lb2, la2, lb2};
-#pragma unroll
-            for (int t = 0; t < NG; ++t) mma4(s[t], lf, qs[t][0], qs[t][1]);
-        }
-        if (CAP) {
-#pragma unroll
-            for (int t = 0; t < NG; ++t)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) s[t][c] = cap_out * tanhf(s[t][c] * cap_in);
-        }
-        if (ragged) {                                        // what does not count gets -inf
-            const int ta = base + gid, tb = ta + 8;
-            const bool la = ta < cc.tokens && !((bits & 1) && ta < cached), lb = tb < cc.tokens && !((bits & 2) && tb < cached);
-#pragma unroll
-            for (int t = 0; t < NG; ++t) {
-                if (!la) s[t][0] = s[t][1] = -INFINITY;
-                if (!lb) s[t][2] = s[t][3] = -INFINITY;
-            }
-        }
-        if (ACC) {                                           // kept, in base 2, until the sum over the whole unit is known
-            float* col = a.scores + ((long long)cc.unit * a.g + cc.grp * kDecodeHeads + 2 * tig) * a.unit_rows + base + gid;
-#pragma unroll
-            for (int t = 0; t < NG; ++t)
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (t * 8 + 2 * tig + c < heads) {       // 32 bytes of a head's scores per group of eight lanes
-                        float* at = col + (long long)(t * 8 + c) * a.unit_rows;
-                        at[0] = s[t][c] * scale2;
-                        at[8] = s[t][c + 2] * scale2;
-                    }
-        }
-        bool above = false;
-#pragma unroll
-        for (int t = 0; t < NG; ++t)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) above |= s[t][c] > most[t][c & 1];
-        if (__any_sync(0xffffffffu, above)) {
-#pragma unroll
-            for (int t = 0; t < NG; ++t) {
-                float by[2];
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float m = fmaxf(s[t][c], s[t][c + 2]);
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) * scale2;
-                    const bool none = most[t][c] == -INFINITY;               // nothing summed yet
-                    const float now = m == -INFINITY ? ref[t][c] : none ? m : fmaxf(m, ref[t][c]);
-                    by[c] = none ? 1.f : ex2f(ref[t][c] - now);
-                    ref[t][c] = now;
-                    sum[t][c] *= by[c];
-                    if (m != -INFINITY) most[t][c] = (now + kSlack) * from_base2;
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    o[t][j][0] *= by[0]; o[t][j][1] *= by[1];
-                    o[t][j][2] *= by[0]; o[t][j][3] *= by[1];
-                }
-                ol[t][0] *= by[0]; ol[t][1] *= by[1];
-            }
-        }
-        uint32_t pf[NG][2], pl[NG][2];                       // weights as two bf16 terms, the first cut off, the second rounded: within 2^-16
-#pragma unroll
-        for (int t = 0; t < NG; ++t) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float x = ex2f(fmaf(s[t][2 * i], scale2, -ref[t][0])), y = ex2f(fmaf(s[t][2 * i + 1], scale2, -ref[t][1]));
-                sum[t][0] += x; sum[t][1] += y;
-                const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
-                pf[t][i] = transpose8x8(__byte_perm(xb, yb, 0x7632));
-                pl[t][i] = transpose8x8(pack_bf16(x - __uint_as_float(xb & 0xffff0000u), y - __uint_as_float(yb & 0xffff0000u)));
-            }
-        }
-        // O^T += V^T P^T: 128 channels x 8 NG heads.  The lane has the 16 channels 16 gid + 0..15 of tokens 2 tig, + 1, + 8 and + 9; row gid of the j-th
-        // instruction is channel 16 gid + j, row gid + 8 is 16 gid + 8 + j.
-        {
-            const unsigned char* r = tile_k + kTileBytes + 2 * tig * kRow4;
-            uint2 v[4];
-            uint32_t par[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const unsigned char* row = r + ((i & 1) + (i >> 1) * 8) * kRow4;
-                v[i] = *reinterpret_cast<const uint2*>(row + 8 * gid);
-                par[i] = *reinterpret_cast<const uint32_t*>(row + kRow4Codes + 4 * (gid >> 1));
-            }
-            const uint32_t s0 = __byte_perm(par[0], par[1], 0x5410), s1 = __byte_perm(par[2], par[3], 0x5410);
-            const uint32_t m0 = fma2(s0, 0xc300c300u, 0x80008000u), m1 = fma2(s1, 0xc300c300u, 0x80008000u);
-#pragma unroll
-            for (int j4 = 0; j4 < 8; j4 += 4) {              // the same bytes of two tokens side by side: channels j4, j4 + 2 in the lower halves of the bytes
-                const unsigned sel = j4 == 0 ? 0x5140 : 0x7362;
-                const uint32_t x[4] = {__byte_perm(v[0].x, v[1].x, sel), __byte_perm(v[0].y, v[1].y, sel), __byte_perm(v[2].x, v[3].x, sel), __byte_perm(v[2].y, v[3].y, sel)};
-#pragma unroll
-                for (int odd = 0; odd < 2; ++odd) {
-                    uint32_t c[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) c[i] = (odd == 0 ? x[i] : x[i] >> 4) & kNibbles;
-#pragma unroll
-                    for (int two = 0; two < 2; ++two) {
-                        const int j = j4 + odd + 2 * two;
-                        uint32_t vf[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) vf[i] = fma2(two == 0 ? codes_low(c[i]) : codes_high(c[i]), i < 2 ? s0 : s1, i < 2 ? m0 : m1);
-#pragma unroll
-                        for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pf[t][0], pf[t][1]);
-#pragma unroll
-                        for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pl[t][0], pl[t][1]);
-                    }
-                }
-            }
-            const uint32_t lf[4] = {__byte_perm(par[0], par[1], 0x7632), 0u, __byte_perm(par[2], par[3], 0x7632), 0u};
-#pragma unroll
-            for (int t = 0; t < NG; ++t) mma4(ol[t], lf, pf[t][0], pf[t][1]);
-#pragma unroll
-            for (int t = 0; t < NG; ++t) mma4(ol[t], lf, pl[t][0], pl[t][1]);
-        }
-        __syncwarp();
-        issue();
-
-        stage = stage + 1 == kStages ? 0 : stage + 1;
-        --left_c;
-        const bool unit_ends = ++cc.tile == cc.tiles;
+        const bool unit_ends = cc.tile == cc.tiles;
         if (unit_ends) left_c -= kUnitCost;
         if (unit_ends || left_c <= 0) {                      // hand over what this warp has of the unit
             const long long slot = (long long)worker + cc.unit * a.groups + cc.grp;
