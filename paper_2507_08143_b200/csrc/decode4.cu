@@ -176,16 +176,14 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
     const uint32_t ring_s = smem_u32(my_ring);
 
     // ---- producer: one tile into a stage.  Lane l copies the 16-byte pieces l, l + 32 and l + 64 of the 80 of either tile; pieces 0 .. 39 are rows 0 .. 7.
-    // A tile that goes on in the page of the one before it (run > 0) is where that one ended; else its page ids are looked up.  They and the queries are
-    // asked for ahead as in the other kernel: 64 page ids of the unit (lane l holds entries e0 + l and e0 + 32 + l), the first 32 of
-    // the unit after it, and the queries of a unit when its first tile is issued.
+    // A tile that goes on in the page of the one before it (run > 0) is where that one ended; else its page ids are looked up.  They are asked
+    // for ahead as in the other kernel: 64 page ids of the unit (lane l holds entries e0 + l and e0 + 32 + l) and the first 32 of the unit after it.
+    // (The queries are not, but for the first unit's: the registers that would hold them are worth more than the wait.)
     Cursor pc = start, nc = start;
     int e0 = (pc.tile * kTile) >> a.c.page_shift;
     int ids = page_ids(a, pc, e0, lane), ids_after = page_ids(a, pc, e0 + 32, lane), ids_next_unit = -1;
-    uint4 qn[NG][4];
-    int q_unit = pc.unit, q_grp = pc.grp;                    // whose queries qn holds
-    bool q_waiting = true;
-    load_queries<NG>(a, pc, qn, lane);
+    uint4 q_first[NG][4];
+    load_queries<NG>(a, pc, q_first, lane);
     if (nc.next_unit(a, live)) ids_next_unit = page_ids(a, nc, 0, lane);
     const int appended = a.k_new != nullptr ? 1 : 0;
     const long long v_from_k = reinterpret_cast<const char*>(a.c.v) - reinterpret_cast<const char*>(a.c.k);
@@ -270,10 +268,6 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                 ids = ids_next_unit;
                 ids_after = page_ids(a, pc, 32, lane);
                 if (nc.next_unit(a, live)) ids_next_unit = page_ids(a, nc, 0, lane);
-                if (!q_waiting) {
-                    load_queries<NG>(a, pc, qn, lane);
-                    q_unit = pc.unit; q_grp = pc.grp; q_waiting = true;
-                }
             }
         }
         cp_commit();
@@ -291,33 +285,25 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
     uint32_t qf[NG][4][2][2], qs[NG][2];
     float o[NG][8][4], ol[NG][4];
     float ref[NG][2], most[NG][2], sum[NG][2];               // reference in base 2; score above which it has to follow (-inf: none yet)
-    bool fresh = true;
     int first_tile = 0, head0 = 0, heads = 0, stage = 0;
+    auto enter = [&](const uint4 (&q)[NG][4]) {              // a new unit or group
+        first_tile = cc.tile;
+        head0 = cc.unit / a.c.batch * a.g + cc.grp * kDecodeHeads;
+        heads = min(kDecodeHeads, a.g - cc.grp * kDecodeHeads);
+        query_operands<NG>(q, qf, qs, lane);
+#pragma unroll
+        for (int t = 0; t < NG; ++t) {
+#pragma unroll
+            for (int s = 0; s < 8; ++s) o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.f;
+            ol[t][0] = ol[t][1] = ol[t][2] = ol[t][3] = 0.f;
+            ref[t][0] = ref[t][1] = 0.f;
+            most[t][0] = most[t][1] = -INFINITY;
+            sum[t][0] = sum[t][1] = 0.f;
+        }
+    };
+    enter(q_first);
 
     while (true) {
-        if (fresh) {                                         // a new unit or group: its queries
-            fresh = false;
-            first_tile = cc.tile;
-            head0 = cc.unit / a.c.batch * a.g + cc.grp * kDecodeHeads;
-            heads = min(kDecodeHeads, a.g - cc.grp * kDecodeHeads);
-            if (q_waiting && q_unit == cc.unit && q_grp == cc.grp) {
-                q_waiting = false;
-                query_operands<NG>(qn, qf, qs, lane);
-            } else {
-                uint4 q[NG][4];
-                load_queries<NG>(a, cc, q, lane);
-                query_operands<NG>(q, qf, qs, lane);
-            }
-#pragma unroll
-            for (int t = 0; t < NG; ++t) {
-#pragma unroll
-                for (int s = 0; s < 8; ++s) o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.f;
-                ol[t][0] = ol[t][1] = ol[t][2] = ol[t][3] = 0.f;
-                ref[t][0] = ref[t][1] = 0.f;
-                most[t][0] = most[t][1] = -INFINITY;
-                sum[t][0] = sum[t][1] = 0.f;
-            }
-        }
         if (left_c <= kStages) pdl_trigger();                // the second kernel's blocks are let in when the tiles run out
         const int cached = cc.tokens - appended;
         // COUNT tiles of the unit, whose steps the compiler interleaves
@@ -565,8 +551,10 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                     }
                 }
             if (left_c <= 0) return;
-            fresh = true;
             cc.next_unit(a, live);
+            uint4 q[NG][4];
+            load_queries<NG>(a, cc, q, lane);
+            enter(q);
         }
     }
 }
