@@ -17,6 +17,8 @@
 #include "decode.cuh"
 #include "quant4.cuh"
 
+#include <cuda_fp16.h>
+
 #include <type_traits>
 
 namespace compactor {
@@ -52,28 +54,54 @@ __device__ __forceinline__ void load_queries(const DecodeArgs& a, const Cursor& 
     }
 }
 
-// B operands of a unit's queries: channels (st, st + 2) and (st + 4, st + 6) of the lane's eight of group g, and the sums of a group's
-// channels, group tig, as three bf16 terms.
+// B operands of a unit's queries: of the lane's eight channels of group g the pairs (0, 4) and (2, 6), then (1, 5) and (3, 7) times 2^-4, as
+// fp16 of q 2^k; the sums of a group's channels, group tig, times 2^(k - 24), as three bf16 terms; and for the two heads of the lane's scores
+// 2^(24 - k).  k brings the head's greatest channel to 2^14 .. 2^15: fp16 holds the eight bits of a bf16 down to 2^-32 of that channel.
 template <int NG>
-__device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t (&qf)[NG][4][2][2], uint32_t (&qs)[NG][2], int lane) {
+__device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t (&qf)[NG][4][2][2], uint32_t (&qs)[NG][2], float (&unscale)[NG][2], int lane) {
     const int tig = lane & 3;
 #pragma unroll
     for (int t = 0; t < NG; ++t) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint4 x = q[t][g];
+            top = max_nan2(top, max_nan2(max_nan2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), max_nan2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+        }
+        top = max_nan2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max_nan2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        top = max_nan2(top, top >> 16 | top << 16);
+        // (queries of 2^118 and more, or not finite, become infinite, and their scores no numbers)
+        const int k = max(-102, min(141 - (int)((top >> 7) & 255u), 126));
+        const float up = __int_as_float((k + 127) << 23), down = __int_as_float((127 + 24 - k) << 23);
         float mine = 0.f;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const uint4 x = q[t][g];
-            qf[t][g][0][0] = __byte_perm(x.x, x.y, 0x5410); qf[t][g][0][1] = __byte_perm(x.z, x.w, 0x5410);
-            qf[t][g][1][0] = __byte_perm(x.x, x.y, 0x7632); qf[t][g][1][1] = __byte_perm(x.z, x.w, 0x7632);
-            float sum = ((bf16_lo(x.x) + bf16_hi(x.x)) + (bf16_lo(x.y) + bf16_hi(x.y))) + ((bf16_lo(x.z) + bf16_hi(x.z)) + (bf16_lo(x.w) + bf16_hi(x.w)));
+            float sum = 0.f;
+#pragma unroll
+            for (int odd = 0; odd < 2; ++odd) {
+                const uint32_t w[4] = {x.x, x.z, x.y, x.w};
+                const float by = odd == 0 ? up : up * 0.0625f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float lo = odd == 0 ? bf16_lo(w[2 * i]) : bf16_hi(w[2 * i]), hi = odd == 0 ? bf16_lo(w[2 * i + 1]) : bf16_hi(w[2 * i + 1]);
+                    sum += lo + hi;
+                    const __half2 h = __floats2half2_rn(lo * by, hi * by);
+                    qf[t][g][odd][i] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+            }
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
             if (g == tig) mine = sum;
         }
+        mine *= up * 0x1p-24f;
         const float t0 = __bfloat162float(__float2bfloat16_rn(mine)), r0 = mine - t0;
         const float t1 = __bfloat162float(__float2bfloat16_rn(r0)), t2 = r0 - t1;
         qs[t][0] = pack_bf16(t0, t1);
         qs[t][1] = pack_bf16(t2, 0.f);
+        unscale[t][0] = __shfl_sync(0xffffffffu, down, 8 * tig);
+        unscale[t][1] = __shfl_sync(0xffffffffu, down, 8 * tig + 4);
     }
 }
 
@@ -81,10 +109,18 @@ __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t
 __device__ __forceinline__ uint32_t codes_low(uint32_t x) { return __byte_perm(x, 0x43434343u, 0x4140); }
 __device__ __forceinline__ uint32_t codes_high(uint32_t x) { return __byte_perm(x, 0x43434343u, 0x4342); }
 constexpr uint32_t kNibbles = 0x0f0f0f0fu;
+constexpr uint32_t kFirst = 0x000f000fu, kSecond = 0x00f000f0u;      // codes of two channels as fp16: c 2^-24, and c 2^-20
 
 // The instruction of decode.cuh, free to be placed where its operands are ready.
 __device__ __forceinline__ void mma4(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// The same in fp16: codes of keys times queries.
+__device__ __forceinline__ void mma_codes(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -280,9 +316,9 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
     // tiles need neither the maximum over the warp's lanes nor a new scale of what is summed.
     constexpr float kSlack = 8.f;
     Cursor cc = start;
-    const float scale2 = CAP ? 1.f : a.scale * kLog2e, from_base2 = 1.f / scale2;
-    const float cap_in = CAP ? a.scale / a.softcap : 0.f, cap_out = CAP ? a.softcap * kLog2e : 0.f;
+    const float scale2 = CAP ? a.scale / a.softcap : a.scale * kLog2e, cap_out = CAP ? a.softcap * kLog2e : 0.f;
     uint32_t qf[NG][4][2][2], qs[NG][2];
+    float to_base2[NG][2];                                   // from the scores as they are summed (when they are capped, to what the cap takes)
     float o[NG][8][4], ol[NG][4];
     float ref[NG][2], most[NG][2], sum[NG][2];               // reference in base 2; score above which it has to follow (-inf: none yet)
     int first_tile = 0, head0 = 0, heads = 0, stage = 0;
@@ -290,12 +326,13 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
         first_tile = cc.tile;
         head0 = cc.unit / a.c.batch * a.g + cc.grp * kDecodeHeads;
         heads = min(kDecodeHeads, a.g - cc.grp * kDecodeHeads);
-        query_operands<NG>(q, qf, qs, lane);
+        query_operands<NG>(q, qf, qs, to_base2, lane);
 #pragma unroll
         for (int t = 0; t < NG; ++t) {
 #pragma unroll
             for (int s = 0; s < 8; ++s) o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.f;
             ol[t][0] = ol[t][1] = ol[t][2] = ol[t][3] = 0.f;
+            to_base2[t][0] *= scale2; to_base2[t][1] *= scale2;
             ref[t][0] = ref[t][1] = 0.f;
             most[t][0] = most[t][1] = -INFINITY;
             sum[t][0] = sum[t][1] = 0.f;
@@ -355,26 +392,28 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                 for (int t = 0; t < NG; ++t) s[u][t][0] = s[u][t][1] = s[u][t][2] = s[u][t][3] = 0.f;
                 const unsigned char* ra = tile[u] + gid * kRow4;
                 const unsigned char* rb = ra + 8 * kRow4;
-                const uint4 pa = *reinterpret_cast<const uint4*>(ra + kRow4Codes), pb = *reinterpret_cast<const uint4*>(rb + kRow4Codes);
-                const uint32_t para[4] = {pa.x, pa.y, pa.z, pa.w}, parb[4] = {pb.x, pb.y, pb.z, pb.w};
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const uint32_t wa = *reinterpret_cast<const uint32_t*>(ra + 16 * g + 4 * tig), wb = *reinterpret_cast<const uint32_t*>(rb + 16 * g + 4 * tig);
-                    const uint32_t sa = __byte_perm(para[g], 0u, 0x1010), sb = __byte_perm(parb[g], 0u, 0x1010);
-                    const uint32_t ma = fma2(sa, 0xc300c300u, 0x80008000u), mb = fma2(sb, 0xc300c300u, 0x80008000u);     // -128 s
-#pragma unroll
-                    for (int st = 0; st < 2; ++st) {         // the even channels, the odd ones
-                        const uint32_t ca = (st == 0 ? wa : wa >> 4) & kNibbles, cb = (st == 0 ? wb : wb >> 4) & kNibbles;
-                        const uint32_t kf[4] = {fma2(codes_low(ca), sa, ma), fma2(codes_low(cb), sb, mb), fma2(codes_high(ca), sa, ma), fma2(codes_high(cb), sb, mb)};
-#pragma unroll
-                        for (int t = 0; t < NG; ++t) mma4(s[u][t], kf, qf[t][g][st][0], qf[t][g][st][1]);
-                    }
-                }
                 const uint32_t la = *reinterpret_cast<const uint32_t*>(ra + kRow4Codes + 4 * tig), lb = *reinterpret_cast<const uint32_t*>(rb + kRow4Codes + 4 * tig);
                 const uint32_t la2 = __byte_perm(la, 0u, 0x3232), lb2 = __byte_perm(lb, 0u, 0x3232);
                 const uint32_t lf[4] = {la2, lb2, la2, lb2};
 #pragma unroll
                 for (int t = 0; t < NG; ++t) mma4(s[u][t], lf, qs[t][0], qs[t][1]);
+                const uint4 pa = *reinterpret_cast<const uint4*>(ra + kRow4Codes), pb = *reinterpret_cast<const uint4*>(rb + kRow4Codes);
+                const uint32_t para[4] = {pa.x, pa.y, pa.z, pa.w}, parb[4] = {pb.x, pb.y, pb.z, pb.w};
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const uint32_t wa = *reinterpret_cast<const uint32_t*>(ra + 16 * g + 4 * tig), wb = *reinterpret_cast<const uint32_t*>(rb + 16 * g + 4 * tig);
+                    const uint32_t wa8 = wa >> 8, wb8 = wb >> 8;
+                    const uint32_t kf[2][4] = {{wa & kFirst, wb & kFirst, wa8 & kFirst, wb8 & kFirst}, {wa & kSecond, wb & kSecond, wa8 & kSecond, wb8 & kSecond}};
+                    const float sa = bf16_lo(para[g]), sb = bf16_lo(parb[g]);
+#pragma unroll
+                    for (int t = 0; t < NG; ++t) {
+                        float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int odd = 0; odd < 2; ++odd) mma_codes(x, kf[odd], qf[t][g][odd][0], qf[t][g][odd][1]);
+                        s[u][t][0] = fmaf(sa, x[0], s[u][t][0]); s[u][t][1] = fmaf(sa, x[1], s[u][t][1]);
+                        s[u][t][2] = fmaf(sb, x[2], s[u][t][2]); s[u][t][3] = fmaf(sb, x[3], s[u][t][3]);
+                    }
+                }
             }
             if (CAP) {
 #pragma unroll
@@ -382,7 +421,7 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
 #pragma unroll
                     for (int t = 0; t < NG; ++t)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) s[u][t][c] = cap_out * tanhf(s[u][t][c] * cap_in);
+                        for (int c = 0; c < 4; ++c) s[u][t][c] = cap_out * tanhf(s[u][t][c] * to_base2[t][c & 1]);
             }
             if (ragged) {                                    // what does not count gets -inf
 #pragma unroll
@@ -406,8 +445,8 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                             float* at = col + (long long)(t * 8 + c) * a.unit_rows;
 #pragma unroll
                             for (int u = 0; u < COUNT; ++u) {
-                                at[kTile * u] = s[u][t][c] * scale2;
-                                at[kTile * u + 8] = s[u][t][c + 2] * scale2;
+                                at[kTile * u] = s[u][t][c] * (CAP ? 1.f : to_base2[t][c]);
+                                at[kTile * u + 8] = s[u][t][c + 2] * (CAP ? 1.f : to_base2[t][c]);
                             }
                         }
             }
@@ -429,13 +468,13 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                         for (int u = 1; u < COUNT; ++u) m = fmaxf(m, fmaxf(s[u][t][c], s[u][t][c + 2]));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) * scale2;
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) * (CAP ? 1.f : to_base2[t][c]);
                         const bool none = most[t][c] == -INFINITY;           // nothing summed yet
                         const float now = m == -INFINITY ? ref[t][c] : none ? m : fmaxf(m, ref[t][c]);
                         by[c] = none ? 1.f : ex2f(ref[t][c] - now);
                         ref[t][c] = now;
                         sum[t][c] *= by[c];
-                        if (m != -INFINITY) most[t][c] = (now + kSlack) * from_base2;
+                        if (m != -INFINITY) most[t][c] = CAP ? now + kSlack : (now + kSlack) / to_base2[t][c];
                     }
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
@@ -452,7 +491,8 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                 for (int t = 0; t < NG; ++t)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float x = ex2f(fmaf(s[u][t][2 * i], scale2, -ref[t][0])), y = ex2f(fmaf(s[u][t][2 * i + 1], scale2, -ref[t][1]));
+                        const float x = ex2f(CAP ? s[u][t][2 * i] - ref[t][0] : fmaf(s[u][t][2 * i], to_base2[t][0], -ref[t][0]));
+                        const float y = ex2f(CAP ? s[u][t][2 * i + 1] - ref[t][1] : fmaf(s[u][t][2 * i + 1], to_base2[t][1], -ref[t][1]));
                         sum[t][0] += x; sum[t][1] += y;
                         const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
                         pf[u][t][i] = transpose8x8(__byte_perm(xb, yb, 0x7632));
