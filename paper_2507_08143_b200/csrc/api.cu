@@ -1411,7 +1411,7 @@ extern "C" size_t compactor_paged_select_workspace_bytes(const compactor_paged_c
     const long long capacity = std::min<long long>(max_length, (long long)cache->max_pages * cache->page_tokens);
     const long long pages = (capacity + cache->page_tokens - 1) / cache->page_tokens;
     if (pages > kSelectMaxPages) return 0;
-    return align_up(sizeof(uint32_t) * (size_t)cache->heads * cache->batch * pages);
+    return 2 * align_up(sizeof(uint32_t) * (size_t)cache->heads * cache->batch * pages);
 }
 extern "C" int compactor_paged_select(const compactor_paged_cache* cache, int32_t layer, const compactor_select_options* options,
                                       compactor_rows q, compactor_rows k_new, const int32_t* lengths, void* bounds, int32_t* table_out,
@@ -1435,7 +1435,8 @@ extern "C" int compactor_paged_select(const compactor_paged_cache* cache, int32_
     a.unit_pages = (a.capacity + cache->page_tokens - 1) / cache->page_tokens;
     if (a.unit_pages > kSelectMaxPages || (long long)a.units * a.unit_pages > 0x7fffffffLL || (long long)a.units * options->pages > (1LL << 40))
         return COMPACTOR_E_TOO_LARGE;
-    if (workspace_bytes < sizeof(uint32_t) * (size_t)a.units * a.unit_pages) return COMPACTOR_E_WORKSPACE;
+    const size_t keys_bytes = align_up(sizeof(uint32_t) * (size_t)a.units * a.unit_pages);
+    if (workspace_bytes < 2 * keys_bytes) return COMPACTOR_E_WORKSPACE;
     const size_t first = (size_t)layer * a.units;
     a.c.table += first * cache->max_pages;
     a.lengths = lengths + first;
@@ -1445,6 +1446,7 @@ extern "C" int compactor_paged_select(const compactor_paged_cache* cache, int32_
     a.bounds = static_cast<__nv_bfloat16*>(bounds);
     a.table_out = table_out; a.lengths_out = lengths_out;
     a.keys = static_cast<uint32_t*>(workspace);
+    a.errors = reinterpret_cast<float*>(static_cast<char*>(workspace) + keys_bytes);
     a.g = options->q_per_kv; a.pages = options->pages; a.first_pages = options->first_pages; a.last_pages = options->last_pages;
     if (status != nullptr) CK(cudaMemsetAsync(a.status, 0, sizeof(int32_t) * a.units, st));
     compactor::set_chain_for(0);

@@ -154,7 +154,8 @@ struct SelectArgs {
     int* table_out;                        // [units][pages]
     int* lengths_out;                      // [units]
     int* status;
-    uint32_t* keys;                        // workspace: [units][unit_pages]
+    uint32_t* keys;                        // workspace: [units][unit_pages] scores, as ordered integers
+    float* errors;                         // workspace: [units][unit_pages] how far they may be off
     int g, units, capacity, unit_pages;
     int pages, first_pages, last_pages;
 };
