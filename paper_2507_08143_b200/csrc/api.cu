@@ -1450,7 +1450,7 @@ extern "C" int compactor_paged_select(const compactor_paged_cache* cache, int32_
     a.g = options->q_per_kv; a.pages = options->pages; a.first_pages = options->first_pages; a.last_pages = options->last_pages;
     if (status != nullptr) CK(cudaMemsetAsync(a.status, 0, sizeof(int32_t) * a.units, st));
     compactor::set_chain_for(0);
-    CK(launch_paged_select(a, st));
+    CK(launch_paged_select(a, sm_count(), st));
     return COMPACTOR_OK;
 }
 

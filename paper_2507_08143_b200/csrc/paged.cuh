@@ -160,7 +160,7 @@ struct SelectArgs {
     int pages, first_pages, last_pages;
 };
 constexpr int kSelectMaxPages = 49152;     // most pages of a unit: their keys lie in shared memory
-cudaError_t launch_paged_select(const SelectArgs& a, cudaStream_t stream);
+cudaError_t launch_paged_select(const SelectArgs& a, int sm_count, cudaStream_t stream);
 
 struct EvictArgs {
     Paged c;

@@ -9,11 +9,11 @@
 // The choice must not depend on the order of a sum, and next to the last place that is given away scores lie as close as they like; sums
 // in 64 bits for all pages, though, took 15 us for 8 x 2048 pages and 34 for 128 ragged units, most of it conversions.  So there are two kernels:
 //   1. scores by matrix instructions, 16 pages a warp: the sum is [least | greatest] times [min(q, 0) | max(q, 0)], products exact, sums in fp32; and a
-//      bound of each score's error, from the same sum over absolute values.
-//   2. a block per unit finds the T that the last place would go to by these scores.  With E the greatest of the error bounds, the last place's
-//      true score lies within E of T, so a page more than 3 E above T is taken and one more than 3 E below is not, whatever the errors (and the one rounding
-//      to fp32 that the definition has: 2^-24 of a score is far below E).  If there are just as many pages in between as places, all of them are taken;
-//      else those few are summed again, in 64 bits and rounded once, and compared by that.
+//      bound of each score's error, from the same sum over absolute values.  The warps of a grid that fills the GPU share the pages of all units.
+//   2. a block per unit finds an interval of scores that holds the last place, by a histogram of 2048 even steps between the least and the greatest
+//      score, and another within a step while it holds many pages.  With E the greatest of the error bounds, a page more than 3 E above
+//      the interval is taken and one more than 3 E below is not, whatever the errors (and the one rounding to fp32 that the definition
+//      has: 2^-24 of a score is far below E).  The few pages in between are summed again, in 64 bits and rounded once, and compared by that.
 // Bound by the chain of launches and dependent reads (length, page ids, bounds, scores); the bytes are 512 per page.
 #include "paged.cuh"
 #include "quant4.cuh"
@@ -23,7 +23,6 @@ namespace {
 
 constexpr uint32_t kKeyAlways = 0xffffffffu, kKeyNan = 0xfffffffeu;
 constexpr int kScoreWarps = 4;
-constexpr int kScorePages = 16 * kScoreWarps;
 
 __device__ __forceinline__ uint32_t score_key(float x) {
     if (x != x) return kKeyNan;                              // as in the other selections: not a number ranks above +inf
@@ -49,31 +48,25 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 // summands, three additions: 71 2^-23 of the sum of absolute values (which is itself no more than that far off).
 constexpr float kScoreError = 0x1p-16f;
 
-__global__ void __launch_bounds__(kScoreWarps * 32)
-score_pages_kernel(const __grid_constant__ SelectArgs a, int chunks) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
-    pdl_trigger();
-    pdl_wait();
-    const int unit = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
+// Runs of 16 pages of a unit whose scores are asked for.
+__device__ __forceinline__ int runs_of(const SelectArgs& a, int unit) {
     const long long t = select_tokens(a, unit);
     const int pages = t > 0 ? (int)((t + (1 << a.c.page_shift) - 1) >> a.c.page_shift) : 0;
-    const int h = unit / a.c.batch, b = unit - h * a.c.batch;
-    if (chunk == 0 && a.k_new != nullptr && t > 0 && warp == 0) {            // the new key enters the bounds of its page, whose score is not asked for
-        const int page = page_of<false>(a.c, unit, (int)(t - 1)), piece = lane & 15;
-        if (page >= 0) {
-            const uint4 x = *(reinterpret_cast<const uint4*>(a.k_new + b * a.kn_seq + h * a.kn_head) + piece);
-            uint4* at = reinterpret_cast<uint4*>(a.bounds + (long long)page * 2 * kD + (lane >> 4) * kD) + piece;
-            uint4 y = x;
-            if (((t - 1) & ((1 << a.c.page_shift) - 1)) != 0) {
-                const uint4 old = *at;
-                y = lane < 16 ? make_uint4(min_nan2(old.x, x.x), min_nan2(old.y, x.y), min_nan2(old.z, x.z), min_nan2(old.w, x.w))
-                              : make_uint4(max_nan2(old.x, x.x), max_nan2(old.y, x.y), max_nan2(old.z, x.z), max_nan2(old.w, x.w));
-            }
-            *at = y;
-        }
+    return pages <= a.pages ? 0 : (pages + 15) / 16;         // (where all pages are taken: none)
+}
+
+// Scores of one run, by a warp.  `cum`, `per`: runs before the units unit = i per, for i = 0, 1, ...
+__device__ __forceinline__ void score_run(const SelectArgs& a, const int* cum, int per, int run, int lane) {
+    const int gid = lane >> 2, tig = lane & 3;
+    int lo = 0, hi = kScoreWarps * 32;                       // cum[lo] <= run < cum[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cum[mid] <= run) lo = mid; else hi = mid;
     }
-    const int first = chunk * kScorePages + warp * 16;
-    if (first >= pages || pages <= a.pages) return;          // (all pages are taken: no score is asked for)
+    int unit = lo * per, nth = run - cum[lo];
+    for (int n = runs_of(a, unit); nth >= n; n = runs_of(a, ++unit)) nth -= n;
+    const int pages = (int)((select_tokens(a, unit) + (1 << a.c.page_shift) - 1) >> a.c.page_shift), first = 16 * nth;
+    const int h = unit / a.c.batch, b = unit - h * a.c.batch;
     // rows gid and gid + 8 of the warp's pages; the lane has the 16-byte pieces tig + 4 i of their least and greatest values
     uint4 low[2][4], high[2][4];
     int page[2];
@@ -132,65 +125,47 @@ score_pages_kernel(const __grid_constant__ SelectArgs a, int chunks) {
     }
 }
 
-// A block per unit: radix selection of the key of the last place (digits of 11, 11 and 10 bits), then the pages above it and, as far as there
-// is room, the first of those that have it, in their order.
+__global__ void __launch_bounds__(kScoreWarps * 32, 4)
+score_pages_kernel(const __grid_constant__ SelectArgs a) {
+    constexpr int kThreads = kScoreWarps * 32;
+    __shared__ int cum[kThreads + 1];                        // runs before each thread's share of the units
+    __shared__ int warp_sum[kScoreWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_trigger();
+    pdl_wait();
+    const int per = (a.units + kThreads - 1) / kThreads, u0 = min(a.units, tid * per), u1 = min(a.units, u0 + per);
+    int mine = 0;
+    for (int u = u0; u < u1; ++u) mine += runs_of(a, u);
+    int incl = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+    }
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kScoreWarps; ++w) incl += w < warp ? warp_sum[w] : 0;
+    cum[tid + 1] = incl;
+    if (tid == 0) cum[0] = 0;
+    __syncthreads();
+    const int all = cum[kThreads];
+    for (int run = warp * gridDim.x + blockIdx.x; run < all; run += kScoreWarps * gridDim.x) score_run(a, cum, per, run, lane);
+}
 constexpr int kPickThreads = 512;
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kBins = 2048;
+constexpr int kFew = 32;                       // pages in an interval that are not worth another histogram
+constexpr int kRounds = 8;                     // most histograms
 
 struct PickShared {
     int hist[kBins];
     int warp_a[kPickWarps], warp_b[kPickWarps];
-    float warp_e[kPickWarps];
-    int digit, left;
+    uint32_t warp_x[kPickWarps], warp_y[kPickWarps], warp_e[kPickWarps];
+    int step, step_before, step_count, listed;
+    int list[kPickThreads];                    // pages next to the last place
+    uint32_t list_key[kPickThreads];
 };
-
-// The count-th greatest of the keys; `left`: how many of the keys that equal it are among the count greatest.
-__device__ __forceinline__ uint32_t last_place(PickShared& s, const uint32_t* key, int pages, int count, int& left) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr int kPer = kBins / kPickThreads;
-    uint32_t prefix = 0;
-    int shift = 32;
-    left = count;
-#pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-        const int bits = pass < 2 ? 11 : 10, next = shift - bits;
-        *reinterpret_cast<int4*>(s.hist + tid * kPer) = make_int4(0, 0, 0, 0);
-        static_assert(kPer == 4, "four bins a thread");
-        __syncthreads();
-        for (int i = tid; i < pages; i += kPickThreads) {
-            const uint32_t k = key[i];
-            if (pass == 0 || (k >> shift) == prefix) atomicAdd(&s.hist[(k >> next) & ((1u << bits) - 1u)], 1);
-        }
-        __syncthreads();
-        // from the highest digit down: each thread a run of four
-        const int4 v = *reinterpret_cast<const int4*>(s.hist + kBins - kPer - tid * kPer);
-        const int c[4] = {v.w, v.z, v.y, v.x}, sum = v.x + v.y + v.z + v.w;
-        int upto = sum;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += o;
-        }
-        if (lane == 31) s.warp_a[warp] = upto;
-        __syncthreads();
-        int before = upto - sum;
-#pragma unroll
-        for (int w = 0; w < kPickWarps; ++w) before += w < warp ? s.warp_a[w] : 0;
-        if (before < left && left <= before + sum) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (before < left && left <= before + c[i]) { s.digit = kBins - 1 - tid * kPer - i; s.left = left - before; }
-                before += c[i];
-            }
-        }
-        __syncthreads();
-        prefix = (prefix << bits) | (uint32_t)s.digit;
-        left = s.left;
-        shift = next;
-    }
-    return prefix;
-}
 
 // The score of a page as it is defined, summed in 64 bits and rounded once; by a warp, four channels a lane.
 __device__ __forceinline__ uint32_t exact_key(const SelectArgs& a, int unit, int page) {
@@ -215,6 +190,31 @@ __device__ __forceinline__ uint32_t exact_key(const SelectArgs& a, int unit, int
     return nan ? kKeyNan : score_key((float)best);
 }
 
+// Sums of two counts over the block, in every thread.
+__device__ __forceinline__ void block_sums(PickShared& s, int& x, int& y) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    x = __reduce_add_sync(0xffffffffu, x);
+    y = __reduce_add_sync(0xffffffffu, y);
+    __syncthreads();
+    if (lane == 0) { s.warp_a[warp] = x; s.warp_b[warp] = y; }
+    __syncthreads();
+    x = __reduce_add_sync(0xffffffffu, lane < kPickWarps ? s.warp_a[lane] : 0);
+    y = __reduce_add_sync(0xffffffffu, lane < kPickWarps ? s.warp_b[lane] : 0);
+}
+// The least of x and the greatest of y and e.
+__device__ __forceinline__ void block_range(PickShared& s, uint32_t& x, uint32_t& y, uint32_t& e) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    x = __reduce_min_sync(0xffffffffu, x);
+    y = __reduce_max_sync(0xffffffffu, y);
+    e = __reduce_max_sync(0xffffffffu, e);
+    __syncthreads();
+    if (lane == 0) { s.warp_x[warp] = x; s.warp_y[warp] = y; s.warp_e[warp] = e; }
+    __syncthreads();
+    x = __reduce_min_sync(0xffffffffu, lane < kPickWarps ? s.warp_x[lane] : 0xffffffffu);
+    y = __reduce_max_sync(0xffffffffu, lane < kPickWarps ? s.warp_y[lane] : 0u);
+    e = __reduce_max_sync(0xffffffffu, lane < kPickWarps ? s.warp_e[lane] : 0u);
+}
+
 __global__ void __launch_bounds__(kPickThreads)
 pick_pages_kernel(const __grid_constant__ SelectArgs a) {
     extern __shared__ __align__(16) uint32_t key[];
@@ -223,10 +223,23 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
     pdl_trigger();
     pdl_wait();
     const int unit = blockIdx.x;
+    // what the first pages of a unit are about is asked for before its length is known
+    constexpr int kAhead = 4;
+    const uint32_t* keys = a.keys + (long long)unit * a.unit_pages;
+    const float* errors = a.errors + (long long)unit * a.unit_pages;
+    const int* row = a.c.table + (long long)unit * a.c.max_pages;
+    const bool scored = a.unit_pages > a.pages;
+    uint32_t key_ahead[kAhead];
+    float error_ahead[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+        const bool in = scored && tid + j * kPickThreads < a.unit_pages;
+        key_ahead[j] = in ? keys[tid + j * kPickThreads] : 0u;
+        error_ahead[j] = in ? errors[tid + j * kPickThreads] : 0.f;
+    }
     const long long t = select_tokens(a, unit);
     const int page_tokens = 1 << a.c.page_shift;
     const int pages = t > 0 ? (int)((t + page_tokens - 1) >> a.c.page_shift) : 0, count = min(pages, a.pages);
-    const int* row = a.c.table + (long long)unit * a.c.max_pages;
     int* out = a.table_out + (long long)unit * a.pages;
     if (tid == 0) {
         int n = (int)max(t, -1LL);                           // -1 where there is no sequence, or none that fits
@@ -234,6 +247,20 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
         if (t == -1) n = a.lengths[unit];
         a.lengths_out[unit] = n;
         if (t == -2 && a.status != nullptr) atomicOr(a.status + unit, COMPACTOR_STATUS_CAPACITY);
+    }
+    if (warp == kPickWarps - 1 && a.k_new != nullptr && t > 0) {             // the new key enters the bounds of its page (which is taken without a score)
+        const int page = page_of<false>(a.c, unit, (int)(t - 1)), piece = lane & 15, h = unit / a.c.batch, b = unit - h * a.c.batch;
+        if (page >= 0) {
+            const uint4 x = *(reinterpret_cast<const uint4*>(a.k_new + b * a.kn_seq + h * a.kn_head) + piece);
+            uint4* at = reinterpret_cast<uint4*>(a.bounds + (long long)page * 2 * kD + (lane >> 4) * kD) + piece;
+            uint4 y = x;
+            if (((t - 1) & (page_tokens - 1)) != 0) {
+                const uint4 old = *at;
+                y = lane < 16 ? make_uint4(min_nan2(old.x, x.x), min_nan2(old.y, x.y), min_nan2(old.z, x.z), min_nan2(old.w, x.w))
+                              : make_uint4(max_nan2(old.x, x.x), max_nan2(old.y, x.y), max_nan2(old.z, x.z), max_nan2(old.w, x.w));
+            }
+            *at = y;
+        }
     }
     for (int i = count + tid; i < a.pages; i += kPickThreads) out[i] = -1;
     if (pages <= a.pages) {
@@ -244,84 +271,182 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
         }
         return;
     }
-    const uint32_t* keys = a.keys + (long long)unit * a.unit_pages;
-    const float* errors = a.errors + (long long)unit * a.unit_pages;
-    float worst = 0.f;
+    // pages that this thread has in the emission: a run of whole words of 32 pages per warp; their ids are asked for now
+    const int per_warp = ((pages + 31) / 32 + kPickWarps - 1) / kPickWarps * 32;
+    const int p0 = min(pages, warp * per_warp), p1 = min(pages, p0 + per_warp);
+    int id_ahead[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) id_ahead[j] = p0 + 32 * j + lane < p1 ? row[p0 + 32 * j + lane] : -1;
+    uint32_t worst_bits = 0u, low_key = 0xffffffffu, high_key = 0u;          // greatest error; least and greatest of the finite scores
+    int above = 0, between = 0;                              // keys above the finite scores, finite scores
     bool vague = false;                                      // scores that say nothing: bounds or queries that are not finite, or sums near the end of the range
-#pragma unroll 4
-    for (int i = tid; i < pages; i += kPickThreads) {
-        const float e = errors[i];
-        key[i] = keys[i];
-        if (e < INFINITY) worst = fmaxf(worst, e);
+    const uint32_t kInfinite = score_key(INFINITY), kLeast = score_key(-INFINITY);
+    auto scan = [&](uint32_t k) {
+        above += k >= kInfinite;
+        if (k < kInfinite && k > kLeast) { ++between; low_key = min(low_key, k); high_key = max(high_key, k); }
+    };
+    auto take_in = [&](int i, uint32_t k, float e) {
+        key[i] = k;
+        if (e < INFINITY) { worst_bits = max(worst_bits, __float_as_uint(e)); scan(k); }
         else vague = true;
-    }
+    };
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) worst = fmaxf(worst, __shfl_xor_sync(0xffffffffu, worst, d));
-    if (lane == 0) s.warp_e[warp] = worst;
-    const bool any_vague = __syncthreads_or(vague);
-#pragma unroll
-    for (int w = 0; w < kPickWarps; ++w) worst = fmaxf(worst, s.warp_e[w]);
-    if (any_vague) {
+    for (int j = 0; j < kAhead; ++j)
+        if (tid + j * kPickThreads < pages) take_in(tid + j * kPickThreads, key_ahead[j], error_ahead[j]);
+    for (int i = tid + kAhead * kPickThreads; i < pages; i += kPickThreads) take_in(i, keys[i], errors[i]);
+    if (__syncthreads_or(vague)) {
         for (int i = warp; i < pages; i += kPickWarps) {
             if (errors[i] < INFINITY) continue;
             const uint32_t k = exact_key(a, unit, row[i]);   // (its page is one: those that are none have no error)
-            if (lane == 0) key[i] = k;
+            if (lane == 0) { key[i] = k; scan(k); }
         }
-        __syncthreads();
     }
-    int left;
-    const uint32_t last = last_place(s, key, pages, count, left);
-    uint32_t from = last, upto = last;                       // keys in between share the `left` last places
-    if (last != 0u && last < kKeyNan && key_score(last) - key_score(last) == 0.f && worst > 0.f) {
-        from = max(1u, score_key(key_score(last) - 3.f * worst));
-        upto = score_key(key_score(last) + 3.f * worst);
-        int above = 0, between = 0;
+    block_range(s, low_key, high_key, worst_bits);
+    block_sums(s, above, between);
+    const float worst = __uint_as_float(worst_bits);
+    // Keys above `upto` are taken, those below `from` are not, the `left` last places go to those in between: to the first of them where they
+    // are all alike.  At first: what has no finite score on either side of what has.
+    uint32_t from = low_key, upto = high_key;
+    float low = key_score(low_key), high = key_score(high_key);
+    auto count_keys = [&]() {
+        above = between = 0;
         for (int i = tid; i < pages; i += kPickThreads) {
             const uint32_t k = key[i];
             above += k > upto;
             between += k >= from && k <= upto;
         }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) { above += __shfl_xor_sync(0xffffffffu, above, d); between += __shfl_xor_sync(0xffffffffu, between, d); }
-        if (lane == 0) { s.warp_a[warp] = above; s.warp_b[warp] = between; }
+        block_sums(s, above, between);
+    };
+    bool alike = false;
+    if (count <= above || above + between < count) {         // the last place goes to a key that is no finite score: always taken, not a number, infinite or of no page
+        alike = true;
+        const uint32_t special[5] = {kKeyAlways, kKeyNan, score_key(INFINITY), score_key(-INFINITY), 0u};
+        for (int i = 0; i < 5; ++i) {
+            from = upto = special[i];
+            count_keys();
+            if (above < count && count <= above + between) break;
+        }
+    }
+    // ---- smaller and smaller intervals of scores around the last place
+    for (int round = 0; !alike && between > kFew && round < kRounds; ++round) {
+        if (upto == from) { alike = worst == 0.f; break; }
+        const float per = (float)kBins / (high - low);       // (0, infinite or not a number where the scores leave no room for steps)
+        if (!(per > 0.f) || !(per < 0x1p120f)) break;
+        for (int i = tid; i < kBins; i += kPickThreads) s.hist[i] = 0;
         __syncthreads();
-        above = between = 0;
+        auto step_of = [&](uint32_t k) { return min(kBins - 1, (int)((key_score(k) - low) * per)); };      // rises with the score, ties with ties
+        for (int i = tid; i < pages; i += kPickThreads) {
+            const uint32_t k = key[i];
+            if (k >= from && k <= upto) atomicAdd(&s.hist[step_of(k)], 1);
+        }
+        __syncthreads();
+        // from the highest step down: each thread a run of four
+        constexpr int kPer = kBins / kPickThreads;
+        static_assert(kPer == 4, "four steps a thread");
+        const int4 v = *reinterpret_cast<const int4*>(s.hist + kBins - kPer - tid * kPer);
+        const int c[4] = {v.w, v.z, v.y, v.x}, sum = v.x + v.y + v.z + v.w;
+        int incl = sum;
 #pragma unroll
-        for (int w = 0; w < kPickWarps; ++w) { above += s.warp_a[w]; between += s.warp_b[w]; }
-        left = count - above;
-        if (between > left) {
-            for (int i0 = warp * 32; i0 < pages; i0 += kPickThreads) {       // a warp sums those of 32 pages one after the other
-                const uint32_t k = i0 + lane < pages ? key[i0 + lane] : 0u;
-                uint32_t mine = k > upto ? kKeyAlways : 0u;
-                for (uint32_t m = __ballot_sync(0xffffffffu, k >= from && k <= upto); m != 0u; m &= m - 1u) {
-                    const int at = __ffs(m) - 1;
-                    const uint32_t x = exact_key(a, unit, row[i0 + at]);
-                    if (lane == at) mine = x;
-                }
-                if (i0 + lane < pages) key[i0 + lane] = mine;
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += o;
+        }
+        if (lane == 31) s.warp_a[warp] = incl;
+        __syncthreads();
+        int before = above + incl - sum + __reduce_add_sync(0xffffffffu, lane < warp ? s.warp_a[lane] : 0);
+        if (before < count && count <= before + sum) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (before < count && count <= before + c[i]) { s.step = kBins - 1 - tid * kPer - i; s.step_before = before; s.step_count = c[i]; }
+                before += c[i];
+            }
+        }
+        __syncthreads();
+        // the step's own least and greatest key: the next interval
+        const int step = s.step;
+        uint32_t least = 0xffffffffu, most = 0u;
+        for (int i = tid; i < pages; i += kPickThreads) {
+            const uint32_t k = key[i];
+            if (k >= from && k <= upto && step_of(k) == step) { least = min(least, k); most = max(most, k); }
+        }
+        uint32_t unused = 0u;
+        block_range(s, least, most, unused);
+        const bool narrower = least > from || most < upto;
+        above = s.step_before; between = s.step_count;
+        from = least; upto = most;
+        low = key_score(from); high = key_score(upto);
+        if (!narrower || high - low <= worst) break;
+    }
+    // ---- what the errors leave open is summed again
+    if (!alike && worst > 0.f) {
+        from = max(1u, score_key(low - 3.f * worst));
+        upto = min(kKeyNan - 1u, score_key(high + 3.f * worst));
+        count_keys();
+    }
+    int left = count - above;
+    if (!alike && between > left) {
+        if (tid == 0) s.listed = 0;
+        __syncthreads();
+        for (int i = tid; i < pages; i += kPickThreads) {
+            const uint32_t k = key[i];
+            if (k >= from && k <= upto) {
+                const int at = atomicAdd(&s.listed, 1);
+                if (at < kPickThreads) s.list[at] = i;
+            }
+        }
+        __syncthreads();
+        const int listed = s.listed;
+        if (listed <= kPickThreads) {                        // each of the few is ranked against the others: of equal ones the lower page comes first
+            for (int j = warp; j < listed; j += kPickWarps) {
+                const uint32_t k = exact_key(a, unit, row[s.list[j]]);
+                if (lane == 0) s.list_key[j] = k;
             }
             __syncthreads();
-            from = upto = last_place(s, key, pages, count, left);
+            if (tid < listed) {
+                const uint32_t k = s.list_key[tid];
+                const int i = s.list[tid];
+                int rank = 0;
+                for (int j = 0; j < listed; ++j) rank += s.list_key[j] > k || (s.list_key[j] == k && s.list[j] < i);
+                key[i] = rank < left ? kKeyAlways : 0u;
+            }
+            __syncthreads();
+            // (all of the list that is taken is above `upto` now)
+            from = 1u; upto = max(from, upto);
+            left = 0;
+        } else {                                             // many scores as good as equal: their 64-bit sums, digit by digit
+            for (int i = warp; i < pages; i += kPickWarps) {
+                const uint32_t k = key[i];
+                uint32_t x = k > upto ? kKeyAlways : 0u;
+                if (k >= from && k <= upto) x = exact_key(a, unit, row[i]);
+                if (lane == 0) key[i] = x;
+            }
+            __syncthreads();
+            uint32_t last = 0u;                              // the greatest key that at least `count` are not below
+            for (int bit = 31; bit >= 0; --bit) {
+                from = last | 1u << bit; upto = 0xffffffffu;
+                count_keys();
+                if (between >= count) last = from;
+            }
+            from = upto = last;
+            count_keys();
+            left = count - above;
         }
     }
     // ---- emission: keys above `upto`, and the first `left` from `from` on
-    const int per = ((pages + 31) / 32 + kPickWarps - 1) / kPickWarps * 32;          // a run of whole words of 32 pages per warp
-    const int p0 = min(pages, warp * per), p1 = min(pages, p0 + per);
-    int above = 0, ties = 0;
+    int taken = 0, ties = 0;
     for (int i = p0; i < p1; i += 32) {
         const bool in = i + lane < p1;
         const uint32_t k = in ? key[i + lane] : 0u;
-        above += __popc(__ballot_sync(0xffffffffu, in && k > upto));
+        taken += __popc(__ballot_sync(0xffffffffu, in && k > upto));
         ties += __popc(__ballot_sync(0xffffffffu, in && k >= from && k <= upto));
     }
     __syncthreads();                                         // (the sums of the warps are read until here)
-    if (lane == 0) { s.warp_a[warp] = above; s.warp_b[warp] = ties; }
+    if (lane == 0) { s.warp_a[warp] = taken; s.warp_b[warp] = ties; }
     __syncthreads();
-    int at = 0, tie = 0;
-    for (int w = 0; w < warp; ++w) { at += s.warp_a[w]; tie += s.warp_b[w]; }
+    int at = __reduce_add_sync(0xffffffffu, lane < warp ? s.warp_a[lane] : 0), tie = __reduce_add_sync(0xffffffffu, lane < warp ? s.warp_b[lane] : 0);
     at += min(tie, left);
     const uint32_t lower = (1u << lane) - 1u;
-    for (int i = p0; i < p1; i += 32) {
+    auto emit = [&](int i, int id) {                         // 32 pages from the i-th on
         const bool in = i + lane < p1;
         const uint32_t k = in ? key[i + lane] : 0u;
         const bool same = in && k >= from && k <= upto;
@@ -329,21 +454,27 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
         const bool take = in && (k > upto || (same && tie + __popc(ms & lower) < left));
         const uint32_t mt = __ballot_sync(0xffffffffu, take);
         if (take) {
-            const int id = row[i + lane];
             out[at + __popc(mt & lower)] = id;
             if ((unsigned)id >= (unsigned)a.c.n_pages && a.status != nullptr) atomicOr(a.status + unit, COMPACTOR_STATUS_PAGE);
         }
         at += __popc(mt);
         tie += __popc(ms);
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+        if (p0 + 32 * j < p1) emit(p0 + 32 * j, id_ahead[j]);
+    for (int i = p0 + 32 * kAhead; i < p1; i += 32) emit(i, i + lane < p1 ? row[i + lane] : -1);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_select(const SelectArgs& a, cudaStream_t stream) {
-    const int chunks = (a.unit_pages + kScorePages - 1) / kScorePages;
+cudaError_t launch_paged_select(const SelectArgs& a, int sm_count, cudaStream_t stream) {
     cudaError_t e;
-    if ((e = launch_chained(kPdlOther, score_pages_kernel, dim3((unsigned)(a.units * chunks)), dim3(kScoreWarps * 32), 0, stream, a, chunks)) != cudaSuccess) return e;
+    if (a.unit_pages > a.pages) {                            // (else all pages of every unit are taken)
+        const long long runs = (long long)a.units * ((a.unit_pages + 15) / 16);
+        const int blocks = (int)min((runs + kScoreWarps - 1) / kScoreWarps, 4LL * sm_count);
+        if ((e = launch_chained(kPdlOther, score_pages_kernel, dim3(blocks), dim3(kScoreWarps * 32), 0, stream, a)) != cudaSuccess) return e;
+    }
     static std::atomic<unsigned long long> done;
     if ((e = allow_smem(pick_pages_kernel, kSelectMaxPages * (int)sizeof(uint32_t), done)) != cudaSuccess) return e;
     return launch_chained(kPdlOther, pick_pages_kernel, dim3((unsigned)a.units), dim3(kPickThreads), sizeof(uint32_t) * (size_t)a.unit_pages, stream, a);
