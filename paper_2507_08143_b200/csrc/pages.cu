@@ -11,9 +11,9 @@
 //   1. scores by matrix instructions, 16 pages a warp: the sum is [least | greatest] times [min(q, 0) | max(q, 0)], products exact, sums in fp32; and a
 //      bound of each score's error, from the same sum over absolute values.  The warps of a grid that fills the GPU share the pages of all units.
 //   2. a block per unit finds an interval of scores that holds the last place, by a histogram of 2048 even steps between the least and the greatest
-//      score, and another within a step while it holds many pages.  With E the greatest of the error bounds, a page more than 3 E above
-//      the interval is taken and one more than 3 E below is not, whatever the errors (and the one rounding to fp32 that the definition
-//      has: 2^-24 of a score is far below E).  The few pages in between are summed again, in 64 bits and rounded once, and compared by that.
+//      score, and another within a step while it holds many pages.  With E the greatest of the error bounds, a page more than 2 E and
+//      a little above the interval is taken and one as far below is not, whatever the errors (the little is for the one rounding to fp32 that
+//      the definition has: 2^-24 of a score, where E / 16 is 2^-20 of its absolute values).  The few pages in between are summed again, in 64 bits and rounded once, and compared by that.
 // Bound by the chain of launches and dependent reads (length, page ids, bounds, scores); the bytes are 512 per page.
 #include "paged.cuh"
 #include "quant4.cuh"
@@ -47,6 +47,23 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 // Error of a score: sums of 16 instructions in four chains of four, each of which may drop a unit of 2^-23 of its partial sum for each of 17
 // summands, three additions: 71 2^-23 of the sum of absolute values (which is itself no more than that far off).
 constexpr float kScoreError = 0x1p-16f;
+
+// The new key enters the bounds of its page, by a warp.  (That page is taken without a score.)
+__device__ __forceinline__ void enter_new_key(const SelectArgs& a, int unit, int lane) {
+    const long long t = select_tokens(a, unit);
+    if (a.k_new == nullptr || t <= 0) return;
+    const int page = page_of<false>(a.c, unit, (int)(t - 1)), piece = lane & 15, h = unit / a.c.batch, b = unit - h * a.c.batch;
+    if (page < 0) return;
+    const uint4 x = *(reinterpret_cast<const uint4*>(a.k_new + b * a.kn_seq + h * a.kn_head) + piece);
+    uint4* at = reinterpret_cast<uint4*>(a.bounds + (long long)page * 2 * kD + (lane >> 4) * kD) + piece;
+    uint4 y = x;
+    if (((t - 1) & ((1 << a.c.page_shift) - 1)) != 0) {
+        const uint4 old = *at;
+        y = lane < 16 ? make_uint4(min_nan2(old.x, x.x), min_nan2(old.y, x.y), min_nan2(old.z, x.z), min_nan2(old.w, x.w))
+                      : make_uint4(max_nan2(old.x, x.x), max_nan2(old.y, x.y), max_nan2(old.z, x.z), max_nan2(old.w, x.w));
+    }
+    *at = y;
+}
 
 // Runs of 16 pages of a unit whose scores are asked for.
 __device__ __forceinline__ int runs_of(const SelectArgs& a, int unit) {
@@ -151,7 +168,15 @@ score_pages_kernel(const __grid_constant__ SelectArgs a) {
     __syncthreads();
     const int all = cum[kThreads];
     for (int run = warp * gridDim.x + blockIdx.x; run < all; run += kScoreWarps * gridDim.x) score_run(a, cum, per, run, lane);
+    for (int unit = warp * gridDim.x + blockIdx.x; unit < a.units; unit += kScoreWarps * gridDim.x) enter_new_key(a, unit, lane);
 }
+// A load that stays where it stands.
+__device__ __forceinline__ int load_here(const int* p) {
+    int x;
+    asm volatile("ld.global.s32 %0, [%1];" : "=r"(x) : "l"(p));
+    return x;
+}
+
 constexpr int kPickThreads = 512;
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kBins = 2048;
@@ -167,16 +192,15 @@ struct PickShared {
     uint32_t list_key[kPickThreads];
 };
 
-// The score of a page as it is defined, summed in 64 bits and rounded once; by a warp, four channels a lane.
-__device__ __forceinline__ uint32_t exact_key(const SelectArgs& a, int unit, int page) {
+// The score of a page for the unit's query heads from `first` up to `end` as it is defined, summed in 64 bits and rounded once; by a warp, four channels
+// a lane.
+__device__ __forceinline__ uint32_t exact_key(const SelectArgs& a, int unit, int page, int first, int end) {
     const int lane = threadIdx.x & 31, h = unit / a.c.batch, b = unit - h * a.c.batch;
     const uint2 l = *(reinterpret_cast<const uint2*>(a.bounds + (long long)page * 2 * kD) + lane);
     const uint2 m = *(reinterpret_cast<const uint2*>(a.bounds + (long long)page * 2 * kD + kD) + lane);
     const float low[4] = {bf16_lo(l.x), bf16_hi(l.x), bf16_lo(l.y), bf16_hi(l.y)}, high[4] = {bf16_lo(m.x), bf16_hi(m.x), bf16_lo(m.y), bf16_hi(m.y)};
-    double best = -INFINITY;
-    bool nan = false;
-#pragma unroll 4
-    for (int j = 0; j < a.g; ++j) {
+    uint32_t best = 0u;
+    for (int j = first; j < end; ++j) {
         const uint2 v = *(reinterpret_cast<const uint2*>(a.q + b * a.q_seq + (long long)(h * a.g + j) * a.q_head) + lane);
         const float q[4] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y)};
         double x = 0.;
@@ -184,10 +208,9 @@ __device__ __forceinline__ uint32_t exact_key(const SelectArgs& a, int unit, int
         for (int c = 0; c < 4; ++c) x = fma((double)q[c], (double)(q[c] > 0.f ? high[c] : low[c]), x);
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-        nan |= x != x;
-        best = fmax(best, x);
+        best = max(best, score_key((float)x));               // (not a number above all)
     }
-    return nan ? kKeyNan : score_key((float)best);
+    return best;
 }
 
 // Sums of two counts over the block, in every thread.
@@ -248,20 +271,7 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
         a.lengths_out[unit] = n;
         if (t == -2 && a.status != nullptr) atomicOr(a.status + unit, COMPACTOR_STATUS_CAPACITY);
     }
-    if (warp == kPickWarps - 1 && a.k_new != nullptr && t > 0) {             // the new key enters the bounds of its page (which is taken without a score)
-        const int page = page_of<false>(a.c, unit, (int)(t - 1)), piece = lane & 15, h = unit / a.c.batch, b = unit - h * a.c.batch;
-        if (page >= 0) {
-            const uint4 x = *(reinterpret_cast<const uint4*>(a.k_new + b * a.kn_seq + h * a.kn_head) + piece);
-            uint4* at = reinterpret_cast<uint4*>(a.bounds + (long long)page * 2 * kD + (lane >> 4) * kD) + piece;
-            uint4 y = x;
-            if (((t - 1) & (page_tokens - 1)) != 0) {
-                const uint4 old = *at;
-                y = lane < 16 ? make_uint4(min_nan2(old.x, x.x), min_nan2(old.y, x.y), min_nan2(old.z, x.z), min_nan2(old.w, x.w))
-                              : make_uint4(max_nan2(old.x, x.x), max_nan2(old.y, x.y), max_nan2(old.z, x.z), max_nan2(old.w, x.w));
-            }
-            *at = y;
-        }
-    }
+    if (!scored && warp == kPickWarps - 1) enter_new_key(a, unit, lane);     // (else the first kernel has done it)
     for (int i = count + tid; i < a.pages; i += kPickThreads) out[i] = -1;
     if (pages <= a.pages) {
         for (int i = tid; i < pages; i += kPickThreads) {
@@ -276,7 +286,7 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
     const int p0 = min(pages, warp * per_warp), p1 = min(pages, p0 + per_warp);
     int id_ahead[kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) id_ahead[j] = p0 + 32 * j + lane < p1 ? row[p0 + 32 * j + lane] : -1;
+    for (int j = 0; j < kAhead; ++j) id_ahead[j] = load_here(row + min(p0 + 32 * j + lane, max(p1, 1) - 1));
     uint32_t worst_bits = 0u, low_key = 0xffffffffu, high_key = 0u;          // greatest error; least and greatest of the finite scores
     int above = 0, between = 0;                              // keys above the finite scores, finite scores
     bool vague = false;                                      // scores that say nothing: bounds or queries that are not finite, or sums near the end of the range
@@ -297,7 +307,7 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
     if (__syncthreads_or(vague)) {
         for (int i = warp; i < pages; i += kPickWarps) {
             if (errors[i] < INFINITY) continue;
-            const uint32_t k = exact_key(a, unit, row[i]);   // (its page is one: those that are none have no error)
+            const uint32_t k = exact_key(a, unit, row[i], 0, a.g);   // (its page is one: those that are none have no error)
             if (lane == 0) { key[i] = k; scan(k); }
         }
     }
@@ -379,8 +389,8 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
     }
     // ---- what the errors leave open is summed again
     if (!alike && worst > 0.f) {
-        from = max(1u, score_key(low - 3.f * worst));
-        upto = min(kKeyNan - 1u, score_key(high + 3.f * worst));
+        from = max(1u, score_key(low - 2.0625f * worst));
+        upto = min(kKeyNan - 1u, score_key(high + 2.0625f * worst));
         count_keys();
     }
     int left = count - above;
@@ -391,15 +401,16 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
             const uint32_t k = key[i];
             if (k >= from && k <= upto) {
                 const int at = atomicAdd(&s.listed, 1);
-                if (at < kPickThreads) s.list[at] = i;
+                if (at < kPickThreads) { s.list[at] = i; s.list_key[at] = 0u; }
             }
         }
         __syncthreads();
         const int listed = s.listed;
         if (listed <= kPickThreads) {                        // each of the few is ranked against the others: of equal ones the lower page comes first
-            for (int j = warp; j < listed; j += kPickWarps) {
-                const uint32_t k = exact_key(a, unit, row[s.list[j]]);
-                if (lane == 0) s.list_key[j] = k;
+            for (int j = warp; j < listed * a.g; j += kPickWarps) {          // (a query head of one of them at a time: the chain of a sum is long)
+                const int which = j / a.g, head = j - which * a.g;
+                const uint32_t k = exact_key(a, unit, row[s.list[which]], head, head + 1);
+                if (lane == 0) atomicMax(&s.list_key[which], k);
             }
             __syncthreads();
             if (tid < listed) {
@@ -417,7 +428,7 @@ pick_pages_kernel(const __grid_constant__ SelectArgs a) {
             for (int i = warp; i < pages; i += kPickWarps) {
                 const uint32_t k = key[i];
                 uint32_t x = k > upto ? kKeyAlways : 0u;
-                if (k >= from && k <= upto) x = exact_key(a, unit, row[i]);
+                if (k >= from && k <= upto) x = exact_key(a, unit, row[i], 0, a.g);
                 if (lane == 0) key[i] = x;
             }
             __syncthreads();
