@@ -46,24 +46,33 @@ __device__ __forceinline__ uint32_t quantise8(const uint4& x, uint32_t& param) {
     least = min_nan2(least, least >> 16 | least << 16);      // both halves the same
     most = max_nan2(most, most >> 16 | most << 16);
     const float lo = bf16_hi(least) + 0.f;                   // (-0 is 0)
-    float s = (bf16_hi(most) - lo) / 15.f;
-    const bool good = s <= 0x1p120f;                         // (false for not a number, which the rounding may make a number of)
-    s = __uint_as_float((__float_as_uint(s) + 0xfffffu) & ~0xfffffu);
+    // The least number s of four significant bits with 15 s >= the range: rounded up from a quotient that is a little small, and one up if that was
+    // too little (15 s is exact).
+    const float range = bf16_hi(most) - lo;
+    float s = __uint_as_float((__float_as_uint(range * ((1.f - 0x1p-22f) / 15.f)) + 0xfffffu) & ~0xfffffu);
+    if (15.f * s < range) s = __uint_as_float(__float_as_uint(s) + 0x100000u);
+    const bool good = range <= 15.f * 0x1p120f;              // (false for not a number)
     if (s < 0x1p-120f) s = 0.f;
     param = good ? __float_as_uint(s) >> 16 | __float_as_uint(lo) : 0x7fff7fffu;
     // The quotient by a reciprocal that is a little small gives the right code or, next to a border, the one below it: the remainder, which
     // is exact, tells.  (A division for each channel is twice the instructions, and this is what the fill spends most of them on.)
-    const float inv = s > 0.f ? (1.f / s) * (1.f - 0x1p-22f) : 0.f, half = 0.5f * s;
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    inv *= 1.f - 0x1p-21f;
+    const float half = 0.5f * s;
     const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+    constexpr float kWhole = 12582912.f;                     // 1.5 2^23: added to it, a number is rounded to a whole one in its low bits
     uint32_t codes = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 7; j >= 0; --j) {
         const float d = ((j & 1) != 0 ? bf16_hi(in[j >> 1]) : bf16_lo(in[j >> 1])) - lo;
-        const float t = __fmaf_rn(d, inv, 12582912.f);       // 1.5 2^23: the nearest whole number is in the low bits
-        const float rest = __fmaf_rn(-s, t - 12582912.f, d);
-        codes |= ((__float_as_uint(t) & 15u) + (rest > half ? 1u : 0u)) << (4 * j);
+        const float t = __fmaf_rn(d, inv, kWhole);
+        const float rest = __fmaf_rn(-s, t - kWhole, d);
+        uint32_t bits = __float_as_uint(t);
+        if (rest > half) ++bits;
+        codes = codes * 16u + bits;
     }
-    return good && s > 0.f ? codes : 0u;
+    return good && s > 0.f ? codes - 0x4b400000u * 0x11111111u : 0u;         // (without the eight bit patterns of 1.5 2^23)
 }
 
 // The eight values of a word of codes, rounded to bf16.
