@@ -332,7 +332,8 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
 #pragma unroll
             for (int s = 0; s < 8; ++s) o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.f;
             ol[t][0] = ol[t][1] = ol[t][2] = ol[t][3] = 0.f;
-            to_base2[t][0] *= scale2; to_base2[t][1] *= scale2;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) to_base2[t][c] = fminf(fmaxf(to_base2[t][c] * scale2, 0x1p-126f), 0x1p127f);     // (never 0 or infinite: -inf stays -inf, 0 stays 0)
             ref[t][0] = ref[t][1] = 0.f;
             most[t][0] = most[t][1] = -INFINITY;
             sum[t][0] = sum[t][1] = 0.f;
@@ -491,8 +492,9 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                 for (int t = 0; t < NG; ++t)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float x = ex2f(CAP ? s[u][t][2 * i] - ref[t][0] : fmaf(s[u][t][2 * i], to_base2[t][0], -ref[t][0]));
-                        const float y = ex2f(CAP ? s[u][t][2 * i + 1] - ref[t][1] : fmaf(s[u][t][2 * i + 1], to_base2[t][1], -ref[t][1]));
+                        // (the product is rounded as the reference's was: scores of 2^31 and more, whose last place is a whole power, are told apart by that)
+                        const float x = ex2f(CAP ? s[u][t][2 * i] - ref[t][0] : __fadd_rn(__fmul_rn(s[u][t][2 * i], to_base2[t][0]), -ref[t][0]));
+                        const float y = ex2f(CAP ? s[u][t][2 * i + 1] - ref[t][1] : __fadd_rn(__fmul_rn(s[u][t][2 * i + 1], to_base2[t][1]), -ref[t][1]));
                         sum[t][0] += x; sum[t][1] += y;
                         const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y);
                         pf[u][t][i] = transpose8x8(__byte_perm(xb, yb, 0x7632));

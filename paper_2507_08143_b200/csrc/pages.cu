@@ -81,7 +81,10 @@ __device__ __forceinline__ void score_run(const SelectArgs& a, const int* cum, i
         if (cum[mid] <= run) lo = mid; else hi = mid;
     }
     int unit = lo * per, nth = run - cum[lo];
-    for (int n = runs_of(a, unit); nth >= n; n = runs_of(a, ++unit)) nth -= n;
+    for (int n = runs_of(a, unit); nth >= n; n = runs_of(a, unit)) {
+        nth -= n;
+        if (++unit >= a.units) return;                       // (only if lengths change under the call, which its caller rules out)
+    }
     const int pages = (int)((select_tokens(a, unit) + (1 << a.c.page_shift) - 1) >> a.c.page_shift), first = 16 * nth;
     const int h = unit / a.c.batch, b = unit - h * a.c.batch;
     // rows gid and gid + 8 of the warp's pages; the lane has the 16-byte pieces tig + 4 i of their least and greatest values

@@ -243,10 +243,12 @@ bounds_kernel(const __grid_constant__ BoundsArgs a) {
     }
     int unit = a.first_unit + lo * per, left = begin - cum[lo];
     PageRange r = pages_of(a, unit);
-    while (left >= r.end - r.first) {
+    const int last_unit = a.first_unit + a.units - 1;        // (searches end there even if lengths change under the call, which its caller rules out)
+    while (left >= r.end - r.first && unit < last_unit) {
         left -= r.end - r.first;
         r = pages_of(a, ++unit);
     }
+    if (left >= r.end - r.first) return;
     int index = r.first + left, ids_from = index;            // lane l has the ids of pages ids_from + l
     auto ids_at = [&](int i) { return i + lane < r.end ? page_of<false>(a.c, unit, (i + lane) << a.c.page_shift) : -1; };
     int ids = ids_at(index);
@@ -257,7 +259,10 @@ bounds_kernel(const __grid_constant__ BoundsArgs a) {
         while (to_come > 0) {
             --to_come;
             if (index == r.end) {                            // the next unit that has pages
-                do r = pages_of(a, ++unit); while (r.end == r.first);
+                do {
+                    if (unit >= last_unit) return Place{-1, 0, 0};
+                    r = pages_of(a, ++unit);
+                } while (r.end == r.first);
                 index = ids_from = r.first;
                 ids = ids_at(index);
             } else if (index == ids_from + 32) {
