@@ -7,7 +7,7 @@
 // a value of the row, is one as well.  The rounding up costs on average 3 % of the step.  A step below 2^-120 is 0 (all codes 0); a group
 // that holds a value which is not finite, or whose step exceeds 2^120, is held as not a number throughout.
 #pragma once
-#include "common.cuh"
+#include "two.cuh"
 
 namespace compactor {
 
@@ -64,13 +64,17 @@ __device__ __forceinline__ uint32_t quantise8(const uint4& x, uint32_t& param) {
     constexpr float kWhole = 12582912.f;                     // 1.5 2^23: added to it, a number is rounded to a whole one in its low bits
     uint32_t codes = 0;
 #pragma unroll
-    for (int j = 7; j >= 0; --j) {
-        const float d = ((j & 1) != 0 ? bf16_hi(in[j >> 1]) : bf16_lo(in[j >> 1])) - lo;
-        const float t = __fmaf_rn(d, inv, kWhole);
-        const float rest = __fmaf_rn(-s, t - kWhole, d);
-        uint32_t bits = __float_as_uint(t);
-        if (rest > half) ++bits;
-        codes = codes * 16u + bits;
+    for (int j = 3; j >= 0; --j) {                           // two channels at a time
+        const Two d = add_two(two(bf16_lo(in[j]), bf16_hi(in[j])), two(-lo, -lo));
+        const Two t = fma_two(d, two(inv, inv), two(kWhole, kWhole));
+        const Two rest = fma_two(two(-s, -s), add_two(t, two(-kWhole, -kWhole)), d);
+        float t0, t1, r0, r1;
+        split_two(t, t0, t1);
+        split_two(rest, r0, r1);
+        uint32_t even = __float_as_uint(t0), odd = __float_as_uint(t1);
+        if (r0 > half) ++even;
+        if (r1 > half) ++odd;
+        codes = (codes * 16u + odd) * 16u + even;
     }
     return good && s > 0.f ? codes - 0x4b400000u * 0x11111111u : 0u;         // (without the eight bit patterns of 1.5 2^23)
 }

@@ -12,6 +12,7 @@
 // behind it (at position 131072 the angle would be off by 0.004), taken to a fraction of a turn and then to 32 bits; each lane works out two and
 // the warp shares them.
 #include "rope.cuh"
+#include "two.cuh"
 
 namespace compactor {
 namespace {
@@ -20,24 +21,6 @@ constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kRows = 4;                       // pairs of rows of a warp in flight
 
-// Two fp32 in one register pair, for the instructions that work on both.
-using Two = unsigned long long;
-__device__ __forceinline__ Two two(float x, float y) {
-    Two r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ void split(Two v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-    Two r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ Two mul2(Two a, Two b) {
-    Two r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 // Eight channels as they are read.
 __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -58,7 +41,7 @@ __device__ __forceinline__ uint4 pack(const Two (&x)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float lo, hi;
-        split(x[i], lo, hi);
+        split_two(x[i], lo, hi);
         const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
         w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
@@ -93,11 +76,11 @@ __device__ __forceinline__ void rotate_rows(const Rows& r, const Two (&a)[4], co
             unpack(in[u], x);
             float inv = 1.f;
             if (r.norm) {
-                Two squares = mul2(x[0], x[0]);
+                Two squares = mul_two(x[0], x[0]);
 #pragma unroll
-                for (int i = 1; i < 4; ++i) squares = fma2(x[i], x[i], squares);
+                for (int i = 1; i < 4; ++i) squares = fma_two(x[i], x[i], squares);
                 float sum, odd;
-                split(squares, sum, odd);
+                split_two(squares, sum, odd);
                 sum += odd;
 #pragma unroll
                 for (int d = 1; d < 16; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -108,7 +91,7 @@ __device__ __forceinline__ void rotate_rows(const Rows& r, const Two (&a)[4], co
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float lo, hi;
-                    split(x[i], lo, hi);
+                    split_two(x[i], lo, hi);
                     y[i] = two(hi, lo);
                 }
             } else {
@@ -117,14 +100,14 @@ __device__ __forceinline__ void rotate_rows(const Rows& r, const Two (&a)[4], co
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const Two xa = mul2(x[i], a[i]);
-                z[i] = mul2(FULL || turned ? fma2(y[i], b[i], xa) : xa, inv2);
+                const Two xa = mul_two(x[i], a[i]);
+                z[i] = mul_two(FULL || turned ? fma_two(y[i], b[i], xa) : xa, inv2);
             }
             if (head < r.heads) {
                 *(reinterpret_cast<uint4*>(r.out + head * r.out_head) + l) = pack(z);
                 if (r.plain != nullptr) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] = mul2(mul2(x[i], w[i]), inv2);
+                    for (int i = 0; i < 4; ++i) z[i] = mul_two(mul_two(x[i], w[i]), inv2);
                     *(reinterpret_cast<uint4*>(r.plain + head * r.plain_head) + l) = pack(z);
                 }
             }
