@@ -15,6 +15,8 @@ namespace {
 // moves 128 rows: first a thread per row finds source and target (index, length and page id are three dependent reads,
 // made once per row and not once per 16-byte piece) and moves weight and position, then 16 threads per row move K and V.
 // Bound by HBM: 512 bytes read and written per row.  256 units x 2458 of 8192 rows: 109 us = 6.0 TB/s, 0.92 of the copy rate.
+// FOUR: the row is held in 4 bits on the way, each thread eight channels of it.  160 bytes written instead of 512, but 120 instructions per row
+// and lane more: the same rows take 101 us = 4.4 TB/s, bound by their issue (five blocks to an SM; with what four leave room for, 105).
 constexpr int kFillThreads = 256;
 constexpr int kFillRows = 128;
 constexpr int kFillRowsPerIter = kFillThreads / 16;
@@ -58,7 +60,7 @@ __global__ void fill_lengths_kernel(const __grid_constant__ FillArgs a, const __
 }
 
 template <bool ACROSS, bool FOUR>
-__global__ void __launch_bounds__(kFillThreads)
+__global__ void __launch_bounds__(kFillThreads, FOUR ? 5 : 1)
 fill_kernel(const __grid_constant__ FillArgs a, const __grid_constant__ FillTables t, int row_blocks) {
     __shared__ long long src_k[kFillRows], src_v[kFillRows], dst[kFillRows];       // elements; dst < 0: the row is skipped
     const int tid = threadIdx.x;
