@@ -6,9 +6,10 @@
 //   - keys: a code alone in the lower bits of an fp16 is the number c 2^-24 (below the normal ones), one field up 16 c 2^-24, so that a mask makes
 //     two operands and one shift per eight codes brings the others down.  Queries are scaled by a power of two per head to where fp16 holds all their bits; which
 //     channel is which of the 16 of an instruction is free as long as queries and keys agree.  A group's sum is multiplied by its step afterwards, in fp32.
-//   - values: their step differs from token to token, over which the instruction sums, so it has to be in the operand: 128 + c in bf16 is a byte
-//     under the exponent of 128, and one fused multiply-add with (s, -128 s) makes s c of it (s has four significant bits, so that this is
-//     exact).  The pairs are tokens: a byte permutation per two words brings the same channels of two tokens side by side.
+//   - values: their step differs from token to token, over which the instruction sums, so it has to be in the operand.  A code in the lower bits of a
+//     bf16 is c 2^-133, one field up 16 c 2^-133 (which runs on into the first normal numbers); two products, with 2^126 and with 2^7 s or 2^3 s,
+//     make s c of it (s has four significant bits, so that this is exact).  The pairs are tokens: a permutation per two words brings the
+//     same channels of two tokens side by side.
 //   - lo enters once for a group, not for every channel.  q.k = sum_c q_c s c + sum_groups lo_g (sum of the group's q): one more
 //     matrix instruction per tile with the least values as rows and the sums of the query, in three bf16 terms (24 bits), as columns.
 //     sum_j p_j v_j likewise gets one more instruction with the least values as rows, whose sums are added to the channels at the end.
@@ -17,9 +18,9 @@
 // The rows of a page lie back to back, so that a tile of 16 is 1280 bytes in one piece (two on pages of 8): five 16-byte copies per lane for
 // K and V together.  Twelve warps of 168 registers take two tiles a step, which the compiler interleaves.
 //
-// Measured (both kernels, one layer, device time of calls in a row): 8 heads x 131072 tokens 48.4 - 49.3 us for 1 to 8 query heads (bf16: 89), 77 for 12 and
-// 16, 138 for 32, 259 for 64; with weights 57 - 69.  16 ragged sequences x 8 heads, 470 K tokens, with weights, 41.  The copies alone take 34, the arithmetic
-// alone 48.  455 instructions per tile of 16 tokens (712 at first), 59 % of the issue slots, the logic pipe 46 %, the tensor pipe 20 %: a matrix instruction also holds
+// Measured (both kernels, one layer, device time of calls in a row): 8 heads x 131072 tokens 46.7 - 47.6 us for 1 to 8 query heads (bf16: 89), 75 for 12 and
+// 16, 132 for 32, 249 for 64; with weights 56 - 69.  16 ragged sequences x 8 heads, 470 K tokens, with weights, 41.  The copies alone take 34, the arithmetic
+// alone 47.  423 instructions per tile of 16 tokens (712 at first), 62 % of the issue slots, the logic pipe 41 %, the tensor pipe 20 %: a matrix instruction also holds
 // up the others for three of its nine cycles.  Not better: 16 warps of 128 registers (57 us), 8 of 255 (59); scores of a tile beside the product
 // of the one before (57); codes as e4m3 for the instruction of 8-bit types, which is made of fp16 ones here (68); both terms of the weights in the
 // eight columns of one instruction for up to four heads (2 us less for long contexts, nothing else).
@@ -114,11 +115,7 @@ __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t
     }
 }
 
-// Even bytes 0, 1 (or 2, 3) of four codes as 128 + c in bf16, whose last place is 1 there.
-__device__ __forceinline__ uint32_t codes_low(uint32_t x) { return __byte_perm(x, 0x43434343u, 0x4140); }
-__device__ __forceinline__ uint32_t codes_high(uint32_t x) { return __byte_perm(x, 0x43434343u, 0x4342); }
-constexpr uint32_t kNibbles = 0x0f0f0f0fu;
-constexpr uint32_t kFirst = 0x000f000fu, kSecond = 0x00f000f0u;      // codes of two channels as fp16: c 2^-24, and c 2^-20
+constexpr uint32_t kFirst = 0x000f000fu, kSecond = 0x00f000f0u;      // codes of two channels as they are: in fp16 c 2^-24 and c 2^-20, in bf16 c 2^-133 and c 2^-129
 
 // The instruction of decode.cuh, free to be placed where its operands are ready.
 __device__ __forceinline__ void mma4(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -523,27 +520,24 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                     par[i] = *reinterpret_cast<const uint32_t*>(row + kRow4Codes + 4 * (gid >> 1));
                 }
                 const uint32_t s0 = __byte_perm(par[0], par[1], 0x5410), s1 = __byte_perm(par[2], par[3], 0x5410);
-                const uint32_t m0 = fma2(s0, 0xc300c300u, 0x80008000u), m1 = fma2(s1, 0xc300c300u, 0x80008000u);
+                const uint32_t s0f = fma2(s0, 0x43004300u, 0u), s1f = fma2(s1, 0x43004300u, 0u), s0s = fma2(s0, 0x41004100u, 0u), s1s = fma2(s1, 0x41004100u, 0u);
 #pragma unroll
-                for (int j4 = 0; j4 < 8; j4 += 4) {          // the same bytes of two tokens side by side: channels j4, j4 + 2 in the lower halves of the bytes
-                    const unsigned sel = j4 == 0 ? 0x5140 : 0x7362;
+                for (int j4 = 0; j4 < 8; j4 += 4) {          // the same four channels of two tokens in the halves of a word
+                    const unsigned sel = j4 == 0 ? 0x5410 : 0x7632;
                     const uint32_t x[4] = {__byte_perm(v[0].x, v[1].x, sel), __byte_perm(v[0].y, v[1].y, sel), __byte_perm(v[2].x, v[3].x, sel), __byte_perm(v[2].y, v[3].y, sel)};
 #pragma unroll
-                    for (int odd = 0; odd < 2; ++odd) {
-                        uint32_t c[4];
+                    for (int n = 0; n < 4; ++n) {
+                        const int j = j4 + n;
+                        uint32_t vf[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) c[i] = (odd == 0 ? x[i] : x[i] >> 4) & kNibbles;
-#pragma unroll
-                        for (int two = 0; two < 2; ++two) {
-                            const int j = j4 + odd + 2 * two;
-                            uint32_t vf[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) vf[i] = fma2(two == 0 ? codes_low(c[i]) : codes_high(c[i]), i < 2 ? s0 : s1, i < 2 ? m0 : m1);
-#pragma unroll
-                            for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pf[u][t][0], pf[u][t][1]);
-#pragma unroll
-                            for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pl[u][t][0], pl[u][t][1]);
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t c = (n < 2 ? x[i] : x[i] >> 8) & ((n & 1) == 0 ? kFirst : kSecond);
+                            vf[i] = fma2(fma2(c, 0x7e807e80u, 0u), (n & 1) == 0 ? (i < 2 ? s0f : s1f) : (i < 2 ? s0s : s1s), 0u);
                         }
+#pragma unroll
+                        for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pf[u][t][0], pf[u][t][1]);
+#pragma unroll
+                        for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pl[u][t][0], pl[u][t][1]);
                     }
                 }
                 const uint32_t lf[4] = {__byte_perm(par[0], par[1], 0x7632), 0u, __byte_perm(par[2], par[3], 0x7632), 0u};

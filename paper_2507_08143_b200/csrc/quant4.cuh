@@ -31,9 +31,6 @@ __device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
 }
 __device__ __forceinline__ float bf16_lo(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
-// Codes i and i + 4 of a word of eight, as 128 + c in bf16 (its last place is 1 there).
-__device__ __forceinline__ uint32_t codes128(uint32_t w, int i) { return ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u; }
-
 // Eight channels of a row in each lane, a group in four neighbouring lanes: the word of codes, and in `param` the group's s (lower half) and lo.
 // All lanes of the warp call it.
 __device__ __forceinline__ uint32_t quantise8(const uint4& x, uint32_t& param) {

@@ -138,6 +138,24 @@ def test_select_bounds_that_are_no_numbers_and_pages_that_are_none():
         assert st[0, 0, 1] == 8 and (st[0, 0, 0] == 8) == (pages == 31)
 
 
+def test_select_queries_that_are_no_numbers_infinite_or_nothing():
+    from paper_2507_08143_b200 import binding as B
+    lens = np.array([[[500, 700, 300, 600, 16 * 40]]], np.int32)
+    host, cache, len_d = make_cache(lens, 16, 1, 40)
+    bounds = torch.randn(host["k"].shape[0], 2, 128, generator=torch.Generator().manual_seed(1)).sort(1).values
+    bounds[int(host["table"][0, 0, 4, 7])] *= 1e38                        # sums beyond fp32
+    bounds = bounds.bfloat16().cuda()
+    q = torch.randn(5, 3, 128, generator=torch.Generator().manual_seed(2)).bfloat16()
+    q[0, 1, 3] = float("nan"); q[1, 2, 5] = float("inf"); q[2] = 0; q[3, 0] = -q[3, 0].abs()
+    for pages in (3, 20):
+        table, short = torch.empty(1, 1, 5, pages, dtype=torch.int32, device="cuda"), torch.empty(1, 1, 5, dtype=torch.int32, device="cuda")
+        B.paged_select(cache, 0, 3, q.cuda(), len_d, bounds, table, short, B.alloc_paged_select_workspace(cache, 700), 700)
+        with np.errstate(invalid="ignore", over="ignore"):
+            want, want_len, _ = ro.select(host, 0, 3, H.bits(q), lens, H.bits(bounds), pages, 1, 1, None, 700)
+        np.testing.assert_array_equal(table[0].cpu().numpy(), want)
+        np.testing.assert_array_equal(short[0].cpu().numpy(), want_len)
+
+
 def test_select_units_that_do_not_fit():
     *_, st, _, _ = run_select([[[50, 39, 40, -1]]], 2, 16, 2, max_length=40, seed=6)
     assert st.tolist() == [[[16, 0, 16, 0]]]
