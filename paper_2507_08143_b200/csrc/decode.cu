@@ -712,7 +712,9 @@ cudaError_t launch_paged_attention(const DecodeArgs& a, int sm_count, cudaStream
     const int pairs = a.units * a.g;
     const long long most = a.accumulate ? (long long)a.units * ((a.capacity + kTile - 1) / kTile + kMassUnitCost) : 0;   // cost of the weights
     const long long wanted = (most + kTile - 1) / kTile;     // 256 tokens a block at the least
-    const bool large = 2 * pairs <= sm_count, few_pieces = a.workers < 6 * a.units * a.groups;
+    // (Over 4 bits with the weights of more than 2048 tokens for each SM, these are what counts, and the smaller blocks put four of them to an SM: 8 heads x
+    // 131072 tokens, g = 5, 65.9 -> 57.4 us, x 65536 38.8 -> 38.0; of half as many tokens 27.1 -> 29.0.  Over bf16 it stays as it is, results to the bit.)
+    const bool large = 2 * pairs <= sm_count && !(a.four && wanted > 8LL * sm_count), few_pieces = a.workers < 6 * a.units * a.groups;
     const int join_blocks = large ? 2 * pairs : few_pieces ? (pairs + 3) / 4 : pairs;
     // (not more than fit beside the others, so that those need not wait for a place)
     // and where there are more joining blocks than that, half of the places after a first kernel over 4 bits, whose weights are more of the whole

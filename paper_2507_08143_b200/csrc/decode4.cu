@@ -19,7 +19,7 @@
 // K and V together.  Twelve warps of 168 registers take two tiles a step, which the compiler interleaves.
 //
 // Measured (both kernels, one layer, device time of calls in a row): 8 heads x 131072 tokens 46.7 - 47.6 us for 1 to 8 query heads (bf16: 89), 75 for 12 and
-// 16, 132 for 32, 249 for 64; with weights 56 - 69.  16 ragged sequences x 8 heads, 470 K tokens, with weights, 41.  The copies alone take 34, the arithmetic
+// 16, 132 for 32, 249 for 64; with weights 56 - 57.  16 ragged sequences x 8 heads, 470 K tokens, with weights, 41.  The copies alone take 34, the arithmetic
 // alone 47.  423 instructions per tile of 16 tokens (712 at first), 62 % of the issue slots, the logic pipe 41 %, the tensor pipe 20 %: a matrix instruction also holds
 // up the others for three of its nine cycles.  Not better: 16 warps of 128 registers (57 us), 8 of 255 (59); scores of a tile beside the product
 // of the one before (57); codes as e4m3 for the instruction of 8-bit types, which is made of fp16 ones here (68); both terms of the weights in the

@@ -105,7 +105,7 @@ struct DecodeArgs {
 };
 constexpr int kDecodeTile = 16;            // tokens per tile
 constexpr int kDecodeWarps = 8;
-constexpr int kDecode4Warps = 12;          // of the kernel for rows in 4 bits, up to 8 query heads (registers: 128 each)
+constexpr int kDecode4Warps = 12;          // of the kernel for rows in 4 bits, up to 8 query heads (168 registers a thread)
 constexpr int kDecode4WarpsWide = 8;       // and beyond
 constexpr int kDecodeUnitCost = 3;         // tiles that entering a unit counts for when the work is shared out
 constexpr int kDecodeHeads = 16;           // query heads that one warp serves at once
