@@ -547,6 +547,7 @@ int compactor_paged4_read(const compactor_paged_cache* cache, int32_t first_laye
  * Attention to a few pages of every unit, chosen for each step's queries: compactor_paged_bounds keeps the least and the greatest key of every
  * page, channel by channel; compactor_paged_select scores the pages by them and writes the best as a page table of one layer, which the
  * attention calls take in the place of the cache's own (layers = 1, max_pages = pages, layer 0, the lengths written here).
+ * (A cache with positions then wants new_positions: without them the attention would write the token's place in the chosen pages.)
  *   bounds         device bf16 [n_pages][2][d], 16-byte aligned: least values, then greatest, of the keys of the page's tokens (of a cache in 4 bits:
  *                  of what they stand for, rounded to bf16).  Not-a-number in a channel gives not-a-number.
  *
@@ -566,13 +567,13 @@ int compactor_paged4_read(const compactor_paged_cache* cache, int32_t first_laye
  *   k_new          rows [batch][heads] of the token that the attention is going to append, or ptr NULL (nothing will be appended).  It enters the bounds
  *                  of its page (as given, in a cache of either kind), so that they need no other call while a sequence grows.
  *   lengths        device int32 [units of the cache], without the new token.
- *   table_out      device int32 [heads * batch][pages]: the pages taken, in the unit's order, and -1 behind them.
- *   lengths_out    device int32 [heads * batch], not `lengths`: the unit's length over that table, again without the new token; a
+ *   table_out      device int32 [heads * batch][pages]: the pages taken, in the unit's order, and -1 behind them; no part of the cache's table.
+ *   lengths_out    device int32 [heads * batch], no part of `lengths`: the unit's length over that table, again without the new token; a
  *                  negative length stays, a unit beyond max_length or its pages (COMPACTOR_STATUS_CAPACITY) gets -1.
  *   options (HOST): 1 <= q_per_kv <= 64; max_length, the most tokens a unit may have, the new one included; first_pages >= 0, last_pages
  *                  >= 1 (a unit's last page is filled only in part, and takes the new token), first_pages + last_pages <= pages.
  * Pages that are taken and are none are reported (COMPACTOR_STATUS_PAGE) and left to the attention.
- * At most 49152 pages per unit (COMPACTOR_E_TOO_LARGE).  Workspace: compactor_paged_select_workspace_bytes(), 256-byte aligned, contents
+ * At most 49152 pages per unit, and no more in `pages` than a table may have (COMPACTOR_E_TOO_LARGE).  Workspace: compactor_paged_select_workspace_bytes(), 256-byte aligned, contents
  * not preserved; 0 = bad arguments.  `bounds` is written (one page per unit): calls that share it are ordered by the caller.
  */
 typedef struct compactor_select_options {

@@ -1423,8 +1423,7 @@ extern "C" int compactor_paged_select(const compactor_paged_cache* cache, int32_
         return COMPACTOR_E_INVALID_ARGUMENT;
     if (options->q_per_kv > kMaxQPerKv) return COMPACTOR_E_UNSUPPORTED;
     if (layer < 0 || layer >= cache->layers || !rows_ok(q) || (k_new.ptr != nullptr && !rows_ok(k_new)) || lengths == nullptr ||
-        bounds == nullptr || !aligned(bounds, 16) || table_out == nullptr || lengths_out == nullptr || lengths_out == lengths ||
-        workspace == nullptr || !aligned(workspace, kAlign))
+        bounds == nullptr || !aligned(bounds, 16) || table_out == nullptr || lengths_out == nullptr || workspace == nullptr || !aligned(workspace, kAlign))
         return COMPACTOR_E_INVALID_ARGUMENT;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     SelectArgs a;
@@ -1433,8 +1432,13 @@ extern "C" int compactor_paged_select(const compactor_paged_cache* cache, int32_
     a.units = cache->heads * cache->batch;
     a.capacity = (int)std::min<long long>(options->max_length, (long long)cache->max_pages * cache->page_tokens);
     a.unit_pages = (a.capacity + cache->page_tokens - 1) / cache->page_tokens;
-    if (a.unit_pages > kSelectMaxPages || (long long)a.units * a.unit_pages > 0x7fffffffLL || (long long)a.units * options->pages > (1LL << 40))
+    if (a.unit_pages > kSelectMaxPages || (long long)a.units * a.unit_pages > 0x7fffffffLL || (long long)options->pages * cache->page_tokens > 0x7fff0000LL)
         return COMPACTOR_E_TOO_LARGE;
+    // what the kernels read while they write
+    auto overlap = [](const int32_t* x, size_t nx, const int32_t* y, size_t ny) { return (uintptr_t)x < (uintptr_t)(y + ny) && (uintptr_t)y < (uintptr_t)(x + nx); };
+    const size_t all_units = (size_t)cache->layers * a.units;
+    if (overlap(lengths_out, a.units, lengths, all_units) || overlap(table_out, (size_t)a.units * options->pages, cache->page_table, all_units * cache->max_pages))
+        return COMPACTOR_E_INVALID_ARGUMENT;
     const size_t keys_bytes = align_up(sizeof(uint32_t) * (size_t)a.units * a.unit_pages);
     if (workspace_bytes < 2 * keys_bytes) return COMPACTOR_E_WORKSPACE;
     const size_t first = (size_t)layer * a.units;

@@ -122,6 +122,23 @@ def test_bounds_and_select_refusals():
     assert size(ctypes.byref(_cache()), 100) == 2 * 256 and size(ctypes.byref(_cache4(heads=8, batch=4, max_pages=512)), 8192) == 2 * 8 * 4 * 512 * 4
 
 
+def test_select_refuses_tables_longer_than_a_cache_may_have():
+    """2^31 - 1 pages would run past the end of an int; so would a cache whose table they are."""
+    for pages in (2 ** 31 - 1, 2 ** 31 - 600, 2 ** 28):
+        assert _select(opt=(2, 100, pages, 1, 1)) == -5, pages
+
+
+def test_select_refuses_to_write_what_it_reads():
+    """lengths_out or table_out inside the cache's own (two layers of 2 x 3 units), not only where they begin."""
+    c = _cache4()
+    units = c.heads * c.batch
+    assert c.layers >= 2
+    for n in (1, units, c.layers * units - 1):
+        assert _select(out=(1 << 12) + 4 * n) == -1 and _select(out=(1 << 12) - 4 * min(n, units - 1)) == -1, n
+    inside = c.page_table + 4 * (c.layers * units * c.max_pages - 1)
+    assert _select(table=c.page_table) == -1 and _select(table=inside) == -1 and _select(table=c.page_table - 4) == -1
+
+
 def _norm(o=(4, 2, 128, 128, 0, 1e-6), tokens=5, q=(1 << 20, 1024, 128), k=(1 << 21, 1024, 128), qw=1 << 12, kw=1 << 12, pos=1 << 13, freq=1 << 14,
           qo=(1 << 22, 512, 128), ko=(1 << 23, 256, 128), kp=(0, 0, 0)):
     return B.LIB.compactor_norm_rope(ctypes.byref(B.CompactorNormRopeOptions(*o)), tokens, rows(q), rows(k), dev(qw), dev(kw), dev(pos), dev(freq),
