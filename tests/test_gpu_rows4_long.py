@@ -61,3 +61,55 @@ def test_attention4_of_long_units(lens, heads, g, accumulate):
             if accumulate:
                 w = mass[table[0, h, b, : per[b]].long()].flatten()[:n].double()
                 assert torch.all((w - p.sum(0)).abs() <= (1.01 * rel + (g + 2) * 2.0 ** -24) * p.sum(0))
+
+
+@pytest.mark.parametrize("page", [8, 16, 32])
+@pytest.mark.parametrize("append", [True, False])
+def test_attention4_of_long_units_with_pages_that_are_none(page, append):
+    """Every warp goes through more than 32 pages of a unit, one in thirty of which is none: rows of random codes, steps and least values."""
+    from paper_2507_08143_b200 import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(page)
+    heads, g, n = 8, 3, 150003
+    per = -(-(n + 1) // page)
+    pools = []
+    for _ in range(2):
+        pool = torch.randint(0, 256, (heads * per, page, 80), generator=gen, device="cuda", dtype=torch.uint8)
+        s = (torch.randint(8, 16, (heads * per, page, 4), generator=gen, device="cuda") / 64.0)          # four significant bits
+        lo = torch.randn(heads * per, page, 4, generator=gen, device="cuda").bfloat16() - 1
+        pool[..., 64:] = torch.stack([s.bfloat16(), lo], -1).flatten(2).contiguous().view(torch.uint8)
+        pools.append(pool)
+    table = torch.randperm(heads * per, generator=gen, device="cuda").to(torch.int32).view(1, heads, 1, per)
+    lost = torch.rand(1, heads, 1, per, generator=gen, device="cuda") < 1 / 30
+    lost[..., -1] = False
+    bad = torch.where(torch.rand(lost.shape, generator=gen, device="cuda") < 0.5, -1, heads * per).to(torch.int32)
+    mass = torch.zeros(heads * per, page, device="cuda")
+    cache = B.PagedCache4(*pools, torch.where(lost, bad, table).contiguous(), mass=mass)
+    lengths = torch.full((1, heads, 1), n, dtype=torch.int32, device="cuda")
+    q = (torch.randn(1, heads * g, 128, generator=gen, device="cuda") / 8).bfloat16()
+    new = [torch.randn(1, heads, 128, generator=gen, device="cuda").bfloat16() for _ in range(2)] if append else [None, None]
+    opt = B.decode_options(g, n + 1, accumulate=True)
+    out, lse, status = torch.empty_like(q), torch.empty(1, heads * g, device="cuda"), torch.zeros(1, heads, 1, dtype=torch.int32, device="cuda")
+    B.paged_attention(cache, 0, opt, q, lengths, out, B.alloc_paged_attention_workspace(cache, opt), k_new=new[0], v_new=new[1], lse_out=lse, status=status)
+    assert torch.all(status == 8)                            # COMPACTOR_STATUS_PAGE
+    assert not mass[table[lost].long()].any()                # nothing is written where no page is
+    total, scale = n + append, float(np.float32(128 ** -0.5))
+    for h in range(heads):
+        def values(pool):                                    # of the rows as they are held now, the new token's among them
+            rows = pool[table[0, h, 0].long()].flatten(0, 1)[:total]
+            par = rows[:, 64:].contiguous().view(torch.bfloat16).double().view(-1, 4, 2)
+            codes = torch.stack([rows[:, :64] & 15, rows[:, :64] >> 4], -1).flatten(1).double().view(-1, 4, 32)
+            sc, lo = par[..., :1] * codes, par[..., 1:].expand_as(codes)
+            return (sc + lo).flatten(1), (sc.abs() + lo.abs()).flatten(1)
+        (k, ka), (v, va) = values(pools[0]), values(pools[1])
+        rows, there = slice(h * g, (h + 1) * g), ~lost[0, h, 0].repeat_interleave(page)[:total]
+        qq = q[0, rows].double()
+        y = (scale * (qq @ k.T)).masked_fill(~there, float("-inf"))
+        dy = 161 * 2.0 ** -23 * float((scale * (qq.abs() @ ka.T)).max())                 # as above
+        p = torch.softmax(y, 1)
+        rel = 2 * dy + 2 * 2.0 ** -22 + (total / 8 + 64) * 2.0 ** -24
+        tol = (rel + 2.0 ** -16 + (total / 16 + 17) * 17 * 2.0 ** -23) * 1.01 * (p @ va) + 2.0 ** -8 * (p @ v).abs()
+        assert torch.all((out[0, rows].double() - p @ v).abs() <= tol)
+        want = torch.logsumexp(y, 1)
+        assert torch.all((lse[0, rows].double() - want).abs() <= dy + rel + 2.0 ** -22 * want.abs())
+        w = mass[table[0, h, 0].long()].flatten()[:total].double()
+        assert torch.all((w - p.sum(0)).abs() <= (1.01 * rel + (g + 2) * 2.0 ** -24) * p.sum(0))
