@@ -12,7 +12,11 @@
 //     same channels of two tokens side by side.
 //   - lo enters once for a group, not for every channel.  q.k = sum_c q_c s c + sum_groups lo_g (sum of the group's q): one more
 //     matrix instruction per tile with the least values as rows and the sums of the query, in three bf16 terms (24 bits), as columns.
-//     sum_j p_j v_j likewise gets one more instruction with the least values as rows, whose sums are added to the channels at the end.
+//     sum_j p_j v_j likewise gets one more instruction, whose sums are added to the channels at the end.
+//   - values are summed as s (c - 7) and lo + 7 s, not as s c and lo: of values on both sides of 0 the latter are two sums of one sign each, over a long
+//     context some hundred times their own sum, and fp32 rounds them accordingly (16 heads x 131072 tokens: 28 % of the outputs were not the bf16 nearest to the
+//     exact ones, now 0.4 %, for 51.0 -> 53.3 us of 8 heads, g = 5).  7 and not 7.5 because steps are rounded up, which takes the middle code down.  s (c - 7) is
+//     exact in bf16 and free, as the product with s has a summand; lo + 7 s is two bf16 terms, exact as well, in the two halves of the instruction's rows.
 // So every product that a matrix instruction sees is exact but for the weights' two bf16 terms, as in the other kernel.
 //
 // The rows of a page lie back to back, so that a tile of 16 is 1280 bytes in one piece (two on pages of 8): five 16-byte copies per lane for
@@ -122,6 +126,14 @@ __device__ __forceinline__ void mma4(float (&c)[4], const uint32_t (&a)[4], uint
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// lo + 7 s of two tokens as two terms whose sum is exact: what a sum of bf16 is rounded by is a bf16 itself.  less: -7 s.
+__device__ __forceinline__ void middle(uint32_t lo, uint32_t s, uint32_t less, uint32_t& sum, uint32_t& rest) {
+    constexpr uint32_t kOne = 0x3f803f80u, kMinus = 0xbf80bf80u;
+    sum = fma2(s, 0x40e040e0u, lo);
+    const uint32_t of_s = fma2(lo, kMinus, sum), of_lo = fma2(of_s, kMinus, sum);
+    rest = fma2(fma2(of_s, kOne, less), kMinus, fma2(of_lo, kMinus, lo));
 }
 
 // The same in fp16: codes of keys times queries.
@@ -499,6 +511,7 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                         o[t][j][2] *= by[0]; o[t][j][3] *= by[1];
                     }
                     ol[t][0] *= by[0]; ol[t][1] *= by[1];
+                    ol[t][2] *= by[0]; ol[t][3] *= by[1];
                 }
             }
             uint32_t pf[COUNT][NG][2], pl[COUNT][NG][2];     // weights as two bf16 terms, the first cut off, the second rounded: within 2^-16
@@ -531,6 +544,7 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                 }
                 const uint32_t s0 = __byte_perm(par[0], par[1], 0x5410), s1 = __byte_perm(par[2], par[3], 0x5410);
                 const uint32_t s0f = fma2(s0, 0x43004300u, 0u), s1f = fma2(s1, 0x43004300u, 0u), s0s = fma2(s0, 0x41004100u, 0u), s1s = fma2(s1, 0x41004100u, 0u);
+                const uint32_t s0m = fma2(s0, 0xc0e0c0e0u, 0u), s1m = fma2(s1, 0xc0e0c0e0u, 0u);         // -7 s
 #pragma unroll
                 for (int j4 = 0; j4 < 8; j4 += 4) {          // the same four channels of two tokens in the halves of a word
                     const unsigned sel = j4 == 0 ? 0x5410 : 0x7632;
@@ -542,7 +556,7 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const uint32_t c = (n < 2 ? x[i] : x[i] >> 8) & ((n & 1) == 0 ? kFirst : kSecond);
-                            vf[i] = fma2(fma2(c, 0x7e807e80u, 0u), (n & 1) == 0 ? (i < 2 ? s0f : s1f) : (i < 2 ? s0s : s1s), 0u);
+                            vf[i] = fma2(fma2(c, 0x7e807e80u, 0u), (n & 1) == 0 ? (i < 2 ? s0f : s1f) : (i < 2 ? s0s : s1s), i < 2 ? s0m : s1m);
                         }
 #pragma unroll
                         for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pf[u][t][0], pf[u][t][1]);
@@ -550,7 +564,9 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                         for (int t = 0; t < NG; ++t) mma4(o[t][j], vf, pl[u][t][0], pl[u][t][1]);
                     }
                 }
-                const uint32_t lf[4] = {__byte_perm(par[0], par[1], 0x7632), 0u, __byte_perm(par[2], par[3], 0x7632), 0u};
+                uint32_t lf[4];
+                middle(__byte_perm(par[0], par[1], 0x7632), s0, s0m, lf[0], lf[1]);
+                middle(__byte_perm(par[2], par[3], 0x7632), s1, s1m, lf[2], lf[3]);
 #pragma unroll
                 for (int t = 0; t < NG; ++t) mma4(ol[t], lf, pf[u][t][0], pf[u][t][1]);
 #pragma unroll
@@ -589,7 +605,7 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                     }
                     float x[16];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) { x[j] = o[t][j][c] + ol[t][c]; x[8 + j] = o[t][j][c + 2] + ol[t][c]; }
+                    for (int j = 0; j < 8; ++j) { x[j] = (o[t][j][c] + ol[t][c]) + ol[t][c + 2]; x[8 + j] = (o[t][j][c + 2] + ol[t][c]) + ol[t][c + 2]; }
                     if (whole) {
                         const float inv = l == 0.f ? 0.f : 1.f / l;
                         uint4* dst = reinterpret_cast<uint4*>(a.out + b * a.out_seq + (long long)(head0 + head) * a.out_head + 16 * gid);
