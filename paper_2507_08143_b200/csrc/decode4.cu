@@ -71,6 +71,8 @@ __device__ __forceinline__ void load_queries(const DecodeArgs& a, const Cursor& 
 // B operands of a unit's queries: of the lane's eight channels of group g the pairs (0, 4) and (2, 6), then (1, 5) and (3, 7) times 2^-4, as
 // fp16 of q 2^k; the sums of a group's channels, group tig, times 2^(k - 24), as three bf16 terms; and for the two heads of the lane's scores
 // 2^(24 - k).  k brings the head's greatest channel to 2^14 .. 2^15: fp16 holds the eight bits of a bf16 down to 2^-32 of that channel.
+// Queries of 2^118 and more, whose scale back to a score would be beyond fp32, and those that are not finite make all of their head's scores
+// not a number (as infinite ones, the scores of a head could all be -inf, and its row zero).
 template <int NG>
 __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t (&qf)[NG][4][2][2], uint32_t (&qs)[NG][2], float (&unscale)[NG][2], int lane) {
     const int tig = lane & 3;
@@ -85,7 +87,6 @@ __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t
         top = max_nan2(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max_nan2(top, __shfl_xor_sync(0xffffffffu, top, 2));
         top = max_nan2(top, top >> 16 | top << 16);
-        // (queries of 2^118 and more, or not finite, become infinite, and their scores no numbers)
         const int k = max(-102, min(141 - (int)((top >> 7) & 255u), 126));
         const float up = __int_as_float((k + 127) << 23), down = __int_as_float((127 + 24 - k) << 23);
         float mine = 0.f;
@@ -109,7 +110,7 @@ __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
             if (g == tig) mine = sum;
         }
-        mine *= up * 0x1p-24f;
+        mine = (top & 0x7fffu) >= 0x7a80u ? __int_as_float(0x7fffffff) : mine * (up * 0x1p-24f);      // (the bits of 2^118)
         const float t0 = __bfloat162float(__float2bfloat16_rn(mine)), r0 = mine - t0;
         const float t1 = __bfloat162float(__float2bfloat16_rn(r0)), t2 = r0 - t1;
         qs[t][0] = pack_bf16(t0, t1);
