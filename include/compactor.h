@@ -510,9 +510,10 @@ int compactor_paged_evict(const compactor_paged_cache* cache, int32_t first_laye
  * A cache of one kind is refused by the calls for the other.  Everything else is as in the calls without the 4:
  *   paged4_fill       holds the rows as above instead of copying them;
  *   paged4_attention  attends to the values that the rows stand for.  The new token's row is held in 4 bits first and attended to as it is
- *                     held, so that later steps see the same.  Its products are exact before they are summed in fp32; weights enter
- *                     the product with V as two bf16 terms (within 2^-16 of the weight).  A head with a query channel of 2^118 or more, or
- *                     not finite, gives not-a-number.  Its workspace has a size of its own;
+ *                     held, so that later steps see the same.  Its products are exact before they are summed in fp32, but for two: weights enter
+ *                     the product with V as two bf16 terms (within 2^-16 of the weight), and a query channel below 2^-31 (odd channels: 2^-27) of
+ *                     its head's greatest is taken to within 2^-39 (2^-35) of that one.  Values are summed as s (c - 7) and lo + 7 s.  A head with a query
+ *                     channel of 2^118 or more, or not finite, gives not-a-number.  Its workspace has a size of its own;
  *   paged4_evict      moves rows as they are.
  */
 int compactor_paged4_fill(const compactor_paged_cache* cache, int32_t first_layer, const compactor_shape* shape,

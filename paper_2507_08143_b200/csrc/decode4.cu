@@ -17,7 +17,8 @@
 //     context some hundred times their own sum, and fp32 rounds them accordingly (16 heads x 131072 tokens: 28 % of the outputs were not the bf16 nearest to the
 //     exact ones, now 0.4 %, for 51.0 -> 53.3 us of 8 heads, g = 5).  7 and not 7.5 because steps are rounded up, which takes the middle code down.  s (c - 7) is
 //     exact in bf16 and free, as the product with s has a summand; lo + 7 s is two bf16 terms, exact as well, in the two halves of the instruction's rows.
-// So every product that a matrix instruction sees is exact but for the weights' two bf16 terms, as in the other kernel.
+// So every product that a matrix instruction sees is exact but for the weights' two bf16 terms, as in the other kernel, and for query channels some 2^-27 below
+// their head's greatest (query_operands).
 //
 // The rows of a page lie back to back, so that a tile of 16 is 1280 bytes in one piece (two on pages of 8): five 16-byte copies per lane for
 // K and V together.  Twelve warps of 168 registers take two tiles a step, which the compiler interleaves.
@@ -70,8 +71,9 @@ __device__ __forceinline__ void load_queries(const DecodeArgs& a, const Cursor& 
 
 // B operands of a unit's queries: of the lane's eight channels of group g the pairs (0, 4) and (2, 6), then (1, 5) and (3, 7) times 2^-4, as
 // fp16 of q 2^k; the sums of a group's channels, group tig, times 2^(k - 24), as three bf16 terms; and for the two heads of the lane's scores
-// 2^(24 - k).  k brings the head's greatest channel to 2^14 .. 2^15: fp16 holds the eight bits of a bf16 down to 2^-32 of that channel.
-// Queries of 2^118 and more, whose scale back to a score would be beyond fp32, and those that are not finite make all of their head's scores
+// 2^(24 - k).  k brings the head's greatest channel to 2^14 .. 2^15.  The last place of an fp16 is never below 2^-24, so that the eight bits of a bf16 are all held
+// down to 2^-31 of that channel's power of two, those of odd channels, because of the 2^-4, to 2^-27; below, a channel is off by at most 2^-39, or
+// 2^-35, of it.  Queries of 2^118 and more, whose scale back to a score would be beyond fp32, and those that are not finite make all of their head's scores
 // not a number (as infinite ones, the scores of a head could all be -inf, and its row zero).
 template <int NG>
 __device__ __forceinline__ void query_operands(const uint4 (&q)[NG][4], uint32_t (&qf)[NG][4][2][2], uint32_t (&qs)[NG][2], float (&unscale)[NG][2], int lane) {

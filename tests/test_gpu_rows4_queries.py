@@ -1,4 +1,4 @@
-"""Attention over rows in 4 bits with queries of a wide range: heads that are too large."""
+"""Attention over rows in 4 bits with queries of a wide range: how many bits of a channel far below its head's greatest count, and heads that are too large."""
 import numpy as np
 import pytest
 import torch
@@ -30,6 +30,36 @@ def attend(k, v, q, scale):
 
 def bf16(x):
     return bf16_bits_to_f64(ro.f64_to_bf16_bits(np.asarray(x, np.float64)))
+
+
+@pytest.mark.parametrize("g", [3, 11])
+@pytest.mark.parametrize("channel, exponent, exact", [(40, -31, True), (41, -27, True), (40, -35, False), (41, -31, False), (41, -28, False)])
+def test_channels_far_below_the_greatest(g, channel, exponent, exact):
+    """One channel of the queries lies 2^exponent below the greatest, 1, with keys that make up for it.  Queries enter as fp16 of 2^14 q, those of odd
+    channels as 2^10 q, whose last place is never below 2^-24: a bf16 of eight bits fits from 2^-31 (odd: 2^-27) on, and is off by at most 2^-25 2^-14 =
+    2^-39 (2^-35) below.  Everything else as in the other tests: 161 2^-23 of the largest sum for a score."""
+    rng = np.random.default_rng(3)
+    n = 60
+    k, v = bf16(rng.standard_normal((n, 128))), bf16(rng.standard_normal((n, 128)))
+    k[:, 32:64] = 0.0
+    k[:, channel] = bf16(rng.standard_normal(n) * 2.0 ** -exponent)
+    q = bf16(rng.uniform(-0.25, 0.25, (g, 128)))
+    q[:, 32:64] = 0.0
+    q[:, 0] = 1.0
+    q[:, channel] = (2 - 2.0 ** -7 * (1 + 2 * np.arange(g))) * 2.0 ** exponent            # odd in the last of eight bits
+    out, lse, ((ks, kl), (vs, vl)) = attend(k, v, q, 1.0)
+    y = q @ (ks + kl).T
+    mag = (np.abs(q) @ (np.abs(ks) + np.abs(kl)).T).max()
+    dy = 161 * 2.0 ** -23 * mag
+    if not exact:
+        dy += (2.0 ** -39 * np.abs(ks[:, 0::2]).sum(1) + 2.0 ** -35 * np.abs(ks[:, 1::2]).sum(1)).max()
+    top = y.max(1, keepdims=True)
+    want = (top + np.log(np.exp(y - top).sum(1, keepdims=True)))[:, 0]
+    rel = 2 * dy + 2 * 2.0 ** -22 + (n / 8 + 64) * 2.0 ** -24
+    assert np.all(np.abs(lse - want) <= dy + rel + 2.0 ** -22 * np.abs(want))
+    p = np.exp(y - want[:, None])
+    tol = (np.expm1(rel) + 2.0 ** -16 + (n / 16 + 17) * 17 * 2.0 ** -23) * 1.01 * (p @ (np.abs(vs) + np.abs(vl))) + 2.0 ** -8 * np.abs(p @ (vs + vl))
+    assert np.all(np.abs(out - p @ (vs + vl)) <= tol)
 
 
 @pytest.mark.parametrize("g", [4, 12])
