@@ -131,12 +131,11 @@ __device__ __forceinline__ void mma4(float (&c)[4], const uint32_t (&a)[4], uint
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// lo + 7 s of two tokens as two terms whose sum is exact: what a sum of bf16 is rounded by is a bf16 itself.  less: -7 s.
-__device__ __forceinline__ void middle(uint32_t lo, uint32_t s, uint32_t less, uint32_t& sum, uint32_t& rest) {
-    constexpr uint32_t kOne = 0x3f803f80u, kMinus = 0xbf80bf80u;
-    sum = fma2(s, 0x40e040e0u, lo);
-    const uint32_t of_s = fma2(lo, kMinus, sum), of_lo = fma2(of_s, kMinus, sum);
-    rest = fma2(fma2(of_s, kOne, less), kMinus, fma2(of_lo, kMinus, lo));
+// lo + 7 s of two tokens as two terms whose sum is exact: what a sum of two bf16 is rounded by is a bf16 itself.  less: -7 s.
+__device__ __forceinline__ void middle(uint32_t lo, uint32_t less, uint32_t& sum, uint32_t& rest) {
+    sum = sub2(lo, less);
+    const uint32_t of_s = sub2(sum, lo), of_lo = sub2(sum, of_s);        // the shares of 7 s and of lo in the rounded sum
+    rest = sub2(sub2(lo, of_lo), add2(of_s, less));
 }
 
 // The same in fp16: codes of keys times queries.
@@ -568,8 +567,8 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
                     }
                 }
                 uint32_t lf[4];
-                middle(__byte_perm(par[0], par[1], 0x7632), s0, s0m, lf[0], lf[1]);
-                middle(__byte_perm(par[2], par[3], 0x7632), s1, s1m, lf[2], lf[3]);
+                middle(__byte_perm(par[0], par[1], 0x7632), s0m, lf[0], lf[1]);
+                middle(__byte_perm(par[2], par[3], 0x7632), s1m, lf[2], lf[3]);
 #pragma unroll
                 for (int t = 0; t < NG; ++t) mma4(ol[t], lf, pf[u][t][0], pf[u][t][1]);
 #pragma unroll
