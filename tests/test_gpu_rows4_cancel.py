@@ -80,3 +80,29 @@ def test_a_row_of_one_token_is_what_it_is_held_as(g):
     got = out.double().cpu().numpy()
     for j in range(g):
         np.testing.assert_array_equal(got[:, j], want)
+
+
+@pytest.mark.parametrize("g", [5, 12])
+def test_a_channel_of_zeros_among_others_of_one_sign_stays_zero(g):
+    """Its code is that of the least (or the greatest) value in every row, or it is the least value 0 itself: both sums that it is made of are each other's opposites,
+    product by product."""
+    from paper_2507_08143_b200 import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    heads, page, n = 3, 16, 20011
+    per = -(-n // page)
+    table = torch.randperm(heads * per, generator=gen, device="cuda").to(torch.int32).view(1, heads, 1, per)
+    pools = [torch.empty(heads * per, page, 80, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    cache = B.PagedCache4(*pools, table)
+    lengths = torch.zeros(1, heads, 1, dtype=torch.int32, device="cuda")
+    k = torch.randn(1, heads, n, 128, generator=gen, device="cuda").bfloat16()
+    v = torch.randn(1, heads, n, 128, generator=gen, device="cuda").abs().bfloat16()
+    v[..., 0::8] = 0
+    v[..., 64:96] = torch.where(torch.arange(32, device="cuda") % 8 == 0, 0.0, 100.0)
+    B.paged_fill(cache, B.Shape(1, heads, 128, 48, [n]), k, v, [n], lengths_out=lengths)
+    q = torch.randn(1, heads * g, 128, generator=gen, device="cuda").bfloat16()
+    opt = B.decode_options(g, n)
+    out = torch.empty_like(q)
+    B.paged_attention(cache, 0, opt, q, lengths, out, B.alloc_paged_attention_workspace(cache, opt))
+    assert not out[..., 0::8].any()
+    others = out[..., torch.arange(128, device="cuda") % 8 != 0]
+    assert torch.all(others > 0.5)
