@@ -567,7 +567,10 @@ int compactor_paged4_read(const compactor_paged_cache* cache, int32_t first_laye
  * (summed in 64 bits, rounded to fp32; of equal scores the lower page; not-a-number ranks above +inf, a page that is none below all), `pages` in all.
  *   q              rows [batch][heads * q_per_kv] of the layer's queries, as the attention gets them.
  *   k_new          rows [batch][heads] of the token that the attention is going to append, or ptr NULL (nothing will be appended).  It enters the bounds
- *                  of its page (as given, in a cache of either kind), so that they need no other call while a sequence grows.
+ *                  of its page (as given, in a cache of either kind), so that they need no other call while a sequence grows.  In 4 bits they
+ *                  then differ from bounds made anew, which are those of the rows as they are held, by up to half a step of the new row and
+ *                  a rounding to bf16, and a later step may choose other pages by the ones than by the others (compactor_paged4_bounds after a step, `first`
+ *                  = the lengths before it, makes them those of the held rows again).
  *   lengths        device int32 [units of the cache], without the new token.
  *   table_out      device int32 [heads * batch][pages]: the pages taken, in the unit's order, and -1 behind them; no part of the cache's table.
  *   lengths_out    device int32 [heads * batch], no part of `lengths`: the unit's length over that table, again without the new token; a

@@ -2,7 +2,8 @@
 //
 //   score(page) = max over the KV head's query heads of sum_c (q_c > 0 ? q_c greatest_c : q_c least_c)
 //
-// is the most that q.k can be for a key between the bounds.  The first and the last pages of a unit are always taken, the other places
+// is the most that q.k can be for a key between the bounds.  (Of a page in 4 bits the bounds are rounded to the nearest bf16, and keys that were appended entered as
+// given, up to half a step away from what is held: a key of such a page may lie that far outside.)  The first and the last pages of a unit are always taken, the other places
 // go to the greatest scores (of equal ones the lower page).  What comes out is a row of a page table and a length, in the order of the
 // unit's pages, so that the attention takes it like any other unit and the new token finds its slot behind the last one.
 //
