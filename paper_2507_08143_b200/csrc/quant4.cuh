@@ -4,7 +4,7 @@
 //   s = (greatest - least) / 15 rounded up to four significant bits,  c = ceil((x - lo) / s - 1/2)
 //
 // With four significant bits in s and four in c the product s c is exact in bf16, so that it can enter a matrix instruction as it is; lo,
-// a value of the row, is one as well.  The rounding up costs on average 3 % of the step.  A step below 2^-120 is 0 (all codes 0); a group
+// a value of the row, is one as well.  The rounding up costs 5 % of the step on average (groups of 32 normal values).  A step below 2^-120 is 0 (all codes 0); a group
 // that holds a value which is not finite, or whose step exceeds 2^120, is held as not a number throughout.
 #pragma once
 #include "two.cuh"
