@@ -713,12 +713,15 @@ cudaError_t launch_paged_attention(const DecodeArgs& a, int sm_count, cudaStream
     const long long most = a.accumulate ? (long long)a.units * ((a.capacity + kTile - 1) / kTile + kMassUnitCost) : 0;   // cost of the weights
     const long long wanted = (most + kTile - 1) / kTile;     // 256 tokens a block at the least
     // (Over 4 bits with the weights of more than 2048 tokens for each SM, these are what counts, and the smaller blocks put four of them to an SM: 8 heads x
-    // 131072 tokens, g = 5, 65.9 -> 57.4 us, x 65536 38.8 -> 38.0; of half as many tokens 27.1 -> 29.0.  Over bf16 it stays as it is, results to the bit.)
+    // 131072 tokens 57.5 -> 57.1 us for g = 1, 67.1 -> 58.5 for 5, 69.9 -> 58.3 for 8; x 65536 35.2 -> 37.6, 39.7 -> 38.6, 41.3 -> 38.9; 4 heads x 4 sequences x 65536
+    // 63.0 -> 55.4, x 32768 37.9 -> 35.3.  Below it they are slower: 8 heads x 32768 22.7 -> 28.2, 27.3 -> 28.9, 28.4 -> 29.4; 2 heads x 131072 25.1 -> 46.5.  Over bf16 it
+    // stays as it is, results to the bit.)
     const bool large = 2 * pairs <= sm_count && !(a.four && wanted > 8LL * sm_count), few_pieces = a.workers < 6 * a.units * a.groups;
     const int join_blocks = large ? 2 * pairs : few_pieces ? (pairs + 3) / 4 : pairs;
     // (not more than fit beside the others, so that those need not wait for a place)
-    // and where there are more joining blocks than that, half of the places after a first kernel over 4 bits, whose weights are more of the whole
-    // (ragged batch of 16 sequences x 8 heads 46.2 -> 44.7 us; over bf16 118.2 -> 119.1)
+    // and where there are more joining blocks than that, half of the places after a first kernel over 4 bits, whose weights are more of the whole: up to
+    // 3 % less for batches of up to 1 M tokens (8 heads x 16 ragged sequences, 231 K 25.6 -> 24.7 us; 8 x 32, 524 K 40.7 -> 39.5; 8 x 16, g = 16, 1 M 100.4 -> 97.4), up to
+    // 2.4 % more beyond (8 x 16, 1.4 M 72.2 -> 73.9, 2.1 M 102.4 -> 104.8), and the host does not know the lengths.  Over bf16 118.2 -> 119.1
     const int room = large ? max(sm_count / 2, sm_count - join_blocks) : join_blocks <= 2 * sm_count ? 4 * sm_count - join_blocks : (a.four ? 2 : 4) * sm_count;
     const int mass_blocks = (int)min(wanted, (long long)room);
     const dim3 blocks(mass_blocks + join_blocks);
