@@ -147,7 +147,7 @@ __device__ __forceinline__ void score_run(const SelectArgs& a, const int* cum, i
     }
 }
 
-__global__ void __launch_bounds__(kScoreWarps * 32, 4)
+__global__ void __launch_bounds__(kScoreWarps * 32, 4)       // (128 registers a thread, 4 bytes spilled)
 score_pages_kernel(const __grid_constant__ SelectArgs a) {
     constexpr int kThreads = kScoreWarps * 32;
     __shared__ int cum[kThreads + 1];                        // runs before each thread's share of the units

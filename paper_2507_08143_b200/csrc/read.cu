@@ -128,7 +128,7 @@ struct Bounds16 {
 struct Bounds4 {
     static constexpr int kRows = 32;
     static constexpr bool kAhead = true;                     // (61 -> 46 us for a ragged batch of 1.9 M tokens)
-    static constexpr int kBlocks = 2;
+    static constexpr int kBlocks = 2;                        // (128 registers a thread; 8 bytes are spilled where many pages are gone through)
     struct Rows { uint4 codes[4]; uint32_t param[4]; };
     uint32_t least[16], most[16];                            // pair n of word j, channels 8 j + n and 8 j + n + 4 of the group, at 4 j + n
     __device__ __forceinline__ void clear() {

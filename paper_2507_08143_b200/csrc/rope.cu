@@ -118,7 +118,8 @@ __device__ __forceinline__ void rotate_rows(const Rows& r, const Two (&a)[4], co
 
 // `parts` warps share a token's heads.
 template <bool INTERLEAVED, bool FULL>
-__global__ void __launch_bounds__(kThreads, 7)               // (72 registers; left alone 84, and 39.2 us for 8192 tokens x 40 heads against 37.4)
+// (72 registers a thread, for which the half-split ones spill 56 bytes; left alone 84 and none, and 39.2 us for 8192 tokens x 40 heads against 37.4)
+__global__ void __launch_bounds__(kThreads, 7)
 rope_kernel(const __grid_constant__ RopeArgs a, int parts) {
     __shared__ __align__(16) float turn[kWarps][2][kD / 2];  // cosines and sines
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & 15;
