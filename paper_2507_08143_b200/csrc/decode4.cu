@@ -21,12 +21,13 @@
 // their head's greatest (query_operands).
 //
 // The rows of a page lie back to back, so that a tile of 16 is 1280 bytes in one piece (two on pages of 8): five 16-byte copies per lane for
-// K and V together.  Twelve warps of 168 registers take two tiles a step, which the compiler interleaves.
+// K and V together.  Twelve warps of 168 registers take two tiles a step, which the compiler interleaves; beyond eight heads eight warps of 255 (nothing is spilled).
 //
-// Measured (both kernels, one layer, device time of calls in a row): 8 heads x 131072 tokens 46.7 - 47.6 us for 1 to 8 query heads (bf16: 89), 75 for 12 and
-// 16, 132 for 32, 249 for 64; with weights 56 - 57.  16 ragged sequences x 8 heads, 470 K tokens, with weights, 41.  The copies alone take 34, the arithmetic
-// alone 47.  423 instructions per tile of 16 tokens (712 at first), 62 % of the issue slots, the logic pipe 41 %, the tensor pipe 20 %: a matrix instruction also holds
-// up the others for three of its nine cycles.  Not better: 16 warps of 128 registers (57 us), 8 of 255 (59); scores of a tile beside the product
+// Measured (both kernels, one layer, device time of calls in a row): 8 heads x 131072 tokens 49.4 - 50.2 us for 1 to 8 query heads (bf16: 89), 75 for 12,
+// 76 for 16, 133 for 32, 252 for 64; with weights 57 - 58.5; capped 54.  16 ragged sequences x 8 heads, 470 K tokens, with weights, 41.  The copies alone take 34,
+// the arithmetic alone 47 (before values were summed about their middle, the whole 47.3).  437 instructions per tile of 16 tokens (712 at first), 61 % of the issue
+// slots, the logic pipe 39 %, the tensor pipe 20 %; the largest stall is the latency of dependent instructions, at three warps a scheduler.  A matrix instruction also
+// holds up the others for three of its nine cycles.  Not better (before that as well): 16 warps of 128 registers (57 us), 8 of 255 (59); scores of a tile beside the product
 // of the one before (57); codes as e4m3 for the instruction of 8-bit types, which is made of fp16 ones here (68); both terms of the weights in the
 // eight columns of one instruction for up to four heads (2 us less for long contexts, nothing else).
 #include "decode.cuh"
@@ -258,7 +259,7 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
             if (run > 0 && whole) {
                 --run;
                 p0 = 0;
-            } else if (whole && a.c.page_shift >= 4) {       // one page: little to look up, which on pages of 16 is for every tile (8 heads x 131072 51.1 -> 50.3 us, ragged 71.4 -> 69.7)
+            } else if (whole && a.c.page_shift >= 4) {       // one page: little to look up, which on pages of 16 is for every tile (8 heads x 131072 51.1 -> 50.3 us, now 52.5; ragged 71.4 -> 69.7)
                 if (e >= e0 + 32) {
                     e0 += 32;
                     ids = ids_after;
