@@ -49,6 +49,9 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 // Error of a score: sums of 16 instructions in four chains of four, each of which may drop a unit of 2^-23 of its partial sum for each of 17
 // summands, three additions: 71 2^-23 of the sum of absolute values (which is itself no more than that far off).
 constexpr float kScoreError = 0x1p-16f;
+// The last place of an fp32 is never below 2^-149, which each of the 256 products and their sums may lose as well.  Where the rest of the error is not
+// far above that, it is added, unless there is nothing to lose: all queries or all bounds are 0.
+constexpr float kLeastError = 0x1p-139f;
 
 // The new key enters the bounds of its page, by a warp.  (That page is taken without a score.)
 __device__ __forceinline__ void enter_new_key(const SelectArgs& a, int unit, int lane) {
@@ -137,6 +140,28 @@ __device__ __forceinline__ void score_run(const SelectArgs& a, const int* cum, i
             best[p] = fmaxf(best[p], __shfl_xor_sync(0xffffffffu, best[p], d));
             error[p] = fmaxf(error[p], __shfl_xor_sync(0xffffffffu, error[p], d));
         }
+    }
+    if (__any_sync(0xffffffffu, fminf(error[0], error[1]) < 0x1p-110f)) {
+        uint32_t asked = 0u;                                 // not 0 where a query is not
+        for (int head = gid; head < a.g; head += 8) {
+            const uint4* q = reinterpret_cast<const uint4*>(a.q + b * a.q_seq + (long long)(h * a.g + head) * a.q_head) + tig;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asked |= (q[4 * i].x | q[4 * i].y | q[4 * i].z | q[4 * i].w) & 0x7fff7fffu;
+        }
+        const bool any = __any_sync(0xffffffffu, asked != 0u);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            uint32_t bits = 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                bits |= low[p][i].x | low[p][i].y | low[p][i].z | low[p][i].w | high[p][i].x | high[p][i].y | high[p][i].z | high[p][i].w;
+            bits |= __shfl_xor_sync(0xffffffffu, bits, 1);
+            bits |= __shfl_xor_sync(0xffffffffu, bits, 2);
+            if (any && (bits & 0x7fff7fffu) != 0u) error[p] += kLeastError;
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
         const int index = first + gid + 8 * p;
         if (tig == 0 && index < pages) {
             const bool always = index < a.first_pages || index >= pages - a.last_pages;
@@ -147,7 +172,7 @@ __device__ __forceinline__ void score_run(const SelectArgs& a, const int* cum, i
     }
 }
 
-__global__ void __launch_bounds__(kScoreWarps * 32, 4)       // (128 registers a thread, 4 bytes spilled)
+__global__ void __launch_bounds__(kScoreWarps * 32, 4)       // (128 registers a thread)
 score_pages_kernel(const __grid_constant__ SelectArgs a) {
     constexpr int kThreads = kScoreWarps * 32;
     __shared__ int cum[kThreads + 1];                        // runs before each thread's share of the units
