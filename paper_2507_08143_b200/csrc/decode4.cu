@@ -364,7 +364,10 @@ decode4_kernel(const __grid_constant__ DecodeArgs a) {
             for (int s = 0; s < 8; ++s) o[t][s][0] = o[t][s][1] = o[t][s][2] = o[t][s][3] = 0.f;
             ol[t][0] = ol[t][1] = ol[t][2] = ol[t][3] = 0.f;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) to_base2[t][c] = fminf(fmaxf(to_base2[t][c] * scale2, 0x1p-126f), 0x1p127f);     // (never 0 or infinite: -inf stays -inf, 0 stays 0)
+            for (int c = 0; c < 2; ++c)
+                // (Queries times a scale beyond 2^117 end at 2^127 and have their scores too small by the rest: among keys above 2^-110 they are still
+                // so far apart that one token takes all.)
+                to_base2[t][c] = fminf(fmaxf(to_base2[t][c] * scale2, 0x1p-149f), 0x1p127f);     // (never 0 or infinite: -inf stays -inf, 0 stays 0)
             ref[t][0] = ref[t][1] = 0.f;
             most[t][0] = most[t][1] = -INFINITY;
             sum[t][0] = sum[t][1] = 0.f;

@@ -90,3 +90,22 @@ def test_heads_of_2_to_the_118_and_more_give_not_a_number(g):
     p = np.exp(y - want[:, None])
     tol = (np.expm1(rel) + 2.0 ** -16 + (n / 16 + 17) * 17 * 2.0 ** -23) * 1.01 * (p @ (np.abs(vs) + np.abs(vl))) + 2.0 ** -8 * np.abs(p @ (vs + vl))
     assert np.all(np.abs(out[fine] - p @ (vs + vl)) <= tol)
+
+
+@pytest.mark.parametrize("softcap", [0.0, 2.0 ** -100])
+@pytest.mark.parametrize("g", [2, 9])
+def test_scores_of_small_queries_and_small_scales_are_small(g, softcap):
+    """Queries at 2^-112 times keys at 2^123 times a scale of 2^-126: all scores are below 2^-100, and the output is the mean, whose two halves are opposite.
+    What is left of a score may be off by 2^121 (the largest sum of a query 2^126 of its size) times the least fp32."""
+    from paper_2507_08143_b200 import binding as B
+    n = 64
+    sign = np.where(np.arange(n) % 2 == 0, 1.0, -1.0)[:, None]
+    rows = [torch.from_numpy(ro.hold4(ro.f64_to_bf16_bits(sign * x * np.ones(128)))).cuda() for x in (2.0 ** 123, 1.0)]
+    pools = [r.view(4, 16, 80).contiguous() for r in rows]
+    cache = B.PagedCache4(*pools, torch.arange(4, dtype=torch.int32, device="cuda").view(1, 1, 1, 4))
+    q = torch.full((1, g, 128), 2.0 ** -112, device="cuda").bfloat16()
+    opt = B.decode_options(g, n, scale=2.0 ** -126, softcap=softcap)
+    out, lse = torch.empty_like(q), torch.empty(1, g, device="cuda")
+    B.paged_attention(cache, 0, opt, q, torch.full((1, 1, 1), n, dtype=torch.int32, device="cuda"), out, B.alloc_paged_attention_workspace(cache, opt), lse_out=lse)
+    assert torch.all(out.double().abs() <= 2 * 2.0 ** (121 - 149) + (n / 8 + 64) * 2.0 ** -24)
+    assert torch.all((lse.double() - np.log(n)).abs() <= 2.0 ** -22 * np.log(n) + (n / 8 + 64) * 2.0 ** -24)
